@@ -365,6 +365,50 @@ int onebit_error_materialize_padded(onebit_plan plan, const float *err_state,
                              int64_t scales_ld, int32_t rows, float *delta_out,
                              int64_t out_ld, onebit_stream stream);
 
+/* ---------------------------------------------------------------------------
+ * Token embedding (the table is usually the largest tensor of the buffers)
+ * ---------------------------------------------------------------------------
+ * A table has `vocab` rows of `width` elements, table_ld elements apart; it
+ * may lie inside the flat parameter buffer, and its gradient inside a row of
+ * the gradient buffer.  Element types are ONEBIT_GRAD_*; pointers and leading
+ * dimensions need no alignment beyond the element's own.  ids: `tokens`
+ * consecutive integers of ids_bytes 4 (int32) or 8 (int64).  An id outside
+ * [0, vocab) marks a place that holds no token: its output row is zero and it
+ * adds to no gradient.  No plan is needed; the calls run on the current HIP
+ * device.  tokens = 0, vocab = 0 and width = 0 are allowed. */
+
+/* out[t] = scale * table[ids[t]], computed in fp32 and rounded once to the
+ * output's type; rows of `width` elements, out_ld apart.
+ * Errors: EINVAL (null, a size below 0 or 2^31 and above, a leading dimension
+ * below width with more than one row, unknown type), EALIGN, EHIP. */
+int onebit_embedding_forward(const void *table, int32_t table_dtype, int64_t table_ld,
+                             int64_t vocab, int64_t width, const void *ids, int32_t ids_bytes,
+                             int64_t tokens, float scale, void *out, int32_t out_dtype,
+                             int64_t out_ld, onebit_stream stream);
+
+/* Bytes of workspace that onebit_embedding_grad needs for at most this many
+ * tokens, rows and columns.  Errors: EINVAL (as above, bytes NULL). */
+int onebit_embedding_grad_workspace(int64_t tokens, int64_t vocab, int64_t width,
+                                    size_t *bytes);
+
+/* grad[v] = scale * sum of dout[t] over the places t with ids[t] = v, for
+ * every row v of the table (rows without a place become zero); with
+ * accumulate != 0 the sum is added to grad[v] instead, and rows without a
+ * place are not touched.  Places with ids[t] = padding_id add nothing
+ * (padding_id < 0: no such row).  The places are sorted by id, stably, and a
+ * row's are added in fp32 in an order that depends on the sorted list alone
+ * (no atomics on values): results are the same bit for bit from call to call.
+ * One rounding to the gradient's type, after the old value is added in fp32.
+ * dout: `tokens` rows of `width` elements, dout_ld apart; grad: `vocab` rows,
+ * grad_ld apart, in/out; workspace: onebit_embedding_grad_workspace() bytes,
+ * 16-byte aligned.  Errors: EINVAL (as above; more than 2^31 places times
+ * groups of 1,024 columns), EALIGN, EHIP. */
+int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld, const void *ids,
+                          int32_t ids_bytes, int64_t tokens, int64_t vocab, int64_t width,
+                          int64_t padding_id, float scale, void *grad, int32_t grad_dtype,
+                          int64_t grad_ld, int32_t accumulate, void *workspace,
+                          onebit_stream stream);
+
 /* Name of a status code (static string). */
 const char *onebit_status_str(int32_t status);
 

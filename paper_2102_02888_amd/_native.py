@@ -53,6 +53,11 @@ SIGNATURES = {
                                  _i64, _vp],
     "onebit_error_materialize": [_vp, _vp, _i64, _vp, _i64, _i32, _vp, _i64, _vp],
     "onebit_error_materialize_padded": [_vp, _vp, _i64, _vp, _i64, _i32, _vp, _i64, _vp],
+    "onebit_embedding_forward": [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _i64, _f32, _vp, _i32,
+                                 _i64, _vp],
+    "onebit_embedding_grad_workspace": [_i64, _i64, _i64, _vp],
+    "onebit_embedding_grad": [_vp, _i32, _i64, _vp, _i32, _i64, _i64, _i64, _i64, _f32, _vp, _i32,
+                              _i64, _i32, _vp, _vp],
     "onebit_status_str": [_i32],
     "onebit_last_error": [],
 }

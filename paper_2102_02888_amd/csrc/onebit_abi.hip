@@ -16,6 +16,7 @@
 
 #include "../../include/onebit.h"
 #include "onebit_internal.h"
+#include "onebit_status.h"
 
 static_assert(onebit::kScratchBytes == ONEBIT_NOALLOC_SCRATCH_BYTES,
               "the scratch array and the header's limit must agree");
@@ -43,10 +44,11 @@ struct onebit_plan_s {
 };
 
 namespace {
-
 thread_local char g_last_error[512] = "";
+}  // namespace
 
-int fail(int status, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+namespace onebit {
+
 int fail(int status, const char *fmt, ...)
 {
     va_list ap;
@@ -60,6 +62,13 @@ int hip_fail(hipError_t e, const char *where)
 {
     return fail(ONEBIT_EHIP, "%s: %s", where, hipGetErrorString(e));
 }
+
+}  // namespace onebit
+
+namespace {
+
+using onebit::fail;
+using onebit::hip_fail;
 
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 

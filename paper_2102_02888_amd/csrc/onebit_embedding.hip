@@ -1,0 +1,682 @@
+// Token embedding: lookup with scaling, and the table's gradient by sorted
+// tokens.  Both stream: the lookup reads a row and writes a row per token; the
+// gradient reads every token's row once and writes every row of the table once.
+// See include/onebit.h for the contract of the entry points.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "../../include/onebit.h"
+#include "onebit_internal.h"
+#include "onebit_status.h"
+
+namespace onebit {
+namespace {
+
+// N consecutive elements of type T as fp32.  Rows need no alignment (an odd
+// width leaves every second row of a 16-bit table on an odd element), so the
+// vector access is stated as a copy of bytes, which the compiler turns into one
+// load or store of up to 16 bytes (gfx950 takes them at any address).
+template <class T, int N>
+__device__ __forceinline__ void load_vec(const T *p, float (&v)[N])
+{
+    T t[N];
+    __builtin_memcpy(t, p, sizeof t);
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = (float)t[k];
+}
+
+template <class T, int N>
+__device__ __forceinline__ void store_vec(T *p, const float (&v)[N])
+{
+    T t[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) t[k] = (T)v[k];
+    __builtin_memcpy(p, t, sizeof t);
+}
+
+// The first `left` of N elements (a row's end); the others are 0 or not stored.
+template <class T, int N>
+__device__ __forceinline__ void load_some(const T *p, float (&v)[N], int left)
+{
+    if (left >= N) return load_vec(p, v);
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = k < left ? (float)p[k] : 0.f;
+}
+
+template <class T, int N>
+__device__ __forceinline__ void store_some(T *p, const float (&v)[N], int left)
+{
+    if (left >= N) return store_vec(p, v);
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        if (k < left) p[k] = (T)v[k];
+}
+
+__device__ __forceinline__ int64_t load_id(const void *ids, int ids_bytes, int64_t t)
+{
+    return ids_bytes == 8 ? ((const int64_t *)ids)[t] : (int64_t)((const int32_t *)ids)[t];
+}
+
+// Columns that one thread holds of a row.
+constexpr int kCols = 8;
+
+// Item `base + threadIdx.x` of items that are rows of `per_row`: its row, and its
+// place in the row.  base is the same in every lane, so that the 64-bit
+// division is done once per wave and a lane's own is in 32 bits.
+__device__ __forceinline__ int64_t row_of(int64_t base, int per_row, int &in_row)
+{
+    const int64_t first = base / per_row;
+    const uint32_t at = (uint32_t)(base - first * per_row) + threadIdx.x;
+    const uint32_t row = at / (uint32_t)per_row;
+    in_row = (int)(at - row * per_row);
+    return first + row;
+}
+
+// out[t] = scale * table[ids[t]]: one thread per kCols columns of a place.
+template <class T, class O>
+__global__ __launch_bounds__(256) void k_embedding(const T *__restrict__ table, int64_t table_ld,
+                                                   int64_t vocab, int width, int per_row,
+                                                   const void *__restrict__ ids, int ids_bytes,
+                                                   int64_t tokens, float scale,
+                                                   O *__restrict__ out, int64_t out_ld)
+{
+    for (int64_t base = (int64_t)blockIdx.x * 256; base < tokens * per_row;
+         base += (int64_t)gridDim.x * 256) {
+        int c;
+        const int64_t t = row_of(base, per_row, c);
+        if (t >= tokens) return;
+        c *= kCols;
+        const int64_t id = load_id(ids, ids_bytes, t);
+        float v[kCols] = {};
+        if (id >= 0 && id < vocab) {
+            load_some(table + id * table_ld + c, v, width - c);
+#pragma unroll
+            for (int k = 0; k < kCols; ++k) v[k] *= scale;
+        }
+        store_some(out + t * out_ld + c, v, width - c);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Sorting the places by id: a stable radix sort, least significant digit first.
+// A key is the id, or `vocab` for a place that adds nothing (these come last).
+// ---------------------------------------------------------------------------
+
+constexpr int kDigits = 256;
+constexpr int kSmallTokens = 4096;   // sorted by one workgroup, in LDS
+constexpr int kSmallThreads = 1024;
+constexpr int kSortBlocks = 128;     // workgroups of a pass over more
+constexpr int kFillBlocks = 512;
+
+struct Key {
+    int64_t vocab, padding;
+    __device__ __forceinline__ uint32_t of(int64_t id) const
+    {
+        return id >= 0 && id < vocab && id != padding ? (uint32_t)id : (uint32_t)vocab;
+    }
+};
+
+// Zeros rows [begin, end) of the gradient, by workgroup `part` of `parts`.
+// These run beside the sort, which keeps few CUs busy and no memory; rows with
+// places are then written a second time.
+struct Fill {
+    void *grad;
+    int64_t ld;
+    int64_t begin, end;  // rows
+    int width, elem;     // elem: bytes of an element
+};
+
+__device__ void fill_rows(const Fill &f, int part, int parts)
+{
+    const int64_t rows = f.end - f.begin;
+    const int64_t r0 = f.begin + rows * part / parts, r1 = f.begin + rows * (part + 1) / parts;
+    if (r0 >= r1) return;
+    const int64_t row_bytes = (int64_t)f.width * f.elem;
+    char *base = (char *)f.grad + r0 * f.ld * f.elem;
+    int64_t pieces = r1 - r0, len = row_bytes, pitch = f.ld * f.elem;
+    if (f.ld == f.width) len *= pieces, pieces = 1;  // one run of bytes
+    for (int64_t p = 0; p < pieces; ++p) {
+        char *at = base + p * pitch, *stop = at + len;
+        char *first = (char *)(((uintptr_t)at + 15) & ~(uintptr_t)15);
+        char *last = (char *)((uintptr_t)stop & ~(uintptr_t)15);
+        if (first > last) first = last = stop;  // a short run that crosses no 16 bytes
+        for (char *q = at + threadIdx.x * 2; q < first && q < stop; q += blockDim.x * 2)
+            *(uint16_t *)q = 0;
+        for (char *q = first + threadIdx.x * 16; q < last; q += blockDim.x * 16)
+            *(uint4 *)q = uint4{0, 0, 0, 0};
+        for (char *q = last + threadIdx.x * 2; q < stop; q += blockDim.x * 2) *(uint16_t *)q = 0;
+    }
+}
+
+// Lanes of the wave that hold the same digit as this one (bits: its width), of
+// those that are `on`.
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, bool on)
+{
+    uint64_t same = __ballot(on);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot((digit >> b) & 1);
+        same &= (digit >> b) & 1 ? set : ~set;
+    }
+    return same;
+}
+
+// Exclusive sums of v over the workgroup's first 256 threads (all call it).
+__device__ __forceinline__ uint32_t scan256(uint32_t v, uint32_t *wave_sums)
+{
+    const int tid = threadIdx.x, lane = tid & 63;
+    uint32_t x = v;
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    if (tid < kDigits && lane == 63) wave_sums[tid >> 6] = x;
+    __syncthreads();
+    if (tid < kDigits)
+        for (int w = 0; w < (tid >> 6); ++w) x += wave_sums[w];
+    __syncthreads();
+    return x - v;
+}
+
+// Up to kSmallTokens places: workgroup 0 sorts them whole, the others zero the
+// gradient.  Every wave owns consecutive keys, so that ranks within a wave and
+// waves in order keep the sort stable.
+__global__ __launch_bounds__(kSmallThreads) void k_sort_small(const void *__restrict__ ids,
+                                                              int ids_bytes, int tokens, Key key,
+                                                              int bits, uint32_t *keys,
+                                                              uint32_t *order, Fill fill)
+{
+    if (blockIdx.x > 0) return fill_rows(fill, blockIdx.x - 1, gridDim.x - 1);
+    constexpr int kWaves = kSmallThreads / 64;
+    __shared__ uint32_t s_key[2][kSmallTokens], s_at[2][kSmallTokens];
+    __shared__ uint32_t s_count[kWaves][kDigits];
+    __shared__ uint32_t s_sums[4];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int per_wave = (tokens + kWaves * 64 - 1) / (kWaves * 64) * 64;
+    const int begin = min(wave * per_wave, tokens), end = min(begin + per_wave, tokens);
+    for (int t = tid; t < tokens; t += kSmallThreads) {
+        s_key[0][t] = key.of(load_id(ids, ids_bytes, t));
+        s_at[0][t] = t;
+    }
+    int from = 0;
+    for (int shift = 0; shift < bits; shift += 8, from ^= 1) {
+        const int width = min(8, bits - shift);
+        for (int d = tid; d < kWaves * kDigits; d += kSmallThreads) (&s_count[0][0])[d] = 0;
+        __syncthreads();
+        for (int t = begin + lane; t < end; t += 64)
+            atomicAdd(&s_count[wave][(s_key[from][t] >> shift) & 255], 1u);
+        __syncthreads();
+        uint32_t total = 0;
+        if (tid < kDigits)
+            for (int w = 0; w < kWaves; ++w) total += s_count[w][tid];
+        uint32_t at = scan256(total, s_sums);
+        if (tid < kDigits)
+            for (int w = 0; w < kWaves; ++w) {
+                const uint32_t n = s_count[w][tid];
+                s_count[w][tid] = at;
+                at += n;
+            }
+        __syncthreads();
+        for (int t0 = begin; t0 < end; t0 += 64) {
+            const int t = t0 + lane;
+            const bool on = t < end;
+            const uint32_t k = on ? s_key[from][t] : 0;
+            const uint32_t digit = (k >> shift) & 255;
+            const uint64_t same = same_digit(digit, width, on);
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            uint32_t pos = 0;
+            if (on) {
+                pos = s_count[wave][digit] + rank;
+                s_key[from ^ 1][pos] = k;
+                s_at[from ^ 1][pos] = s_at[from][t];
+            }
+            __builtin_amdgcn_wave_barrier();  // every lane has read its digit's place
+            if (on && rank == 0) s_count[wave][digit] += (uint32_t)__popcll(same);
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+    }
+    for (int t = tid; t < tokens; t += kSmallThreads) {
+        keys[t] = s_key[from][t];
+        order[t] = s_at[from][t];
+    }
+}
+
+// One digit's counts per workgroup.  FIRST: keys come from the ids.
+template <bool FIRST>
+__device__ __forceinline__ uint32_t key_at(const void *src, int ids_bytes, const Key &key,
+                                           int64_t t)
+{
+    return FIRST ? key.of(load_id(src, ids_bytes, t)) : ((const uint32_t *)src)[t];
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(256) void k_sort_count(const void *__restrict__ src, int ids_bytes,
+                                                    int64_t tokens, int64_t per_block, int blocks,
+                                                    Key key, int shift, uint32_t *counts,
+                                                    Fill fill)
+{
+    if ((int)blockIdx.x >= blocks)
+        return fill_rows(fill, blockIdx.x - blocks, gridDim.x - blocks);
+    __shared__ uint32_t s_count[kDigits];
+    s_count[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t begin = blockIdx.x * per_block, end = min(begin + per_block, tokens);
+    for (int64_t t = begin + threadIdx.x; t < end; t += 256)
+        atomicAdd(&s_count[(key_at<FIRST>(src, ids_bytes, key, t) >> shift) & 255], 1u);
+    __syncthreads();
+    counts[blockIdx.x * kDigits + threadIdx.x] = s_count[threadIdx.x];
+}
+
+// Moves a workgroup's keys to their places, from the counts of all workgroups.
+template <bool FIRST>
+__global__ __launch_bounds__(256) void k_sort_move(const void *__restrict__ src,
+                                                   const uint32_t *__restrict__ src_at,
+                                                   int ids_bytes, int64_t tokens,
+                                                   int64_t per_block, int blocks, Key key,
+                                                   int shift, int width,
+                                                   const uint32_t *__restrict__ counts,
+                                                   uint32_t *__restrict__ keys,
+                                                   uint32_t *__restrict__ order, Fill fill)
+{
+    if ((int)blockIdx.x >= blocks)
+        return fill_rows(fill, blockIdx.x - blocks, gridDim.x - blocks);
+    __shared__ uint32_t s_count[4][kDigits];
+    __shared__ uint32_t s_sums[4];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    uint32_t before = 0, total = 0;
+#pragma unroll 8
+    for (int b = 0; b < blocks; ++b) {
+        const uint32_t n = counts[b * kDigits + tid];
+        total += n;
+        if (b < (int)blockIdx.x) before += n;
+    }
+    for (int w = 0; w < 4; ++w) s_count[w][tid] = 0;
+    const uint32_t base = scan256(total, s_sums) + before;
+    const int64_t per_wave = per_block / 4;  // a multiple of 64
+    const int64_t block_end = min((blockIdx.x + 1) * per_block, tokens);
+    const int64_t begin = min(blockIdx.x * per_block + wave * per_wave, block_end);
+    const int64_t end = min(begin + per_wave, block_end);
+    for (int64_t t = begin + lane; t < end; t += 64)
+        atomicAdd(&s_count[wave][(key_at<FIRST>(src, ids_bytes, key, t) >> shift) & 255], 1u);
+    __syncthreads();
+    uint32_t at = base;
+    for (int w = 0; w < 4; ++w) {
+        const uint32_t n = s_count[w][tid];
+        s_count[w][tid] = at;
+        at += n;
+    }
+    __syncthreads();
+    for (int64_t t0 = begin; t0 < end; t0 += 64) {
+        const int64_t t = t0 + lane;
+        const bool on = t < end;
+        const uint32_t k = on ? key_at<FIRST>(src, ids_bytes, key, t) : 0;
+        const uint32_t digit = (k >> shift) & 255;
+        const uint64_t same = same_digit(digit, width, on);
+        const int rank = __popcll(same & ((1ull << lane) - 1));
+        if (on) {
+            const uint32_t pos = s_count[wave][digit] + rank;
+            keys[pos] = k;
+            order[pos] = FIRST ? (uint32_t)t : src_at[t];
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (on && rank == 0) s_count[wave][digit] += (uint32_t)__popcll(same);
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Sums over the sorted places
+// ---------------------------------------------------------------------------
+
+// The sorted list is cut into pieces of `piece` places, whatever rows they
+// belong to, so that a frequent token costs what its places do.  A thread adds
+// kCols columns of a piece's places in order.  A row that lies inside a piece is
+// finished there; a row that crosses a piece's end leaves one partial sum per
+// piece it touches (slot 0: it began in an earlier piece, slot 1: it begins
+// here), which k_grad_join adds in order.
+struct Sums {
+    const uint32_t *keys, *order;
+    int64_t tokens, vocab;
+    int width, per_row, piece;
+    int64_t pieces;
+    float scale;
+    int accumulate;
+    int64_t dout_ld, grad_ld;
+    float *partial;  // [pieces][2][per_row * kCols]
+};
+
+template <class G>
+__device__ __forceinline__ void finish_row(const Sums &s, G *__restrict__ grad, uint32_t row,
+                                           int c, const float (&acc)[kCols])
+{
+    G *p = grad + (int64_t)row * s.grad_ld + c;
+    float v[kCols] = {};
+    if (s.accumulate) load_some(p, v, s.width - c);
+#pragma unroll
+    for (int k = 0; k < kCols; ++k)
+        v[k] = s.accumulate ? v[k] + s.scale * acc[k] : s.scale * acc[k];
+    store_some(p, v, s.width - c);
+}
+
+__device__ __forceinline__ float *partial_at(const Sums &s, int64_t piece, int slot, int c)
+{
+    return s.partial + ((piece * 2 + slot) * s.per_row) * kCols + c;
+}
+
+constexpr int kAhead = 8;  // rows whose loads are in flight together
+
+template <class D, class G>
+__global__ __launch_bounds__(256) void k_grad_sum(Sums s, const D *__restrict__ dout,
+                                                  G *__restrict__ grad)
+{
+    int c;
+    const int64_t piece = row_of((int64_t)blockIdx.x * 256, s.per_row, c);
+    if (piece >= s.pieces) return;
+    c *= kCols;
+    const int64_t begin = piece * s.piece, end = min(begin + s.piece, s.tokens);
+    uint32_t row = s.keys[begin];
+    if (row >= s.vocab) return;  // places that add nothing, as all that follow
+    bool before = begin > 0 && s.keys[begin - 1] == row;
+    float acc[kCols] = {};
+    for (int64_t at = begin; at < end; at += kAhead) {
+        uint32_t k[kAhead];
+        float v[kAhead][kCols];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const bool on = at + u < end;
+            k[u] = on ? s.keys[at + u] : (uint32_t)s.vocab;
+            const int64_t t = on && k[u] < s.vocab ? s.order[at + u] : s.order[begin];
+            load_some(dout + t * s.dout_ld + c, v[u], s.width - c);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (k[u] >= s.vocab) break;
+            if (k[u] != row) {  // the row ends here
+                if (before)
+                    store_vec(partial_at(s, piece, 0, c), acc);
+                else
+                    finish_row(s, grad, row, c, acc);
+                row = k[u];
+                before = false;
+#pragma unroll
+                for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) acc[i] += v[u][i];
+        }
+    }
+    const bool after = end < s.tokens && s.keys[end] == row;
+    if (before)
+        store_vec(partial_at(s, piece, 0, c), acc);
+    else if (after)
+        store_vec(partial_at(s, piece, 1, c), acc);
+    else
+        finish_row(s, grad, row, c, acc);
+}
+
+// Rows that cross pieces, by the piece they begin in.
+template <class G>
+__global__ __launch_bounds__(256) void k_grad_join(Sums s, G *__restrict__ grad)
+{
+    int c;
+    const int64_t piece = row_of((int64_t)blockIdx.x * 256, s.per_row, c);
+    c *= kCols;
+    const int64_t begin = piece * s.piece, end = begin + s.piece;
+    if (piece >= s.pieces || end >= s.tokens) return;
+    const uint32_t row = s.keys[end];
+    if (row >= s.vocab || s.keys[end - 1] != row) return;
+    if (begin > 0 && s.keys[begin - 1] == row) return;  // it began earlier
+    float acc[kCols];
+    load_vec(partial_at(s, piece, 1, c), acc);
+    for (int64_t q = piece + 1;; q += kAhead) {
+        float v[kAhead][kCols];
+        bool on[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t p = q + u < s.pieces ? q + u : q;
+            on[u] = q + u < s.pieces && s.keys[p * s.piece] == row;
+            load_vec(partial_at(s, p, 0, c), v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (on[u])
+#pragma unroll
+                for (int i = 0; i < kCols; ++i) acc[i] += v[u][i];
+        if (!on[kAhead - 1] || q + kAhead >= s.pieces) break;
+    }
+    finish_row(s, grad, row, c, acc);
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+
+constexpr int64_t kSizeLimit = (int64_t)1 << 31;
+
+struct GradLayout {
+    int piece;
+    int64_t pieces, per_row;
+    size_t keys[2], order[2], counts, partial, total;  // byte offsets
+};
+
+size_t round_up(size_t a, size_t m) { return (a + m - 1) / m * m; }
+
+// Places per piece: enough pieces to fill the GPU, and up to 128 places where
+// there are many, which bounds the partial sums and the join's chains.
+int piece_of(int64_t tokens)
+{
+    int p = 8;
+    while (p < 128 && tokens / p > 1024) p *= 2;
+    return p;
+}
+
+GradLayout grad_layout(int64_t tokens, int64_t width)
+{
+    GradLayout l{};
+    l.piece = piece_of(tokens);
+    l.pieces = (tokens + l.piece - 1) / l.piece;
+    l.per_row = (width + kCols - 1) / kCols;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += round_up(bytes, 256);
+        return here;
+    };
+    for (int k = 0; k < 2; ++k) {
+        l.keys[k] = take((size_t)tokens * 4);
+        l.order[k] = take((size_t)tokens * 4);
+    }
+    l.counts = take((size_t)kSortBlocks * kDigits * 4);
+    l.partial = take((size_t)l.pieces * 2 * l.per_row * kCols * 4);
+    l.total = at;
+    return l;
+}
+
+int check_size(int64_t v, const char *name)
+{
+    if (v < 0 || v >= kSizeLimit)
+        return fail(ONEBIT_EINVAL, "%s = %lld is not in [0, 2^31)", name, (long long)v);
+    return ONEBIT_OK;
+}
+
+int elem_bytes(int32_t dtype)
+{
+    return dtype == ONEBIT_GRAD_F32 ? 4
+         : dtype == ONEBIT_GRAD_BF16 || dtype == ONEBIT_GRAD_F16 ? 2 : 0;
+}
+
+int check_rows(const void *p, int32_t dtype, int64_t ld, int64_t rows, int64_t width,
+               const char *name)
+{
+    const int bytes = elem_bytes(dtype);
+    if (!bytes) return fail(ONEBIT_EINVAL, "%s: type %d is not one of ONEBIT_GRAD_*", name, dtype);
+    if (rows > 1 && (ld < width || ld > ((int64_t)1 << 40)))
+        return fail(ONEBIT_EINVAL, "%s: leading dimension %lld, width %lld", name, (long long)ld,
+                    (long long)width);
+    if (!p && rows > 0 && width > 0) return fail(ONEBIT_EINVAL, "%s is NULL", name);
+    if ((uintptr_t)p % bytes) return fail(ONEBIT_EALIGN, "%s is not %d-byte aligned", name, bytes);
+    return ONEBIT_OK;
+}
+
+int check_ids(const void *ids, int32_t ids_bytes, int64_t tokens)
+{
+    if (ids_bytes != 4 && ids_bytes != 8)
+        return fail(ONEBIT_EINVAL, "ids_bytes = %d is neither 4 nor 8", ids_bytes);
+    if (!ids && tokens > 0) return fail(ONEBIT_EINVAL, "ids is NULL");
+    if ((uintptr_t)ids % ids_bytes)
+        return fail(ONEBIT_EALIGN, "ids is not %d-byte aligned", ids_bytes);
+    return ONEBIT_OK;
+}
+
+#define TRY(expr)                         \
+    do {                                  \
+        int _st = (expr);                 \
+        if (_st != ONEBIT_OK) return _st; \
+    } while (0)
+
+// Calls f with a null pointer of the element type's C++ type.
+template <class F>
+void with_type(int32_t dtype, F &&f)
+{
+    if (dtype == ONEBIT_GRAD_F32) f((float *)nullptr);
+    else if (dtype == ONEBIT_GRAD_BF16) f((__bf16 *)nullptr);
+    else f((_Float16 *)nullptr);
+}
+
+int launched(const char *what)
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? ONEBIT_OK : hip_fail(e, what);
+}
+
+}  // namespace
+}  // namespace onebit
+
+using namespace onebit;
+
+extern "C" {
+
+int onebit_embedding_forward(const void *table, int32_t table_dtype, int64_t table_ld,
+                             int64_t vocab, int64_t width, const void *ids, int32_t ids_bytes,
+                             int64_t tokens, float scale, void *out, int32_t out_dtype,
+                             int64_t out_ld, onebit_stream stream)
+{
+    TRY(check_size(vocab, "vocab"));
+    TRY(check_size(width, "width"));
+    TRY(check_size(tokens, "tokens"));
+    TRY(check_rows(table, table_dtype, table_ld, vocab, width, "table"));
+    TRY(check_rows(out, out_dtype, out_ld, tokens, width, "out"));
+    TRY(check_ids(ids, ids_bytes, tokens));
+    if (tokens == 0 || width == 0) return ONEBIT_OK;
+    const int per_row = (int)((width + kCols - 1) / kCols);
+    const int64_t items = tokens * per_row;
+    const int blocks = (int)std::min<int64_t>((items + 255) / 256, 1 << 22);
+    with_type(table_dtype, [&](auto *t) {
+        with_type(out_dtype, [&](auto *o) {
+            using T = std::remove_pointer_t<decltype(t)>;
+            using O = std::remove_pointer_t<decltype(o)>;
+            k_embedding<T, O><<<blocks, 256, 0, (hipStream_t)stream>>>(
+                (const T *)table, table_ld, vocab, (int)width, per_row, ids, ids_bytes, tokens,
+                scale, (O *)out, out_ld);
+        });
+    });
+    return launched("embedding kernel launch");
+}
+
+int onebit_embedding_grad_workspace(int64_t tokens, int64_t vocab, int64_t width, size_t *bytes)
+{
+    if (!bytes) return fail(ONEBIT_EINVAL, "bytes is NULL");
+    TRY(check_size(tokens, "tokens"));
+    TRY(check_size(vocab, "vocab"));
+    TRY(check_size(width, "width"));
+    *bytes = grad_layout(tokens, width).total;
+    return ONEBIT_OK;
+}
+
+int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld, const void *ids,
+                          int32_t ids_bytes, int64_t tokens, int64_t vocab, int64_t width,
+                          int64_t padding_id, float scale, void *grad, int32_t grad_dtype,
+                          int64_t grad_ld, int32_t accumulate, void *workspace,
+                          onebit_stream stream)
+{
+    TRY(check_size(vocab, "vocab"));
+    TRY(check_size(width, "width"));
+    TRY(check_size(tokens, "tokens"));
+    TRY(check_rows(dout, dout_dtype, dout_ld, tokens, width, "dout"));
+    TRY(check_rows(grad, grad_dtype, grad_ld, vocab, width, "grad"));
+    TRY(check_ids(ids, ids_bytes, tokens));
+    if (!workspace) return fail(ONEBIT_EINVAL, "workspace is NULL");
+    if ((uintptr_t)workspace % 16) return fail(ONEBIT_EALIGN, "workspace is not 16-byte aligned");
+    if (vocab == 0 || width == 0 || (tokens == 0 && accumulate)) return ONEBIT_OK;
+    hipStream_t st = (hipStream_t)stream;
+    const GradLayout l = grad_layout(tokens, width);
+    const int64_t blocks = (l.pieces * l.per_row + 255) / 256;
+    if (blocks > (1 << 23))
+        return fail(ONEBIT_EINVAL, "%lld places of %lld columns are too many for one call",
+                    (long long)tokens, (long long)width);
+    char *ws = (char *)workspace;
+    const Key key{vocab, padding_id < 0 ? -1 : padding_id};
+    const int bits = 32 - __builtin_clz((uint32_t)vocab);  // keys are 0..vocab
+    Fill fill{grad, vocab > 1 ? grad_ld : width, 0, accumulate ? 0 : vocab, (int)width,
+              elem_bytes(grad_dtype)};
+    const int fills = accumulate ? 0 : (int)std::min<int64_t>(kFillBlocks, vocab);
+    int now = 0;
+    if (tokens <= kSmallTokens) {
+        k_sort_small<<<1 + fills, kSmallThreads, 0, st>>>(
+            ids, ids_bytes, (int)tokens, key, bits, (uint32_t *)(ws + l.keys[0]),
+            (uint32_t *)(ws + l.order[0]), fill);
+    } else {
+        const int sorters = (int)std::min<int64_t>(kSortBlocks, (tokens + 1023) / 1024);
+        const int64_t per_block = ((tokens + sorters - 1) / sorters + 255) / 256 * 256;
+        uint32_t *counts = (uint32_t *)(ws + l.counts);
+        const int passes = (bits + 7) / 8;
+        const void *src = ids;
+        const uint32_t *src_at = nullptr;
+        for (int p = 0; p < passes; ++p) {
+            // the rows are zeroed in equal parts beside every launch of the sort
+            auto part = [&](int k) {
+                Fill f = fill;
+                f.begin = fill.end * k / (2 * passes);
+                f.end = fill.end * (k + 1) / (2 * passes);
+                return f;
+            };
+            const int shift = 8 * p, width_bits = std::min(8, bits - shift);
+            uint32_t *keys = (uint32_t *)(ws + l.keys[p & 1]);
+            uint32_t *order = (uint32_t *)(ws + l.order[p & 1]);
+            if (p == 0) {
+                k_sort_count<true><<<sorters + fills, 256, 0, st>>>(
+                    src, ids_bytes, tokens, per_block, sorters, key, shift, counts, part(0));
+                k_sort_move<true><<<sorters + fills, 256, 0, st>>>(
+                    src, src_at, ids_bytes, tokens, per_block, sorters, key, shift, width_bits,
+                    counts, keys, order, part(1));
+            } else {
+                k_sort_count<false><<<sorters + fills, 256, 0, st>>>(
+                    src, ids_bytes, tokens, per_block, sorters, key, shift, counts, part(2 * p));
+                k_sort_move<false><<<sorters + fills, 256, 0, st>>>(
+                    src, src_at, ids_bytes, tokens, per_block, sorters, key, shift, width_bits,
+                    counts, keys, order, part(2 * p + 1));
+            }
+            src = keys;
+            src_at = order;
+            now = p & 1;
+        }
+    }
+    TRY(launched("embedding gradient sort launch"));
+    if (tokens == 0) return ONEBIT_OK;
+    Sums s{(const uint32_t *)(ws + l.keys[now]), (const uint32_t *)(ws + l.order[now]), tokens,
+           vocab, (int)width, (int)l.per_row, l.piece, l.pieces, scale, accumulate, dout_ld,
+           grad_ld, (float *)(ws + l.partial)};
+    with_type(grad_dtype, [&](auto *g) {
+        using G = std::remove_pointer_t<decltype(g)>;
+        with_type(dout_dtype, [&](auto *d) {
+            using D = std::remove_pointer_t<decltype(d)>;
+            k_grad_sum<D, G><<<blocks, 256, 0, st>>>(s, (const D *)dout, (G *)grad);
+        });
+        if (l.pieces > 1) k_grad_join<G><<<blocks, 256, 0, st>>>(s, (G *)grad);
+    });
+    return launched("embedding gradient launch");
+}
+
+}  // extern "C"
