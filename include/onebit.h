@@ -409,6 +409,81 @@ int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld,
                           int64_t grad_ld, int32_t accumulate, void *workspace,
                           onebit_stream stream);
 
+/* ---------------------------------------------------------------------------
+ * Orthogonalised updates (the Muon step) of a list of matrices
+ * ---------------------------------------------------------------------------
+ * Matrices.  onebit_matrices_create() describes `count` matrices inside flat
+ *   buffers: matrix k has rows[k] x cols[k] elements, row i starting at
+ *   element offset[k] + i * ld[k] of every buffer of a call.  offset NULL:
+ *   one after another, each from the next multiple of 64 elements (the layout
+ *   of a plan over the same sizes); ld NULL: ld[k] = cols[k].  The handle owns
+ *   small device tables.
+ * Orthogonalisation.  O(u) is `steps` Newton-Schulz steps from
+ *   X = u / (||u||_F + eps), taken in the orientation with the smaller side
+ *   first:  A = X X^T,  X <- a X + (b A + c A A) X.
+ *   The products are formed in the equivalent form around t = ||X||_F^2 / m
+ *   (m the smaller side): with D = A - t I,
+ *     X <- (a + b t + c t^2) X + ((b + 2 c t) D + c D D) X,
+ *   whose operands are smaller, so that their rounding counts for less.
+ *   A zero matrix gives zeros; a NaN or an infinity makes its whole matrix NaN.
+ * Products.  ONEBIT_PRODUCTS_F32: every operand is a pair of fp16 numbers (the
+ *   value rounded, and the rest), and a product adds three fp16 products in
+ *   fp32: the result is as near to the exact one as an fp32 computation's.
+ *   ONEBIT_PRODUCTS_F16: operands are single fp16 numbers, the iterate X itself
+ *   stays a pair: about 1e-3 off as a whole (2-norm), a third of the work;
+ *   meant for 16-bit outputs.
+ * Coefficients.  The three numbers a, b, c (host array, read during the call;
+ *   NULL: 3.4445, -4.7750, 2.0315).  Refused when the singular values could
+ *   leave the range that the fp16 operands hold (|X|, |A| and the polynomial's
+ *   change up to 7.5). */
+typedef struct onebit_matrices_s *onebit_matrices;
+
+#define ONEBIT_PRODUCTS_F32 0
+#define ONEBIT_PRODUCTS_F16 1
+
+/* How the step's update is scaled, by the matrix's shape. */
+#define ONEBIT_MUON_SCALE_NONE 0     /* 1                          */
+#define ONEBIT_MUON_SCALE_SPECTRAL 1 /* sqrt(max(1, rows / cols))  */
+#define ONEBIT_MUON_SCALE_RMS 2      /* 0.2 sqrt(max(rows, cols))  */
+
+/* Errors: EINVAL (null, count < 1, a side below 0 or above 2^20, 2^31 or more
+ * elements in a matrix, an offset below 0, ld below cols, an extent above 2^40,
+ * too many tiles), ENOMEM, EHIP.  Overlapping matrices are the caller's fault. */
+int onebit_matrices_create(const int64_t *rows, const int64_t *cols, const int64_t *offset,
+                           const int64_t *ld, int32_t count, onebit_matrices *out);
+
+/* The caller must ensure that no call using the handle is still running. */
+int onebit_matrices_destroy(onebit_matrices mats);
+
+/* extent: elements that every flat buffer of a call must hold; offset[count]:
+ * the matrices' offsets; workspace_bytes: for calls with these `products`.
+ * Any output may be NULL.  Errors: EINVAL. */
+int onebit_matrices_info(onebit_matrices mats, int32_t products, int64_t *extent,
+                         int64_t *offset, size_t *workspace_bytes);
+
+/* out = O(in), matrix by matrix; elements outside the matrices are not
+ * written.  in, out: flat buffers of `extent` elements of their types; out may
+ * be the same buffer as in (same type).  workspace: 256-byte aligned.
+ * Errors: EINVAL (null, unknown type or products, steps < 1 or > 64, eps not
+ * above 0, coefficients refused), EALIGN, EHIP. */
+int onebit_orthogonalize(onebit_matrices mats, const void *in, int32_t in_dtype, void *out,
+                         int32_t out_dtype, int32_t products, int32_t steps,
+                         const float *coefficients, float eps, void *workspace,
+                         onebit_stream stream);
+
+/* One Muon step of every matrix:
+ *   g = (1/n_grads) sum_i grads[i]     (fp64 sum in row order, one rounding)
+ *   m = momentum * m + g
+ *   u = nesterov ? g + momentum * m : m
+ *   x = (1 - lr * weight_decay) x - lr * scale(rows, cols) * O(u)
+ * x, m: in/out flat fp32 buffers; grads: n_grads rows of grad_ld >= extent
+ * elements of grad_dtype.  Errors: EINVAL, EALIGN, EHIP. */
+int onebit_muon_step(onebit_matrices mats, float *x, float *m, const void *grads,
+                     int32_t grad_dtype, int64_t grad_ld, int32_t n_grads, float lr,
+                     float momentum, int32_t nesterov, float weight_decay, int32_t scale,
+                     int32_t products, int32_t steps, const float *coefficients, float eps,
+                     void *workspace, onebit_stream stream);
+
 /* Name of a status code (static string). */
 const char *onebit_status_str(int32_t status);
 

@@ -9,7 +9,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("onebit_kernels.hip", "onebit_abi.hip",
-                                                   "onebit_embedding.hip")]
+                                                   "onebit_embedding.hip", "onebit_matrices.hip")]
 LIB = os.path.join(HERE, "lib", "libonebit.so")
 ARGS_SOURCE = os.path.join(HERE, "csrc", "binding_args.cpp")
 PROBE_SOURCE = os.path.join(HERE, "csrc", "hbm_probe.hip")

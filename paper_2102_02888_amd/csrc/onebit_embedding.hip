@@ -150,6 +150,14 @@ __device__ void fill_rows(const Fill &f, int part, int parts)
     }
 }
 
+// Orders a wave's LDS accesses: every lane has read (written) what comes before.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Lanes of the wave that hold the same digit as this one (bits: its width), of
 // those that are `on`.
 __device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, bool on)
@@ -231,9 +239,9 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const void *__rest
                 s_key[from ^ 1][pos] = k;
                 s_at[from ^ 1][pos] = s_at[from][t];
             }
-            __builtin_amdgcn_wave_barrier();  // every lane has read its digit's place
+            wave_sync();  // every lane has read its digit's place
             if (on && rank == 0) s_count[wave][digit] += (uint32_t)__popcll(same);
-            __builtin_amdgcn_wave_barrier();
+            wave_sync();
         }
         __syncthreads();
     }
@@ -320,9 +328,9 @@ __global__ __launch_bounds__(256) void k_sort_move(const void *__restrict__ src,
             keys[pos] = k;
             order[pos] = FIRST ? (uint32_t)t : src_at[t];
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
         if (on && rank == 0) s_count[wave][digit] += (uint32_t)__popcll(same);
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
     }
 }
 

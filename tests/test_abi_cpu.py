@@ -94,3 +94,21 @@ def test_binding_fails_loudly_without_library(tmp_path, monkeypatch):
     monkeypatch.setattr(_native, "_lib", None)
     with pytest.raises(ImportError):
         _native.lib()
+
+
+def test_matrix_argument_errors_before_device(native):
+    lib = native.lib()
+    out = ctypes.c_void_p(1)
+
+    def create(rows, cols, offset=None, ld=None):
+        arrays = [None if v is None else (ctypes.c_int64 * len(v))(*v)
+                  for v in (rows, cols, offset, ld)]
+        return lib.onebit_matrices_create(*arrays, len(rows), ctypes.byref(out))
+    assert lib.onebit_matrices_create(None, None, None, None, 1, ctypes.byref(out)) == -1
+    assert out.value is None  # cleared on error
+    assert create([], []) == -1
+    assert lib.onebit_matrices_destroy(None) == -1
+    assert lib.onebit_matrices_info(None, 0, None, None, None) == -1
+    assert lib.onebit_orthogonalize(None, None, 0, None, 0, 0, 5, None, 1e-7, None, None) == -1
+    assert lib.onebit_muon_step(None, None, None, None, 0, 0, 1, 0.1, 0.9, 1, 0.0, 0, 0, 5, None,
+                                1e-7, None, None) == -1
