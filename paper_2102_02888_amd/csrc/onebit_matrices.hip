@@ -8,10 +8,10 @@
 //   poly   B = (b + 2 c t) D + c D D  (symmetric)
 //   next   X <- (a + b t + c t^2) X + B X
 // all of them over every tile of every matrix.  A product is always rows times
-// rows (both operands contiguous along the summed index), for which the iterate
-// is kept in both orientations, X (m x n) and XT (n x m), and D and B are
-// symmetric.  Every operand lies in the workspace, padded with zeros to
-// multiples of kTile, so that the product kernel has no bounds to check.
+// rows (both operands contiguous along the summed index; D and B are symmetric),
+// but for X in B X, whose fragments are read transposed from LDS.  Every operand
+// lies in the workspace, padded with zeros to multiples of the tile, so that the
+// product kernel has no bounds to check.
 //
 // Numbers.  Operands are fp16 times kScale.  PRODUCTS_F32 ("pairs"): a value is
 // hi + lo, two fp16 numbers, together as fine as an fp32 one; a product adds
@@ -34,6 +34,7 @@
 #include <cstring>
 #include <memory>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "../../include/onebit.h"
@@ -44,7 +45,7 @@ namespace onebit {
 namespace {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
@@ -54,7 +55,6 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 constexpr float kScale = 8192.f;
 constexpr double kRange = 7.5;
 
-constexpr int kTile = 128;   // rows and columns of an output tile
 constexpr int kSlab = 64;    // fp16 numbers of an operand's row that are staged together
 constexpr int kNormChunk = 8192;  // elements of a matrix per workgroup of the norm
 constexpr int kPrep = 64;    // rows and columns of a workgroup of the first iterate
@@ -76,11 +76,11 @@ struct Item {
     uint16_t i, j;
 };
 
-// Areas of the workspace.  Pairs: rows of X, XT, D and B hold 32 hi numbers and
-// then the same 32 lo numbers, so that 64 consecutive numbers are a slab of
-// either kind.  Halves: hi alone, and xt_lo holds the iterate's lo.
+// Areas of the workspace.  Pairs: rows of X, D and B hold 32 hi numbers and then
+// the same 32 lo numbers, so that 64 consecutive numbers are a slab of either
+// kind.  Halves: hi alone, and x_lo holds the iterate's lo.
 struct Areas {
-    _Float16 *x, *xt, *xt_next, *xt_lo, *d, *b;
+    _Float16 *x, *x_next, *x_lo, *d, *b;
     double *norm;   // per norm chunk
     float *part;    // per tile of the iterate
     float *t;       // per matrix
@@ -91,12 +91,6 @@ struct Coefficients {
     float a, b, c;
     float fade;  // of gamma in a step: a power of two, at most 1/2
 };
-
-// Workgroups go to the XCDs round-robin: each takes a contiguous eighth.
-__device__ __forceinline__ int item_index()
-{
-    return (int)((blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds);
-}
 
 __device__ __forceinline__ void split(float v, _Float16 &hi, _Float16 &lo)
 {
@@ -110,6 +104,14 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Workgroup barrier behind loads straight into LDS: every wave waits for its own
+// before it arrives (a plain barrier does not wait for them).
+__device__ __forceinline__ void staged_sync()
+{
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0), the other counters at their most
+    __syncthreads();
 }
 
 // Sum over the workgroup of 256, the same in every thread; scratch: 4 values.
@@ -188,25 +190,11 @@ __global__ __launch_bounds__(256) void k_norm(const Mat *__restrict__ mats,
     if (threadIdx.x == 0) norm[mt.norm_first + chunk] = sum;
 }
 
-// Writes `n` consecutive numbers (a multiple of 8, at most 32, inside one block
-// of 32) of an operand's row from packed (lo << 16 | hi) words.
-template <bool PAIRS, int N>
-__device__ __forceinline__ void put_row(_Float16 *row, _Float16 *row_lo, int k,
-                                        const uint32_t (&w)[N])
+// Place of number k of an operand's row (its hi; lo follows 32 further for pairs).
+template <bool PAIRS>
+__device__ __forceinline__ int column(int k)
 {
-    uint32_t hi[N / 2], lo[N / 2];
-#pragma unroll
-    for (int q = 0; q < N / 2; ++q) {
-        hi[q] = (w[2 * q] & 0xffffu) | w[2 * q + 1] << 16;
-        lo[q] = w[2 * q] >> 16 | (w[2 * q + 1] & 0xffff0000u);
-    }
-    _Float16 *ph = PAIRS ? row + (k >> 5) * 64 + (k & 31) : row + k;
-    _Float16 *pl = PAIRS ? ph + 32 : row_lo ? row_lo + k : nullptr;
-#pragma unroll
-    for (int q = 0; q < N / 2; q += 4) {
-        *(v4u *)(ph + 2 * q) = v4u{hi[q], hi[q + 1], hi[q + 2], hi[q + 3]};
-        if (PAIRS || pl) *(v4u *)(pl + 2 * q) = v4u{lo[q], lo[q + 1], lo[q + 2], lo[q + 3]};
-    }
+    return PAIRS ? (k >> 5) * 64 + (k & 31) : k;
 }
 
 __device__ __forceinline__ uint32_t pack(float v)
@@ -217,7 +205,7 @@ __device__ __forceinline__ uint32_t pack(float v)
            (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16;
 }
 
-// First iterate, X = u / (||u||_F + eps) in both orientations, padding zeroed.
+// First iterate, X = u / (||u||_F + eps), padding zeroed.
 template <bool PAIRS, class S>
 __global__ __launch_bounds__(256) void k_first(const Mat *__restrict__ mats,
                                                const Item *__restrict__ items, S src, double eps,
@@ -246,24 +234,26 @@ __global__ __launch_bounds__(256) void k_first(const Mat *__restrict__ mats,
         tile[r - r0][lane] = pack(v);
     }
     __syncthreads();
-    // along the matrix's rows: X, or XT where it is transposed; then along its columns
-    const int64_t ex = mt.ex * (PAIRS ? 2 : 1);
-    const int kind = PAIRS ? 2 : 1;
+    // rows of X: the matrix's rows, or its columns where X is the transpose
     const int line = threadIdx.x >> 2, part = (threadIdx.x & 3) * 16;
     uint32_t u[16];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) u[k] = tile[line][part + k];
-    const int row_pitch = mt.flip ? mt.mp : mt.np, col_pitch = mt.flip ? mt.np : mt.mp;
-    _Float16 *rows_to = (mt.flip ? w.xt : w.x) + ex;
-    _Float16 *rows_lo = !PAIRS && mt.flip ? w.xt_lo + ex : nullptr;
-    int64_t at = (int64_t)(r0 + line) * row_pitch;
-    put_row<PAIRS>(rows_to + at * kind, rows_lo ? rows_lo + at : nullptr, c0 + part, u);
+    for (int k = 0; k < 16; ++k) u[k] = mt.flip ? tile[part + k][line] : tile[line][part + k];
+    const int row = (mt.flip ? c0 : r0) + line, col = (mt.flip ? r0 : c0) + part;
+    constexpr int kind = PAIRS ? 2 : 1;
+    _Float16 *hi_at = w.x + mt.ex * kind + (int64_t)row * mt.np * kind + column<PAIRS>(col);
+    _Float16 *lo_at = PAIRS ? hi_at + 32 : w.x_lo + mt.ex + (int64_t)row * mt.np + col;
+    uint32_t hi[8], lo[8];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) u[k] = tile[part + k][line];
-    _Float16 *cols_to = (mt.flip ? w.x : w.xt) + ex;
-    _Float16 *cols_lo = !PAIRS && !mt.flip ? w.xt_lo + ex : nullptr;
-    at = (int64_t)(c0 + line) * col_pitch;
-    put_row<PAIRS>(cols_to + at * kind, cols_lo ? cols_lo + at : nullptr, r0 + part, u);
+    for (int q = 0; q < 8; ++q) {
+        hi[q] = (u[2 * q] & 0xffffu) | u[2 * q + 1] << 16;
+        lo[q] = u[2 * q] >> 16 | (u[2 * q + 1] & 0xffff0000u);
+    }
+#pragma unroll
+    for (int q = 0; q < 8; q += 4) {
+        *(v4u *)(hi_at + 2 * q) = v4u{hi[q], hi[q + 1], hi[q + 2], hi[q + 3]};
+        *(v4u *)(lo_at + 2 * q) = v4u{lo[q], lo[q + 1], lo[q + 2], lo[q + 3]};
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -272,25 +262,48 @@ __global__ __launch_bounds__(256) void k_first(const Mat *__restrict__ mats,
 
 constexpr int kGram = 0, kPoly = 1, kNext = 2, kLast = 3;
 
-// Where the last product goes: a tensor, or the parameters.
+// Where the last product goes, 8 numbers of a row (of which `left` exist): a
+// tensor, or the parameters.  Rows need no alignment: the vector accesses are
+// stated as copies of bytes.
 template <class T>
 struct ToTensor {
     T *out;
-    __device__ __forceinline__ void put(int64_t e, float o, float) const { out[e] = (T)o; }
+    __device__ __forceinline__ void put(int64_t e, const float *o, int left, float) const
+    {
+        T t[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = (T)o[k];
+        if (left >= 8) {
+            __builtin_memcpy(out + e, t, sizeof t);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < left) out[e + k] = t[k];
+        }
+    }
 };
 
 struct ToMuon {
     float *x;
     float keep, lr;  // 1 - lr weight decay, lr
-    __device__ __forceinline__ void put(int64_t e, float o, float scale) const
+    __device__ __forceinline__ void put(int64_t e, const float *o, int left, float scale) const
     {
-        x[e] = keep * x[e] - (lr * scale) * o;
+        const float by = lr * scale;
+        if (left >= 8) {
+            float t[8];
+            __builtin_memcpy(t, x + e, sizeof t);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t[k] = keep * t[k] - by * o[k];
+            __builtin_memcpy(x + e, t, sizeof t);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < left) x[e + k] = keep * x[e + k] - by * o[k];
+        }
     }
 };
 
-struct NoOut {
-    __device__ __forceinline__ void put(int64_t, float, float) const {}
-};
+struct NoOut {};
 
 __device__ __forceinline__ float muon_scale(int mode, int rows, int cols)
 {
@@ -300,96 +313,278 @@ __device__ __forceinline__ float muon_scale(int mode, int rows, int cols)
     return 1.f;
 }
 
-constexpr int kRowBytes = kSlab * 2;            // 128 bytes of LDS per staged row
-constexpr int kStage = 2 * kTile * kRowBytes;   // one slab of both operands
+constexpr int kRowBytes = kSlab * 2;  // 128 bytes of LDS per staged row
 
-// Place of 16-byte chunk c of staged row r.  Eight lanes that read chunk c of
-// rows r..r+7 would meet in the same banks (a row is 128 bytes); the row's number
-// permutes its chunks so that any 16 consecutive rows cover all banks.
-__device__ __forceinline__ int lds_chunk(int r, int c) { return r * kRowBytes + ((c ^ (r >> 1)) & 7) * 16; }
-
-// Stages kTile rows of an operand: each wave 32 of them, 8 rows of 128 bytes per
-// instruction, straight into LDS (a wave's 64 lanes fill 1 KB in lane order, so
-// the permutation is applied to the address that is read).
-__device__ __forceinline__ void stage_rows(const _Float16 *src, int64_t pitch, char *lds)
+// Place of 16-byte chunk c of staged row r.  A fragment is chunk c of 32 rows;
+// a row is 128 bytes, so that all of them would begin in the same bank: the
+// row's number permutes its chunks, and any 16 consecutive rows cover all banks.
+__device__ __forceinline__ int row_chunk(int r, int c)
 {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-#pragma unroll
-    for (int k = 0; k < kTile / 32; ++k) {
-        const int r = wave * (kTile / 4) + k * 8 + (lane >> 3);
-        const int c = ((lane & 7) ^ (r >> 1)) & 7;
-        __builtin_amdgcn_global_load_lds(
-            (const __attribute__((address_space(1))) void *)(src + r * pitch + c * 8),
-            (__attribute__((address_space(3))) void *)(lds + (wave * (kTile / 4) + k * 8) * kRowBytes),
-            16, 0, 0);
-    }
+    return r * kRowBytes + ((c ^ (r >> 1)) & 7) * 16;
 }
 
-template <bool PAIRS, int STEP, class O>
-__global__ __launch_bounds__(256, 2) void k_product(const Mat *__restrict__ mats,
-                                                    const Item *__restrict__ items, int count,
-                                                    Areas w, Coefficients co, float faded, O out,
-                                                    int scale_mode)
+// The same for an operand that is staged with the summed index along its rows
+// (X in X <- B X): 32-byte chunks of row k are permuted by k mod 4 so that the four
+// rows and two chunks which 32 lanes of a transposing read take lie in different
+// banks, of 32 or of 64.
+__device__ __forceinline__ int deep_swizzle(int k)
 {
-    __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
-    __shared__ float scratch[4];
-    const int index = item_index();
-    if (index >= count) return;
-    const Item it = items[index];
+    const int b = k & 3;
+    return b << 1 | ((b >> 1) ^ (b & 1));
+}
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// The wave's number, in a scalar register.
+__device__ __forceinline__ int wave_number()
+{
+    return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+}
+
+// 16 bytes per lane, from `base` (the same in all lanes) + lane_at + scalar_at, to
+// consecutive places from `lds` on.  The base sits in scalar registers, in a
+// buffer resource of 2 GiB (its fourth word is the gfx9-family format word).  The
+// host compiler, which only needs the kernels' names, does not take the builtin
+// at this size.
+__device__ __forceinline__ void load_to_lds(const void *base, char *lds, int lane_at, int scalar_at)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const uint64_t a = (uint64_t)base;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+        (void *)(((uint64_t)hi << 32) | lo), (short)0, 0x7FFFFFFF, 0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)lds, 16, lane_at, scalar_at, 0, 0);
+#endif
+}
+
+// Stages BT rows of an operand, 8 rows of 128 bytes per instruction, straight
+// into LDS: a wave's 64 lanes fill 1 KB in lane order, so the permutation is
+// applied to the address that is read.  The base and a row block's offset (below
+// 256 rows of 2^22 bytes) are scalars, and two lane offsets serve all.
+template <int BT, int WAVES>
+struct RowStager {
+    static constexpr int kEach = BT / 8 / WAVES;  // instructions of a wave
+    static_assert(kEach % 2 == 0, "the permutation alternates with the instruction");
+    const char *base;
+    int pitch, lane_at[2];  // bytes
+    __device__ __forceinline__ RowStager(const _Float16 *src, int64_t row_numbers)
+        : base((const char *)src), pitch((int)row_numbers * 2)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            lane_at[k] = (lane >> 3) * pitch + ((lane & 7) ^ (4 * k | lane >> 4)) * 16;
+    }
+    __device__ __forceinline__ void operator()(int slab, char *lds) const
+    {
+        const char *from = base + (int64_t)slab * kRowBytes;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int block = wave_number() * kEach + k;
+            load_to_lds(from, lds + block * 1024, lane_at[k & 1], block * 8 * pitch);
+        }
+    }
+};
+
+// Stages a slab of an operand with the summed index along its rows: kSlab / kind
+// rows of BT numbers (pairs: of BT hi and BT lo).
+template <bool PAIRS, int BT, int WAVES>
+struct DeepStager {
+    static constexpr int kEach = BT / 8 / WAVES, kBytes = BT * (PAIRS ? 4 : 2);
+    static constexpr int kRows = 1024 / kBytes;  // of an instruction
+    static constexpr int kKinds = 4 / kRows;     // permutations that an instruction can have
+    static_assert(kRows <= 4 && kEach % kKinds == 0, "rows of an instruction");
+    const char *base;
+    int pitch, lane_at[kKinds];
+    __device__ __forceinline__ DeepStager(const _Float16 *src, int64_t row_numbers)
+        : base((const char *)src), pitch((int)row_numbers * 2)
+    {
+        const int at = (threadIdx.x & 63) * 16, r = at / kBytes, p = at % kBytes / 16;
+#pragma unroll
+        for (int k = 0; k < kKinds; ++k)
+            lane_at[k] = r * pitch + (((p >> 1) ^ deep_swizzle(k * kRows + r)) * 2 + (p & 1)) * 16;
+    }
+    __device__ __forceinline__ void operator()(int slab, char *lds) const
+    {
+        constexpr int kSlabRows = kSlab / (PAIRS ? 2 : 1);
+        const char *from = base + (int64_t)slab * kSlabRows * pitch;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int block = wave_number() * kEach + k;
+            load_to_lds(from, lds + block * 1024, lane_at[k % kKinds], block * kRows * pitch);
+        }
+    }
+};
+
+// Eight numbers of the summed index for 32 columns from a deep slab: two
+// transposing reads, each of 4 rows x 16 columns per 16 lanes.  at: the lane's
+// place for the first (deep_place); a row further on adds row_bytes.
+__device__ __forceinline__ half8 deep_fragment(const char *at, int row_bytes)
+{
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    typedef short v8s __attribute__((ext_vector_type(8)));
+    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) v4s *)at);
+    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) v4s *)(at + 4 * row_bytes));
+    return __builtin_bit_cast(half8, (v8s)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+__device__ __forceinline__ int deep_place(int row_bytes, int byte)
+{
+    const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
+    const int r = 8 * (g >> 1) + (j >> 2), at = byte + (g & 1) * 32 + (j & 3) * 8;
+    return r * row_bytes + ((at >> 5) ^ deep_swizzle(r)) * 32 + (at & 31);
+}
+
+// One product launch: a workgroup forms a BT x BT tile, each of its waves 32 WR x
+// 32 WC of it with 32 x 32 x 16 matrix instructions.  Slabs of both operands are
+// staged in two buffers by turns, the next one's loads in flight under the
+// present one's products.  Two buffers of their own, not halves of one: only then
+// does the compiler know that reading one need not wait for loads into the other.
+template <bool PAIRS, int STEP, int BT, int WR, int WC, int THREADS, class O>
+__global__ __launch_bounds__(THREADS, 2) void k_product(
+    const Mat *__restrict__ mats, const Item *__restrict__ items, Areas w, Coefficients co,
+    float faded, O out, int scale_mode)
+{
+    constexpr int kWaves = BT * BT / (1024 * WR * WC);
+    static_assert(THREADS == kWaves * 64, "a wave for every part of the tile");
+    constexpr int kOperand = BT * kRowBytes;
+    constexpr bool kDeep = STEP == kNext || STEP == kLast;
+    __shared__ __attribute__((aligned(1024))) char buffer0[2 * kOperand], buffer1[2 * kOperand];
+    __shared__ float scratch[kWaves];
+    const Item it = items[(blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds];
+    if (it.mat < 0) return;
     const Mat mt = mats[it.mat];
     constexpr int kind = PAIRS ? 2 : 1;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int wr = (wave >> 1) * 64, wc = (wave & 1) * 64;  // the wave's part of the tile
-    const int i0 = it.i * kTile, j0 = it.j * kTile;
+    const int wave = wave_number(), lane = threadIdx.x & 63;
+    constexpr int kAcross = BT / (32 * WC);
+    const int wr = wave / kAcross * (32 * WR), wc = wave % kAcross * (32 * WC);
+    const int i0 = it.i * BT, j0 = it.j * BT;
 
     const int64_t ex = mt.ex * kind, em = mt.em * kind;
-    const int64_t pitch = (int64_t)(STEP == kGram ? mt.np : mt.mp) * kind;
-    const _Float16 *pa = (STEP == kGram ? w.x + ex : STEP == kPoly ? w.d + em : w.b + em) + i0 * pitch;
-    const _Float16 *pb = (STEP == kGram ? w.x + ex : STEP == kPoly ? w.d + em : w.xt + ex) + j0 * pitch;
-    const int slabs = (int)(pitch / kSlab);
+    const int64_t x_pitch = (int64_t)mt.np * kind, d_pitch = (int64_t)mt.mp * kind;
+    const int64_t pitch = STEP == kGram ? x_pitch : d_pitch;
+    const _Float16 *x = w.x + ex, *d = w.d + em, *b = w.b + em;
+    const _Float16 *pa = (STEP == kGram ? x : STEP == kPoly ? d : b) + i0 * pitch;
+    const _Float16 *pb = kDeep ? x + j0 * kind : (STEP == kGram ? x : d) + j0 * pitch;
+    const int slabs = (int)(pitch / kSlab);  // even, as sides are multiples of 128
 
-    f32x16 acc[2][2] = {};
-    stage_rows(pa, pitch, lds);
-    stage_rows(pb, pitch, lds + kTile * kRowBytes);
-    __syncthreads();
-    for (int s = 0; s < slabs; ++s) {
-        const char *la = lds + (s & 1) * kStage, *lb = la + kTile * kRowBytes;
-        if (s + 1 < slabs) {
-            char *next = lds + ((s + 1) & 1) * kStage;
-            stage_rows(pa + (s + 1) * kSlab, pitch, next);
-            stage_rows(pb + (s + 1) * kSlab, pitch, next + kTile * kRowBytes);
-        }
-        const int row = lane & 31, up = lane >> 5;
-        auto frag = [&](const char *base, int r, int c) {
-            return *(const half8 *)(base + lds_chunk(r + row, c + up));
-        };
+    f32x16 acc[WR][WC] = {};
+    const RowStager<BT, kWaves> stage_a(pa, pitch);
+    const std::conditional_t<kDeep, DeepStager<PAIRS, BT, kWaves>, RowStager<BT, kWaves>> stage_b(
+        pb, kDeep ? x_pitch : pitch);
+    auto stage = [&](int s, char *to) {
+        stage_a(s, to);
+        stage_b(s, to + kOperand);
+    };
+    // Fragments of 16 numbers of the summed index: of a slab's kSteps, the k-th.
+    constexpr int kSteps = PAIRS ? 2 : 4, kDeepBytes = BT * 2 * kind;
+    struct Fragments {
+        half8 a[WR], b[WC], a_lo[PAIRS ? WR : 1], b_lo[PAIRS ? WC : 1];
+    };
+    // places that differ by more than a constant from one to the next
+    const int row = lane & 31, up = lane >> 5;
+    int place_a[4], place_b[4];
 #pragma unroll
-        for (int k = 0; k < (PAIRS ? 4 : 8); k += 2) {
-            half8 a[2], b[2], al[2], bl[2];
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                a[q] = frag(la, wr + q * 32, k);
-                b[q] = frag(lb, wc + q * 32, k);
-                if (PAIRS) {
-                    al[q] = frag(la, wr + q * 32, k + 4);
-                    bl[q] = frag(lb, wc + q * 32, k + 4);
-                }
-            }
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    acc[p][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[p], b[q], acc[p][q], 0, 0, 0);
-                    if (PAIRS) {
-                        acc[p][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[p], bl[q], acc[p][q], 0, 0, 0);
-                        acc[p][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(al[p], b[q], acc[p][q], 0, 0, 0);
-                    }
-                }
-        }
-        __syncthreads();
+    for (int c = 0; c < 4; ++c) {
+        place_a[c] = row_chunk(wr + row, c * 2 + up);
+        if (!kDeep) place_b[c] = kOperand + row_chunk(wc + row, c * 2 + up);
+        else place_b[c] = kOperand + deep_place(kDeepBytes, (wc + c / kind * 32) * 2 * kind + c % kind * 64);
     }
+    auto second = [&](const char *buffer, int k, int q, int lo) {
+        if (kDeep)
+            return deep_fragment(buffer + place_b[q * kind + lo] + k * 16 * kDeepBytes, kDeepBytes);
+        return *(const half8 *)(buffer + place_b[k + lo * 2] + q * 32 * kRowBytes);
+    };
+    auto load = [&](const char *buffer, int k, Fragments &f) {
+#pragma unroll
+        for (int p = 0; p < WR; ++p) f.a[p] = *(const half8 *)(buffer + place_a[k] + p * 32 * kRowBytes);
+#pragma unroll
+        for (int q = 0; q < WC; ++q) f.b[q] = second(buffer, k, q, 0);
+        if (PAIRS) {
+#pragma unroll
+            for (int q = 0; q < WC; ++q) f.b_lo[q] = second(buffer, k, q, 1);
+#pragma unroll
+            for (int p = 0; p < WR; ++p)
+                f.a_lo[p] = *(const half8 *)(buffer + place_a[k + 2] + p * 32 * kRowBytes);
+        }
+    };
+    auto multiply = [&](const Fragments &f) {
+        auto all = [&](const half8 *fa, const half8 *fb) {
+#pragma unroll
+            for (int p = 0; p < WR; ++p)
+#pragma unroll
+                for (int q = 0; q < WC; ++q)
+                    acc[p][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[p], fb[q], acc[p][q], 0, 0, 0);
+        };
+        all(f.a, f.b);
+        if (PAIRS) {
+            all(f.a, f.b_lo);
+            all(f.a_lo, f.b);
+        }
+    };
+    // Each step's products run while the next step's fragments are read: two reads,
+    // then one or two products, so that the reads are done well before the step is.
+    constexpr int kReads = (WR + (kDeep ? 2 : 1) * WC) * kind;
+    constexpr int kProducts = WR * WC * (PAIRS ? 3 : 1);
+    constexpr int kGroup = kReads * 2 <= kProducts ? 2 : 1;
+    constexpr int kRest = kProducts - kReads / 2 * kGroup;
+    Fragments f[2];
+    auto step = [&](const char *next, int k, int parity) {
+        load(next, k, f[parity ^ 1]);
+        multiply(f[parity]);
+#pragma unroll
+        for (int g = 0; g < kReads / 2; ++g) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, kGroup, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kRest, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto inner = [&](const char *now, int parity) {  // all of a slab's steps but the last
+#pragma unroll
+        for (int k = 0; k < kSteps - 1; ++k) step(now, k + 1, (parity + k) & 1);
+    };
+    // At a slab's last step all waves have read their fragments of it: its buffer
+    // takes the slab after the next, and the next one, a slab's time under way, is
+    // waited for.  The loop begins there, so that nothing is under way where it
+    // closes: the compiler would wait for all of it.
+    stage(0, buffer0);
+    stage(1, buffer1);
+    staged_sync();
+    load(buffer0, 0, f[0]);
+    inner(buffer0, 0);
+    constexpr int kLastParity = (kSteps - 1) & 1;
+    static_assert(kLastParity == 1, "fragments change places an even number of times a slab");
+    for (int s = 2; s < slabs; s += 2) {
+        staged_sync();
+        stage(s, buffer0);
+        step(buffer1, 0, 1);
+        inner(buffer1, 0);
+        staged_sync();
+        stage(s + 1, buffer1);
+        step(buffer0, 0, 1);
+        inner(buffer0, 0);
+    }
+    staged_sync();
+    step(buffer1, 0, 1);
+    inner(buffer1, 0);
+    multiply(f[1]);
+    staged_sync();
 
     // The shift, and the step's coefficients around it.
+    auto sum_over = [&](float v) {  // the workgroup's, the same in every thread
+        for (int k = 32; k > 0; k /= 2) v += __shfl_xor(v, k);
+        __syncthreads();
+        if (lane == 0) scratch[wave] = v;
+        __syncthreads();
+        float total = 0.f;
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) total += scratch[k];
+        return total;
+    };
     const float gamma0 = w.gamma[it.mat], gamma = fmaxf(gamma0 * faded, 1.f);
     const float inv2 = 1.f / (gamma * gamma);
     float t;
@@ -398,8 +593,8 @@ __global__ __launch_bounds__(256, 2) void k_product(const Mat *__restrict__ mats
             t = 1.f / (float)mt.m;
         } else {
             float sum = 0.f;
-            for (int k = threadIdx.x; k < mt.part_count; k += 256) sum += w.part[mt.part_first + k];
-            t = block_sum(sum, scratch) / (float)mt.m;
+            for (int k = threadIdx.x; k < mt.part_count; k += THREADS) sum += w.part[mt.part_first + k];
+            t = sum_over(sum) / (float)mt.m;
         }
         if (it.i == 0 && it.j == 0 && threadIdx.x == 0) w.t[it.mat] = t;
     } else {
@@ -412,118 +607,142 @@ __global__ __launch_bounds__(256, 2) void k_product(const Mat *__restrict__ mats
     const float linear = STEP == kPoly ? co.b + 2.f * co.c * tx
                                        : (co.a + (co.b + co.c * tx) * tx) * change;
     const float square = STEP == kPoly ? co.c * inv2 : inv2 * change;
+    constexpr float unscale = 1.f / kScale;
+    const float shift = STEP == kGram ? t * kScale : 0.f;
+    const float factor = STEP == kGram ? unscale : square * unscale;
 
-    // Values in place of the sums.  A lane holds column (lane & 31) and, in
-    // register r, row 8 (r / 4) + 4 (lane / 32) + r % 4 of a 32 x 32 part.
+    // The tile's values go through LDS, 32 x 64 of them at a time in a part of each
+    // wave's own, to be read back 8 in a row: what is read and written in memory
+    // is then whole lines.  A lane holds column (lane & 31) and, in register r, row
+    // 8 (r / 4) + 4 (lane / 32) + r % 4 of a 32 x 32 product.
+    float *mine = (float *)buffer0 + wave * 2048;
+    static_assert(kWaves * 2048 * 4 <= 2 * kOperand, "the epilogue's LDS");
     const int col = lane & 31, quad = (lane >> 5) * 4;
-    const float unscale = 1.f / kScale;
+    const int line = lane >> 3, eight = (lane & 7) * 8;  // of 8 rows, and 8 numbers of one
+    auto place = [&](int r, int c) { return r * 64 + (((c >> 2) ^ r) & 15) * 4 + (c & 3); };
+    auto take = [&](int r, float (&v)[8]) {
+        const f32x4 lo = *(const f32x4 *)(mine + place(r, eight));
+        const f32x4 hi = *(const f32x4 *)(mine + place(r, eight + 4));
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
+        for (int k = 0; k < 4; ++k) {
+            v[k] = lo[k];
+            v[4 + k] = hi[k];
+        }
+    };
+    float squares = 0.f;
+    // the values of 8 numbers of the output's row i from column j on, from their sums
+    auto value = [&](int i, int j, float (&v)[8]) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
+        for (int k = 0; k < 8; ++k) v[k] *= factor;
+        if constexpr (STEP == kGram) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int r = i0 + wr + p * 32 + g * 8 + quad, c = j0 + wc + q * 32 + col;
-                half4 hi = {}, lo = {};
-                if (STEP != kGram) {  // D(c, r..r+3), or XT(c, r..r+3)
-                    const _Float16 *line = (STEP == kPoly ? w.d + em : w.xt + ex) + c * pitch;
-                    if (PAIRS) {
-                        const _Float16 *at = line + (r >> 5) * 64 + (r & 31);
-                        hi = *(const half4 *)at;
-                        lo = *(const half4 *)(at + 32);
-                    } else {
-                        hi = *(const half4 *)(line + r);
-                        if (STEP != kPoly) lo = *(const half4 *)(w.xt_lo + ex + c * pitch + r);
+            for (int k = 0; k < 8; ++k)
+                if (i == j + k && i < mt.m) v[k] -= shift;
+        } else {
+            const _Float16 *from = STEP == kPoly ? d + i * d_pitch : x + i * x_pitch;
+            const half8 hi = *(const half8 *)(from + column<PAIRS>(j));
+            half8 lo = {};
+            if constexpr (PAIRS) lo = *(const half8 *)(from + column<PAIRS>(j) + 32);
+            else if constexpr (STEP != kPoly) lo = *(const half8 *)(w.x_lo + ex + i * x_pitch + j);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += linear * ((float)hi[k] + (float)lo[k]);
+        }
+    };
+    auto store = [&](int i, int j, const float (&v)[8]) {
+        half8 hi, lo;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            _Float16 h, l;
+            split(v[k], h, l);
+            hi[k] = h;
+            lo[k] = l;
+        }
+        _Float16 *to = STEP == kNext ? w.x_next + ex + i * x_pitch
+                                     : (STEP == kGram ? w.d : w.b) + em + i * d_pitch;
+        *(half8 *)(to + column<PAIRS>(j)) = hi;
+        if constexpr (PAIRS) *(half8 *)(to + column<PAIRS>(j) + 32) = lo;
+        else if constexpr (STEP == kNext) *(half8 *)(w.x_lo + ex + i * x_pitch + j) = lo;
+    };
+#pragma unroll
+    for (int p = 0; p < WR; ++p)
+#pragma unroll
+        for (int qq = 0; qq < WC; qq += 2) {  // 32 rows x 64 columns
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    mine[place((r >> 2) * 8 + quad + (r & 3), q * 32 + col)] = acc[p][qq + q][r];
+            wave_sync();
+            const int i1 = i0 + wr + p * 32, j1 = j0 + wc + qq * 32;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = k * 8 + line, i = i1 + r, j = j1 + eight;
+                float v[8];
+                take(r, v);
+                value(i, j, v);
+                if constexpr (STEP == kLast) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] *= unscale;
+                    if (!mt.flip) {
+                        if (i < mt.m && j < mt.n)
+                            out.put(mt.off + i * mt.ld + j, v, mt.n - j,
+                                    muon_scale(scale_mode, mt.rows, mt.cols));
+                    } else {  // back, to be read along the columns
+                        *(f32x4 *)(mine + place(r, eight)) = f32x4{v[0], v[1], v[2], v[3]};
+                        *(f32x4 *)(mine + place(r, eight + 4)) = f32x4{v[4], v[5], v[6], v[7]};
                     }
-                }
+                } else {
+                    if constexpr (STEP == kNext)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float v = acc[p][q][g * 4 + k] * unscale;
-                    if (STEP == kGram) {
-                        if (r + k == c && c < mt.m) v -= t * kScale;
-                    } else {
-                        const float old = (float)hi[k] + (float)lo[k];
-                        v = linear * old + square * v;
-                    }
-                    acc[p][q][g * 4 + k] = v;
+                        for (int e = 0; e < 8; ++e) squares += (v[e] * unscale) * (v[e] * unscale);
+                    store(i, j, v);
                 }
             }
-
-    if (STEP == kLast) {
-        const float scale = muon_scale(scale_mode, mt.rows, mt.cols) * unscale;
-        const float plain = unscale;
+            wave_sync();
+            if constexpr (STEP == kLast) {
+                if (mt.flip) {
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
+                    for (int k = 0; k < 4; ++k) {
+                        const int c = k * 16 + (lane >> 2), r = (lane & 3) * 8;
+                        float v[8];
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int i = i0 + wr + p * 32 + (r >> 2) * 8 + quad + (r & 3);
-                    const int j = j0 + wc + q * 32 + col;
-                    if (i < mt.m && j < mt.n)
-                        out.put(mt.off + (mt.flip ? j * mt.ld + i : i * mt.ld + j),
-                                acc[p][q][r] * plain, scale * kScale);
+                        for (int e = 0; e < 8; ++e) v[e] = mine[place(r + e, c)];
+                        if (i1 + r < mt.m && j1 + c < mt.n)
+                            out.put(mt.off + (j1 + c) * mt.ld + i1 + r, v, mt.m - (i1 + r),
+                                    muon_scale(scale_mode, mt.rows, mt.cols));
+                    }
+                    wave_sync();
                 }
-        return;
+            }
+        }
+    if constexpr (STEP == kNext) {
+        const float sum = sum_over(squares);
+        if (threadIdx.x == 0) w.part[mt.part_first + it.i * (mt.np / BT) + it.j] = sum;
     }
-
-    if (STEP == kNext) {
-        float sum = 0.f;
+    if constexpr (STEP == kGram || STEP == kPoly) {
+        if (it.i == it.j) return;  // a diagonal tile is its own transpose
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
+        for (int q = 0; q < WC; ++q)
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+            for (int pp = 0; pp < WR; pp += 2) {  // 32 columns x 64 rows
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float v = acc[p][q][r] * unscale;
-                    sum += v * v;
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        *(f32x4 *)(mine + place(col, p * 32 + g * 8 + quad)) =
+                            f32x4{acc[pp + p][q][g * 4], acc[pp + p][q][g * 4 + 1],
+                                  acc[pp + p][q][g * 4 + 2], acc[pp + p][q][g * 4 + 3]};
+                wave_sync();
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int r = k * 8 + line, i = j0 + wc + q * 32 + r, j = i0 + wr + pp * 32 + eight;
+                    float v[8];
+                    take(r, v);
+                    value(i, j, v);
+                    store(i, j, v);
                 }
-        sum = block_sum(sum, scratch);
-        if (threadIdx.x == 0) w.part[mt.part_first + it.i * (mt.np / kTile) + it.j] = sum;
-    }
-
-    // Both orientations, through the wave's own part of LDS, so that a row's 64
-    // numbers are written by two lanes, 32 each.
-    constexpr int kPitch = 68;  // words
-    uint32_t *mine = (uint32_t *)(lds) + wave * (32 * kPitch);
-    static_assert(4 * 32 * kPitch * 4 <= 2 * kStage, "the epilogue's LDS");
-    _Float16 *rows_to = (STEP == kGram ? w.d + em : STEP == kPoly ? w.b + em : w.x + ex);
-    const int64_t rows_pitch = (int64_t)(STEP == kNext ? mt.np : mt.mp) * kind;
-    _Float16 *cols_to = STEP == kNext ? w.xt_next + ex : rows_to;
-    const int64_t cols_pitch = (int64_t)mt.mp * kind;
-    const int line = lane >> 1, part = (lane & 1) * 32;
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {  // 32 rows x 64 columns at a time
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                mine[((r >> 2) * 8 + quad + (r & 3)) * kPitch + q * 32 + col] = pack(acc[p][q][r]);
-        wave_sync();
-        uint32_t u[32];
-#pragma unroll
-        for (int k = 0; k < 32; k += 4) *(v4u *)(u + k) = *(const v4u *)(mine + line * kPitch + part + k);
-        put_row<PAIRS>(rows_to + (i0 + wr + p * 32 + line) * rows_pitch, nullptr, j0 + wc + part, u);
-        wave_sync();
-    }
-    if (STEP != kNext && it.i == it.j) return;  // a diagonal tile is its own transpose
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {  // 32 columns x 64 rows at a time
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *(v4u *)(mine + col * kPitch + p * 32 + g * 8 + quad) =
-                    v4u{pack(acc[p][q][g * 4]), pack(acc[p][q][g * 4 + 1]),
-                        pack(acc[p][q][g * 4 + 2]), pack(acc[p][q][g * 4 + 3])};
-        wave_sync();
-        uint32_t u[32];
-#pragma unroll
-        for (int k = 0; k < 32; k += 4) *(v4u *)(u + k) = *(const v4u *)(mine + line * kPitch + part + k);
-        const int64_t at = (int64_t)(j0 + wc + q * 32 + line) * cols_pitch;
-        put_row<PAIRS>(cols_to + at, !PAIRS && STEP == kNext ? w.xt_lo + ex + at : nullptr,
-                       i0 + wr + part, u);
-        wave_sync();
+                wave_sync();
+            }
     }
 }
 
@@ -536,7 +755,9 @@ struct onebit_matrices_s {
     int device = 0;
     int32_t count = 0;
     int64_t extent = 0, ex = 0, em = 0;
-    int64_t norms = 0, firsts = 0, syms = 0, nexts = 0;
+    int tile = 128;
+    int64_t norms = 0, firsts = 0, parts = 0;
+    int64_t sym_blocks = 0, next_blocks = 0;  // workgroups of the products' launches
     std::vector<int64_t> offset;
     char *dev = nullptr;
     const Mat *mats = nullptr;
@@ -555,7 +776,7 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
     } while (0)
 
 struct WorkspaceLayout {
-    size_t x, xt0, xt1, xt_lo, d, b, norm, part, t, gamma, total;
+    size_t x0, x1, x_lo, d, b, norm, part, t, gamma, total;
 };
 
 WorkspaceLayout layout_of(const onebit_matrices_s *p, bool pairs)
@@ -568,18 +789,64 @@ WorkspaceLayout layout_of(const onebit_matrices_s *p, bool pairs)
         return here;
     };
     const size_t half = pairs ? 4 : 2;
-    l.x = take(half * p->ex);
-    l.xt0 = take(half * p->ex);
-    l.xt1 = take(half * p->ex);
-    l.xt_lo = take(pairs ? 0 : 2 * p->ex);
+    l.x0 = take(half * p->ex);
+    l.x1 = take(half * p->ex);
+    l.x_lo = take(pairs ? 0 : 2 * p->ex);
     l.d = take(half * p->em);
     l.b = take(half * p->em);
     l.norm = take(8 * (size_t)p->norms);
-    l.part = take(4 * (size_t)p->nexts);
+    l.part = take(4 * (size_t)p->parts);
     l.t = take(4 * (size_t)p->count);
     l.gamma = take(4 * (size_t)p->count);
     l.total = at;
     return l;
+}
+
+// Side of the products' tiles for a list: 256, which reads half as much for each
+// product, where such tiles are enough to fill the GPU; 128 otherwise.
+int tile_for(const int64_t *rows, const int64_t *cols, int32_t count)
+{
+    int64_t tiles = 0;
+    for (int32_t k = 0; k < count; ++k)
+        tiles += std::max<int64_t>(0, (rows[k] + 255) / 256) * std::max<int64_t>(0, (cols[k] + 255) / 256);
+    return tiles >= 1024 ? 256 : 128;
+}
+
+// Workgroups go to the XCDs round-robin, and each XCD has an L2 of its own: a
+// matrix's tiles go to one XCD as far as that keeps the XCDs' work even.  Items
+// (with what one costs, the dearest first) are dealt out in runs of one matrix, each
+// to the XCD with the least so far; entry x * length + k is XCD x's k-th.
+struct Costed {
+    Item item;
+    int64_t cost;
+};
+
+std::vector<Item> deal(std::vector<Costed> all)
+{
+    std::stable_sort(all.begin(), all.end(),
+                     [](const Costed &a, const Costed &b) { return a.cost > b.cost; });
+    int64_t total = 0;
+    for (const Costed &c : all) total += c.cost;
+    const int64_t most = total / (kXcds * 8);  // of a run
+    std::vector<Item> lists[kXcds];
+    int64_t load[kXcds] = {};
+    for (size_t k = 0; k < all.size();) {
+        const int to = (int)(std::min_element(load, load + kXcds) - load);
+        int64_t run = 0;
+        const int32_t mat = all[k].item.mat;
+        do {
+            lists[to].push_back(all[k].item);
+            run += all[k].cost;
+            ++k;
+        } while (k < all.size() && all[k].item.mat == mat && run + all[k].cost <= most);
+        load[to] += run;
+    }
+    size_t length = 0;
+    for (const auto &l : lists) length = std::max(length, l.size());
+    std::vector<Item> out(length * kXcds, Item{-1, 0, 0});
+    for (int x = 0; x < kXcds; ++x)
+        std::copy(lists[x].begin(), lists[x].end(), out.begin() + x * length);
+    return out;
 }
 
 int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
@@ -589,10 +856,12 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
     hipError_t e = hipGetDevice(&p->device);
     if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
     std::vector<Mat> mats(count);
-    std::vector<Item> norm, first, sym, next;
+    std::vector<Item> norm, first;
+    std::vector<Costed> sym, next;
     p->count = count;
     p->offset.resize(count);
     int64_t at = 0;
+    const int tile = p->tile = tile_for(rows, cols, count);
     constexpr int64_t kSide = 1 << 20, kMost = (int64_t)1 << 40, kItems = 1 << 23;
     for (int32_t k = 0; k < count; ++k) {
         const int64_t r = rows[k], c = cols[k];
@@ -624,13 +893,13 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
         m.m = (int32_t)std::min(r, c);
         m.n = (int32_t)std::max(r, c);
         if (m.m == 0) continue;
-        m.mp = (m.m + kTile - 1) / kTile * kTile;
-        m.np = (m.n + kTile - 1) / kTile * kTile;
+        m.mp = (m.m + tile - 1) / tile * tile;
+        m.np = (m.n + tile - 1) / tile * tile;
         m.ex = p->ex;
         m.em = p->em;
         p->ex += (int64_t)m.mp * m.np;
         p->em += (int64_t)m.mp * m.mp;
-        const int tm = m.mp / kTile, tn = m.np / kTile;
+        const int tm = m.mp / tile, tn = m.np / tile;
         m.norm_first = (int32_t)norm.size();
         m.norm_count = (int32_t)((r * c + kNormChunk - 1) / kNormChunk);
         m.part_first = (int32_t)next.size();
@@ -643,14 +912,18 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
         for (int i = 0; i < rp; ++i)
             for (int j = 0; j < cp; ++j) first.push_back(Item{k, (uint16_t)i, (uint16_t)j});
         for (int i = 0; i < tm; ++i)
-            for (int j = 0; j <= i; ++j) sym.push_back(Item{k, (uint16_t)i, (uint16_t)j});
+            for (int j = 0; j <= i; ++j)
+                sym.push_back(Costed{{k, (uint16_t)i, (uint16_t)j}, m.np + m.mp});
         for (int i = 0; i < tm; ++i)
-            for (int j = 0; j < tn; ++j) next.push_back(Item{k, (uint16_t)i, (uint16_t)j});
+            for (int j = 0; j < tn; ++j)
+                next.push_back(Costed{{k, (uint16_t)i, (uint16_t)j}, m.mp});
     }
     p->norms = (int64_t)norm.size();
     p->firsts = (int64_t)first.size();
-    p->syms = (int64_t)sym.size();
-    p->nexts = (int64_t)next.size();
+    p->parts = (int64_t)next.size();
+    const std::vector<Item> sym_dealt = deal(std::move(sym)), next_dealt = deal(std::move(next));
+    p->sym_blocks = (int64_t)sym_dealt.size();
+    p->next_blocks = (int64_t)next_dealt.size();
     // one host buffer in the layout of the device allocation
     size_t total = 0;
     auto take = [&](size_t bytes) {
@@ -660,7 +933,8 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
     };
     const size_t o_mats = take(mats.size() * sizeof(Mat));
     const size_t o_norm = take(norm.size() * sizeof(Item)), o_first = take(first.size() * sizeof(Item));
-    const size_t o_sym = take(sym.size() * sizeof(Item)), o_next = take(next.size() * sizeof(Item));
+    const size_t o_sym = take(sym_dealt.size() * sizeof(Item));
+    const size_t o_next = take(next_dealt.size() * sizeof(Item));
     std::vector<char> host(total);
     auto copy = [&](size_t to, const auto &v) {
         if (!v.empty()) std::memcpy(host.data() + to, v.data(), v.size() * sizeof(v[0]));
@@ -668,8 +942,8 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
     copy(o_mats, mats);
     copy(o_norm, norm);
     copy(o_first, first);
-    copy(o_sym, sym);
-    copy(o_next, next);
+    copy(o_sym, sym_dealt);
+    copy(o_next, next_dealt);
     void *dev = nullptr;
     e = hipMalloc(&dev, total);
     if (e == hipErrorOutOfMemory) return fail(ONEBIT_ENOMEM, "hipMalloc of the matrix tables");
@@ -754,7 +1028,26 @@ int check_coefficients(Coefficients &k, int steps)
     return ONEBIT_OK;
 }
 
-int grid8(int64_t items) { return (int)((items + kXcds - 1) / kXcds * kXcds); }
+template <bool PAIRS, int BT, int WR, int WC, class O>
+void products(const onebit_matrices_s *p, Areas w, const O &out, int scale_mode, int steps,
+              const Coefficients &co, hipStream_t st)
+{
+    constexpr int kThreads = BT * BT / (16 * WR * WC);
+    float faded = 1.f;
+    for (int k = 0; k < steps; ++k, faded *= co.fade) {
+        k_product<PAIRS, kGram, BT, WR, WC, kThreads, NoOut><<<p->sym_blocks, kThreads, 0, st>>>(
+            p->mats, p->sym_items, w, co, faded, NoOut{}, 0);
+        k_product<PAIRS, kPoly, BT, WR, WC, kThreads, NoOut><<<p->sym_blocks, kThreads, 0, st>>>(
+            p->mats, p->sym_items, w, co, faded, NoOut{}, 0);
+        if (k + 1 < steps)
+            k_product<PAIRS, kNext, BT, WR, WC, kThreads, NoOut><<<p->next_blocks, kThreads, 0, st>>>(
+                p->mats, p->next_items, w, co, faded, NoOut{}, 0);
+        else
+            k_product<PAIRS, kLast, BT, WR, WC, kThreads, O><<<p->next_blocks, kThreads, 0, st>>>(
+                p->mats, p->next_items, w, co, faded, out, scale_mode);
+        std::swap(w.x, w.x_next);
+    }
+}
 
 // Everything after the arguments' checks: `src` is what is orthogonalised.
 template <bool PAIRS, class S, class O>
@@ -763,27 +1056,16 @@ int run(const onebit_matrices_s *p, const S &src, const O &out, int scale_mode, 
 {
     const WorkspaceLayout l = layout_of(p, PAIRS);
     char *ws = (char *)workspace;
-    Areas w{(_Float16 *)(ws + l.x), (_Float16 *)(ws + l.xt0), (_Float16 *)(ws + l.xt1),
-            (_Float16 *)(ws + l.xt_lo), (_Float16 *)(ws + l.d), (_Float16 *)(ws + l.b),
+    Areas w{(_Float16 *)(ws + l.x0), (_Float16 *)(ws + l.x1), (_Float16 *)(ws + l.x_lo),
+            (_Float16 *)(ws + l.d), (_Float16 *)(ws + l.b),
             (double *)(ws + l.norm), (float *)(ws + l.part), (float *)(ws + l.t),
             (float *)(ws + l.gamma)};
     k_norm<S><<<(int)p->norms, 256, 0, st>>>(p->mats, p->norm_items, src, w.norm);
     k_first<PAIRS, S><<<(int)p->firsts, 256, 0, st>>>(p->mats, p->first_items, src, (double)eps, w);
-    const int gs = grid8(p->syms), gn = grid8(p->nexts);
-    float faded = 1.f;
-    for (int k = 0; k < steps; ++k, faded *= co.fade) {
-        k_product<PAIRS, kGram, NoOut><<<gs, 256, 0, st>>>(p->mats, p->sym_items, (int)p->syms, w,
-                                                           co, faded, NoOut{}, 0);
-        k_product<PAIRS, kPoly, NoOut><<<gs, 256, 0, st>>>(p->mats, p->sym_items, (int)p->syms, w,
-                                                           co, faded, NoOut{}, 0);
-        if (k + 1 < steps)
-            k_product<PAIRS, kNext, NoOut><<<gn, 256, 0, st>>>(
-                p->mats, p->next_items, (int)p->nexts, w, co, faded, NoOut{}, 0);
-        else
-            k_product<PAIRS, kLast, O><<<gn, 256, 0, st>>>(
-                p->mats, p->next_items, (int)p->nexts, w, co, faded, out, scale_mode);
-        std::swap(w.xt, w.xt_next);
-    }
+    if (p->tile == 256)
+        products<PAIRS, 256, 4, 2>(p, w, out, scale_mode, steps, co, st);
+    else
+        products<PAIRS, 128, 2, 2>(p, w, out, scale_mode, steps, co, st);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? ONEBIT_OK : hip_fail(e, "matrix kernel launch");
 }
