@@ -114,6 +114,15 @@ __device__ __forceinline__ void staged_sync()
     __syncthreads();
 }
 
+// Workgroup barrier that waits for no loads of the wave's own (their count is
+// awaited before it, where that matters).
+__device__ __forceinline__ void bare_sync()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // Sum over the workgroup of 256, the same in every thread; scratch: 4 values.
 template <class T>
 __device__ __forceinline__ T block_sum(T v, T *scratch)
@@ -326,11 +335,13 @@ __device__ __forceinline__ int row_chunk(int r, int c)
 // The same for an operand that is staged with the summed index along its rows
 // (X in X <- B X): 32-byte chunks of row k are permuted by k mod 4 so that the four
 // rows and two chunks which 32 lanes of a transposing read take lie in different
-// banks, of 32 or of 64.
+// banks, of 32 or of 64 (rows of 128 bytes have four chunks, and lie in both
+// halves of 64 banks by themselves).
+template <int ROW_BYTES>
 __device__ __forceinline__ int deep_swizzle(int k)
 {
     const int b = k & 3;
-    return b << 1 | ((b >> 1) ^ (b & 1));
+    return ROW_BYTES == 128 ? b : b << 1 | ((b >> 1) ^ (b & 1));
 }
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -367,9 +378,9 @@ struct RowStager {
     static constexpr int kEach = BT / 8 / WAVES;  // instructions of a wave
     static_assert(kEach % 2 == 0, "the permutation alternates with the instruction");
     const char *base;
-    int pitch, lane_at[2];  // bytes
-    __device__ __forceinline__ RowStager(const _Float16 *src, int64_t row_numbers)
-        : base((const char *)src), pitch((int)row_numbers * 2)
+    int pitch, wave, lane_at[2];  // bytes, but for the wave's number
+    __device__ __forceinline__ RowStager(const _Float16 *src, int64_t row_numbers, int wave_)
+        : base((const char *)src), pitch((int)row_numbers * 2), wave(wave_)
     {
         const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -381,7 +392,7 @@ struct RowStager {
         const char *from = base + (int64_t)slab * kRowBytes;
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
-            const int block = wave_number() * kEach + k;
+            const int block = wave * kEach + k;
             load_to_lds(from, lds + block * 1024, lane_at[k & 1], block * 8 * pitch);
         }
     }
@@ -393,17 +404,17 @@ template <bool PAIRS, int BT, int WAVES>
 struct DeepStager {
     static constexpr int kEach = BT / 8 / WAVES, kBytes = BT * (PAIRS ? 4 : 2);
     static constexpr int kRows = 1024 / kBytes;  // of an instruction
-    static constexpr int kKinds = 4 / kRows;     // permutations that an instruction can have
-    static_assert(kRows <= 4 && kEach % kKinds == 0, "rows of an instruction");
+    static constexpr int kKinds = kRows < 4 ? 4 / kRows : 1;  // permutations of an instruction
+    static_assert(kEach % kKinds == 0, "rows of an instruction");
     const char *base;
-    int pitch, lane_at[kKinds];
-    __device__ __forceinline__ DeepStager(const _Float16 *src, int64_t row_numbers)
-        : base((const char *)src), pitch((int)row_numbers * 2)
+    int pitch, wave, lane_at[kKinds];
+    __device__ __forceinline__ DeepStager(const _Float16 *src, int64_t row_numbers, int wave_)
+        : base((const char *)src), pitch((int)row_numbers * 2), wave(wave_)
     {
         const int at = (threadIdx.x & 63) * 16, r = at / kBytes, p = at % kBytes / 16;
 #pragma unroll
         for (int k = 0; k < kKinds; ++k)
-            lane_at[k] = r * pitch + (((p >> 1) ^ deep_swizzle(k * kRows + r)) * 2 + (p & 1)) * 16;
+            lane_at[k] = r * pitch + (((p >> 1) ^ deep_swizzle<kBytes>(k * kRows + r)) * 2 + (p & 1)) * 16;
     }
     __device__ __forceinline__ void operator()(int slab, char *lds) const
     {
@@ -411,7 +422,7 @@ struct DeepStager {
         const char *from = base + (int64_t)slab * kSlabRows * pitch;
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
-            const int block = wave_number() * kEach + k;
+            const int block = wave * kEach + k;
             load_to_lds(from, lds + block * 1024, lane_at[k % kKinds], block * kRows * pitch);
         }
     }
@@ -419,23 +430,25 @@ struct DeepStager {
 
 // Eight numbers of the summed index for 32 columns from a deep slab: two
 // transposing reads, each of 4 rows x 16 columns per 16 lanes.  at: the lane's
-// place for the first (deep_place); a row further on adds row_bytes.
-__device__ __forceinline__ half8 deep_fragment(const char *at, int row_bytes)
+// place for the first (deep_place).
+template <int ROW_BYTES>
+__device__ __forceinline__ half8 deep_fragment(const char *at)
 {
     typedef short v4s __attribute__((ext_vector_type(4)));
     typedef short v8s __attribute__((ext_vector_type(8)));
     const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
         (__attribute__((address_space(3))) v4s *)at);
     const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) v4s *)(at + 4 * row_bytes));
+        (__attribute__((address_space(3))) v4s *)(at + 4 * ROW_BYTES));
     return __builtin_bit_cast(half8, (v8s)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-__device__ __forceinline__ int deep_place(int row_bytes, int byte)
+template <int ROW_BYTES>
+__device__ __forceinline__ int deep_place(int byte)
 {
     const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     const int r = 8 * (g >> 1) + (j >> 2), at = byte + (g & 1) * 32 + (j & 3) * 8;
-    return r * row_bytes + ((at >> 5) ^ deep_swizzle(r)) * 32 + (at & 31);
+    return r * ROW_BYTES + ((at >> 5) ^ deep_swizzle<ROW_BYTES>(r)) * 32 + (at & 31);
 }
 
 // One product launch: a workgroup forms a BT x BT tile, each of its waves 32 WR x
@@ -443,22 +456,28 @@ __device__ __forceinline__ int deep_place(int row_bytes, int byte)
 // staged in two buffers by turns, the next one's loads in flight under the
 // present one's products.  Two buffers of their own, not halves of one: only then
 // does the compiler know that reading one need not wait for loads into the other.
-template <bool PAIRS, int STEP, int BT, int WR, int WC, int THREADS, class O>
+// With KG above 1 that many groups of waves form the same tile, each from slabs of
+// its own (the k-th slab goes to group k mod KG) in buffers of its own, and their
+// sums are added at the end: for lists with fewer tiles than the GPU has CUs, where
+// the wait for a slab is what counts.
+template <bool PAIRS, int STEP, int BT, int WR, int WC, int KG, int THREADS, class O>
 __global__ __launch_bounds__(THREADS, 2) void k_product(
     const Mat *__restrict__ mats, const Item *__restrict__ items, Areas w, Coefficients co,
     float faded, O out, int scale_mode)
 {
     constexpr int kWaves = BT * BT / (1024 * WR * WC);
-    static_assert(THREADS == kWaves * 64, "a wave for every part of the tile");
+    static_assert(THREADS == KG * kWaves * 64, "a wave for every part of the tile");
     constexpr int kOperand = BT * kRowBytes;
     constexpr bool kDeep = STEP == kNext || STEP == kLast;
-    __shared__ __attribute__((aligned(1024))) char buffer0[2 * kOperand], buffer1[2 * kOperand];
-    __shared__ float scratch[kWaves];
+    __shared__ __attribute__((aligned(1024))) char buffer0[KG * 2 * kOperand],
+        buffer1[KG * 2 * kOperand];
+    __shared__ float scratch[KG * kWaves];
     const Item it = items[(blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds];
     if (it.mat < 0) return;
     const Mat mt = mats[it.mat];
     constexpr int kind = PAIRS ? 2 : 1;
-    const int wave = wave_number(), lane = threadIdx.x & 63;
+    const int group = KG > 1 ? wave_number() / kWaves : 0, wave = wave_number() - group * kWaves;
+    const int lane = threadIdx.x & 63;
     constexpr int kAcross = BT / (32 * WC);
     const int wr = wave / kAcross * (32 * WR), wc = wave % kAcross * (32 * WC);
     const int i0 = it.i * BT, j0 = it.j * BT;
@@ -469,12 +488,12 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     const _Float16 *x = w.x + ex, *d = w.d + em, *b = w.b + em;
     const _Float16 *pa = (STEP == kGram ? x : STEP == kPoly ? d : b) + i0 * pitch;
     const _Float16 *pb = kDeep ? x + j0 * kind : (STEP == kGram ? x : d) + j0 * pitch;
-    const int slabs = (int)(pitch / kSlab);  // even, as sides are multiples of 128
+    const int slabs = (int)(pitch / kSlab);  // even, but for tiles of 64
 
     f32x16 acc[WR][WC] = {};
-    const RowStager<BT, kWaves> stage_a(pa, pitch);
+    const RowStager<BT, kWaves> stage_a(pa, pitch, wave);
     const std::conditional_t<kDeep, DeepStager<PAIRS, BT, kWaves>, RowStager<BT, kWaves>> stage_b(
-        pb, kDeep ? x_pitch : pitch);
+        pb, kDeep ? x_pitch : pitch, wave);
     auto stage = [&](int s, char *to) {
         stage_a(s, to);
         stage_b(s, to + kOperand);
@@ -491,11 +510,11 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     for (int c = 0; c < 4; ++c) {
         place_a[c] = row_chunk(wr + row, c * 2 + up);
         if (!kDeep) place_b[c] = kOperand + row_chunk(wc + row, c * 2 + up);
-        else place_b[c] = kOperand + deep_place(kDeepBytes, (wc + c / kind * 32) * 2 * kind + c % kind * 64);
+        else place_b[c] = kOperand + deep_place<kDeepBytes>((wc + c / kind * 32) * 2 * kind + c % kind * 64);
     }
     auto second = [&](const char *buffer, int k, int q, int lo) {
         if (kDeep)
-            return deep_fragment(buffer + place_b[q * kind + lo] + k * 16 * kDeepBytes, kDeepBytes);
+            return deep_fragment<kDeepBytes>(buffer + place_b[q * kind + lo] + k * 16 * kDeepBytes);
         return *(const half8 *)(buffer + place_b[k + lo * 2] + q * 32 * kRowBytes);
     };
     auto load = [&](const char *buffer, int k, Fragments &f) {
@@ -525,64 +544,98 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
             all(f.a_lo, f.b);
         }
     };
-    // Each step's products run while the next step's fragments are read: two reads,
-    // then one or two products, so that the reads are done well before the step is.
-    constexpr int kReads = (WR + (kDeep ? 2 : 1) * WC) * kind;
-    constexpr int kProducts = WR * WC * (PAIRS ? 3 : 1);
-    constexpr int kGroup = kReads * 2 <= kProducts ? 2 : 1;
-    constexpr int kRest = kProducts - kReads / 2 * kGroup;
-    Fragments f[2];
-    auto step = [&](const char *next, int k, int parity) {
-        load(next, k, f[parity ^ 1]);
-        multiply(f[parity]);
+    if constexpr (KG == 1) {
+        // Each step's products run while the next step's fragments are read: two reads,
+        // then one or two products, so that the reads are done well before the step is.
+        constexpr int kReads = (WR + (kDeep ? 2 : 1) * WC) * kind;
+        constexpr int kProducts = WR * WC * (PAIRS ? 3 : 1);
+        constexpr int kGroup = kReads * 2 <= kProducts ? 2 : 1;
+        constexpr int kRest = kProducts - kReads / 2 * kGroup;
+        Fragments f[2];
+        auto step = [&](const char *next, int k, int parity) {
+            load(next, k, f[parity ^ 1]);
+            multiply(f[parity]);
 #pragma unroll
-        for (int g = 0; g < kReads / 2; ++g) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, kGroup, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, kRest, 0);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    auto inner = [&](const char *now, int parity) {  // all of a slab's steps but the last
+            for (int g = 0; g < kReads / 2; ++g) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, kGroup, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, kRest, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto inner = [&](const char *now, int parity) {  // all of a slab's steps but the last
 #pragma unroll
-        for (int k = 0; k < kSteps - 1; ++k) step(now, k + 1, (parity + k) & 1);
-    };
-    // At a slab's last step all waves have read their fragments of it: its buffer
-    // takes the slab after the next, and the next one, a slab's time under way, is
-    // waited for.  The loop begins there, so that nothing is under way where it
-    // closes: the compiler would wait for all of it.
-    stage(0, buffer0);
-    stage(1, buffer1);
-    staged_sync();
-    load(buffer0, 0, f[0]);
-    inner(buffer0, 0);
-    constexpr int kLastParity = (kSteps - 1) & 1;
-    static_assert(kLastParity == 1, "fragments change places an even number of times a slab");
-    for (int s = 2; s < slabs; s += 2) {
+            for (int k = 0; k < kSteps - 1; ++k) step(now, k + 1, (parity + k) & 1);
+        };
+        // At a slab's last step all waves have read their fragments of it: its buffer
+        // takes the slab after the next, and the next one, a slab's time under way, is
+        // waited for.  The loop begins there, so that nothing is under way where it
+        // closes: the compiler would wait for all of it.
+        stage(0, buffer0);
+        stage(1, buffer1);
         staged_sync();
-        stage(s, buffer0);
+        load(buffer0, 0, f[0]);
+        inner(buffer0, 0);
+        constexpr int kLastParity = (kSteps - 1) & 1;
+        static_assert(kLastParity == 1, "fragments change places an even number of times a slab");
+        for (int s = 2; s < slabs; s += 2) {
+            staged_sync();
+            stage(s, buffer0);
+            step(buffer1, 0, 1);
+            inner(buffer1, 0);
+            staged_sync();
+            stage(s + 1, buffer1);
+            step(buffer0, 0, 1);
+            inner(buffer0, 0);
+        }
+        staged_sync();
         step(buffer1, 0, 1);
         inner(buffer1, 0);
+        multiply(f[1]);
         staged_sync();
-        stage(s + 1, buffer1);
-        step(buffer0, 0, 1);
-        inner(buffer0, 0);
+    } else {
+        char *const mine[2] = {buffer0 + group * 2 * kOperand, buffer1 + group * 2 * kOperand};
+        const int rounds = (slabs + KG - 1) / KG, own = (slabs - group + KG - 1) / KG;
+        auto whole = [&](const char *from) {
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                Fragments f;
+                load(from, k, f);
+                multiply(f);
+            }
+        };
+        // two slabs of the group are under way: the older one is waited for, and its
+        // buffer filled again once all waves have read it
+        constexpr int kLoads = 2 * BT / 8 / kWaves;  // of a wave for a slab
+        auto round = [&](int s, char *from) {
+            if (s < own) {
+                if (s + 1 < own) __builtin_amdgcn_s_waitcnt(0x0f70 | kLoads);  // vmcnt(kLoads)
+                else __builtin_amdgcn_s_waitcnt(0x0f70);
+            }
+            bare_sync();
+            if (s < own) whole(from);
+            bare_sync();
+            if (s + 2 < own) stage((s + 2) * KG + group, from);
+        };
+        static_assert(kLoads < 16, "the counter's low bits");
+        if (own > 0) stage(group, mine[0]);
+        if (own > 1) stage(KG + group, mine[1]);
+        for (int s = 0; s < rounds; s += 2) {
+            round(s, mine[0]);
+            if (s + 1 < rounds) round(s + 1, mine[1]);
+        }
+        __syncthreads();
     }
-    staged_sync();
-    step(buffer1, 0, 1);
-    inner(buffer1, 0);
-    multiply(f[1]);
-    staged_sync();
 
     // The shift, and the step's coefficients around it.
     auto sum_over = [&](float v) {  // the workgroup's, the same in every thread
         for (int k = 32; k > 0; k /= 2) v += __shfl_xor(v, k);
         __syncthreads();
-        if (lane == 0) scratch[wave] = v;
+        if (lane == 0) scratch[wave_number()] = v;
         __syncthreads();
         float total = 0.f;
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k) total += scratch[k];
+        for (int k = 0; k < KG * kWaves; ++k) total += scratch[k];
         return total;
     };
     const float gamma0 = w.gamma[it.mat], gamma = fmaxf(gamma0 * faded, 1.f);
@@ -615,14 +668,27 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     // wave's own, to be read back 8 in a row: what is read and written in memory
     // is then whole lines.  A lane holds column (lane & 31) and, in register r, row
     // 8 (r / 4) + 4 (lane / 32) + r % 4 of a 32 x 32 product.
-    float *mine = (float *)buffer0 + wave * 2048;
+    // With several groups every wave leaves its sums there, and adds and finishes the
+    // KG-th part of the rows that its group has.
+    static_assert(KG == 1 || (KG == 4 && WR == 1 && WC == 2), "a quarter of 32 rows for a group");
     static_assert(kWaves * 2048 * 4 <= 2 * kOperand, "the epilogue's LDS");
+    float *const mine = (float *)buffer0 + wave_number() * 2048;
+    float *const sums = (float *)buffer0 + wave * 2048;  // the first group's
+    auto part_sync = [&] {
+        if constexpr (KG > 1) __syncthreads();
+        else wave_sync();
+    };
     const int col = lane & 31, quad = (lane >> 5) * 4;
     const int line = lane >> 3, eight = (lane & 7) * 8;  // of 8 rows, and 8 numbers of one
     auto place = [&](int r, int c) { return r * 64 + (((c >> 2) ^ r) & 15) * 4 + (c & 3); };
     auto take = [&](int r, float (&v)[8]) {
-        const f32x4 lo = *(const f32x4 *)(mine + place(r, eight));
-        const f32x4 hi = *(const f32x4 *)(mine + place(r, eight + 4));
+        f32x4 lo = *(const f32x4 *)(sums + place(r, eight));
+        f32x4 hi = *(const f32x4 *)(sums + place(r, eight + 4));
+#pragma unroll
+        for (int g = 1; g < KG; ++g) {
+            lo += *(const f32x4 *)(sums + g * kWaves * 2048 + place(r, eight));
+            hi += *(const f32x4 *)(sums + g * kWaves * 2048 + place(r, eight + 4));
+        }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             v[k] = lo[k];
@@ -672,10 +738,11 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     mine[place((r >> 2) * 8 + quad + (r & 3), q * 32 + col)] = acc[p][qq + q][r];
-            wave_sync();
+            part_sync();
             const int i1 = i0 + wr + p * 32, j1 = j0 + wc + qq * 32;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k0 = 0; k0 < 4 / KG; ++k0) {
+                const int k = KG > 1 ? group : k0;
                 const int r = k * 8 + line, i = i1 + r, j = j1 + eight;
                 float v[8];
                 take(r, v);
@@ -688,8 +755,8 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
                             out.put(mt.off + i * mt.ld + j, v, mt.n - j,
                                     muon_scale(scale_mode, mt.rows, mt.cols));
                     } else {  // back, to be read along the columns
-                        *(f32x4 *)(mine + place(r, eight)) = f32x4{v[0], v[1], v[2], v[3]};
-                        *(f32x4 *)(mine + place(r, eight + 4)) = f32x4{v[4], v[5], v[6], v[7]};
+                        *(f32x4 *)(sums + place(r, eight)) = f32x4{v[0], v[1], v[2], v[3]};
+                        *(f32x4 *)(sums + place(r, eight + 4)) = f32x4{v[4], v[5], v[6], v[7]};
                     }
                 } else {
                     if constexpr (STEP == kNext)
@@ -698,20 +765,21 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
                     store(i, j, v);
                 }
             }
-            wave_sync();
+            part_sync();
             if constexpr (STEP == kLast) {
                 if (mt.flip) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
+                    for (int k0 = 0; k0 < 4 / KG; ++k0) {
+                        const int k = KG > 1 ? group : k0;
                         const int c = k * 16 + (lane >> 2), r = (lane & 3) * 8;
                         float v[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = mine[place(r + e, c)];
+                        for (int e = 0; e < 8; ++e) v[e] = sums[place(r + e, c)];
                         if (i1 + r < mt.m && j1 + c < mt.n)
                             out.put(mt.off + (j1 + c) * mt.ld + i1 + r, v, mt.m - (i1 + r),
                                     muon_scale(scale_mode, mt.rows, mt.cols));
                     }
-                    wave_sync();
+                    part_sync();
                 }
             }
         }
@@ -719,7 +787,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
         const float sum = sum_over(squares);
         if (threadIdx.x == 0) w.part[mt.part_first + it.i * (mt.np / BT) + it.j] = sum;
     }
-    if constexpr (STEP == kGram || STEP == kPoly) {
+    if constexpr ((STEP == kGram || STEP == kPoly) && KG == 1) {
         if (it.i == it.j) return;  // a diagonal tile is its own transpose
 #pragma unroll
         for (int q = 0; q < WC; ++q)
@@ -803,13 +871,18 @@ WorkspaceLayout layout_of(const onebit_matrices_s *p, bool pairs)
 }
 
 // Side of the products' tiles for a list: 256, which reads half as much for each
-// product, where such tiles are enough to fill the GPU; 128 otherwise.
+// product, where such tiles are enough to fill the GPU; 64, with the summed index
+// split over four groups of waves, where larger ones would leave CUs without work.
 int tile_for(const int64_t *rows, const int64_t *cols, int32_t count)
 {
-    int64_t tiles = 0;
-    for (int32_t k = 0; k < count; ++k)
-        tiles += std::max<int64_t>(0, (rows[k] + 255) / 256) * std::max<int64_t>(0, (cols[k] + 255) / 256);
-    return tiles >= 1024 ? 256 : 128;
+    auto tiles = [&](int64_t side) {
+        int64_t n = 0;
+        for (int32_t k = 0; k < count; ++k)
+            n += std::max<int64_t>(0, (rows[k] + side - 1) / side) *
+                 std::max<int64_t>(0, (cols[k] + side - 1) / side);
+        return n;
+    };
+    return tiles(256) >= 1024 ? 256 : tiles(128) >= 256 ? 128 : 64;
 }
 
 // Workgroups go to the XCDs round-robin, and each XCD has an L2 of its own: a
@@ -912,7 +985,7 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
         for (int i = 0; i < rp; ++i)
             for (int j = 0; j < cp; ++j) first.push_back(Item{k, (uint16_t)i, (uint16_t)j});
         for (int i = 0; i < tm; ++i)
-            for (int j = 0; j <= i; ++j)
+            for (int j = 0; j < (tile == 64 ? tm : i + 1); ++j)
                 sym.push_back(Costed{{k, (uint16_t)i, (uint16_t)j}, m.np + m.mp});
         for (int i = 0; i < tm; ++i)
             for (int j = 0; j < tn; ++j)
@@ -1028,22 +1101,22 @@ int check_coefficients(Coefficients &k, int steps)
     return ONEBIT_OK;
 }
 
-template <bool PAIRS, int BT, int WR, int WC, class O>
+template <bool PAIRS, int BT, int WR, int WC, int KG, class O>
 void products(const onebit_matrices_s *p, Areas w, const O &out, int scale_mode, int steps,
               const Coefficients &co, hipStream_t st)
 {
-    constexpr int kThreads = BT * BT / (16 * WR * WC);
+    constexpr int kThreads = KG * BT * BT / (16 * WR * WC);
     float faded = 1.f;
     for (int k = 0; k < steps; ++k, faded *= co.fade) {
-        k_product<PAIRS, kGram, BT, WR, WC, kThreads, NoOut><<<p->sym_blocks, kThreads, 0, st>>>(
+        k_product<PAIRS, kGram, BT, WR, WC, KG, kThreads, NoOut><<<p->sym_blocks, kThreads, 0, st>>>(
             p->mats, p->sym_items, w, co, faded, NoOut{}, 0);
-        k_product<PAIRS, kPoly, BT, WR, WC, kThreads, NoOut><<<p->sym_blocks, kThreads, 0, st>>>(
+        k_product<PAIRS, kPoly, BT, WR, WC, KG, kThreads, NoOut><<<p->sym_blocks, kThreads, 0, st>>>(
             p->mats, p->sym_items, w, co, faded, NoOut{}, 0);
         if (k + 1 < steps)
-            k_product<PAIRS, kNext, BT, WR, WC, kThreads, NoOut><<<p->next_blocks, kThreads, 0, st>>>(
+            k_product<PAIRS, kNext, BT, WR, WC, KG, kThreads, NoOut><<<p->next_blocks, kThreads, 0, st>>>(
                 p->mats, p->next_items, w, co, faded, NoOut{}, 0);
         else
-            k_product<PAIRS, kLast, BT, WR, WC, kThreads, O><<<p->next_blocks, kThreads, 0, st>>>(
+            k_product<PAIRS, kLast, BT, WR, WC, KG, kThreads, O><<<p->next_blocks, kThreads, 0, st>>>(
                 p->mats, p->next_items, w, co, faded, out, scale_mode);
         std::swap(w.x, w.x_next);
     }
@@ -1063,9 +1136,11 @@ int run(const onebit_matrices_s *p, const S &src, const O &out, int scale_mode, 
     k_norm<S><<<(int)p->norms, 256, 0, st>>>(p->mats, p->norm_items, src, w.norm);
     k_first<PAIRS, S><<<(int)p->firsts, 256, 0, st>>>(p->mats, p->first_items, src, (double)eps, w);
     if (p->tile == 256)
-        products<PAIRS, 256, 4, 2>(p, w, out, scale_mode, steps, co, st);
+        products<PAIRS, 256, 4, 2, 1>(p, w, out, scale_mode, steps, co, st);
+    else if (p->tile == 128)
+        products<PAIRS, 128, 2, 2, 1>(p, w, out, scale_mode, steps, co, st);
     else
-        products<PAIRS, 128, 2, 2>(p, w, out, scale_mode, steps, co, st);
+        products<PAIRS, 64, 1, 2, 4>(p, w, out, scale_mode, steps, co, st);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? ONEBIT_OK : hip_fail(e, "matrix kernel launch");
 }
