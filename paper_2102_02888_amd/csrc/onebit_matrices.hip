@@ -56,7 +56,6 @@ constexpr float kScale = 8192.f;
 constexpr double kRange = 7.5;
 
 constexpr int kSlab = 64;    // fp16 numbers of an operand's row that are staged together
-constexpr int kNormChunk = 8192;  // elements of a matrix per workgroup of the norm
 constexpr int kPrep = 64;    // rows and columns of a workgroup of the first iterate
 
 struct Mat {
@@ -138,62 +137,127 @@ __device__ __forceinline__ T block_sum(T v, T *scratch)
 // Momentum, norm and the first iterate
 // ---------------------------------------------------------------------------
 
+// N consecutive elements as fp32.  Rows need no alignment: vector accesses are
+// stated as copies of bytes, which become loads and stores of up to 16 bytes.
+template <class T, int N>
+__device__ __forceinline__ void load_vec(const T *p, float (&v)[N])
+{
+    T t[N];
+    __builtin_memcpy(t, p, sizeof t);
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = (float)t[k];
+}
+
 // What is orthogonalised: a tensor, or momentum and gradients of a Muon step.
+// value() is N elements of it from element e of the flat buffers on; first() the
+// same for the norm's pass, which sees every element once and before value().
+// e_u: the element's place in the workspace.
 template <class T>
 struct FromTensor {
     const T *in;
-    __device__ __forceinline__ float value(int64_t e) const { return (float)in[e]; }
-    __device__ __forceinline__ float first(int64_t e) const { return value(e); }
+    template <int N>
+    __device__ __forceinline__ void value(int64_t e, int64_t, float (&v)[N]) const
+    {
+        load_vec(in + e, v);
+    }
+    template <int N>
+    __device__ __forceinline__ void first(int64_t e, int64_t e_u, float (&v)[N]) const
+    {
+        value(e, e_u, v);
+    }
 };
 
 template <class T>
 struct FromMuon {
     const T *grads;
     float *m;
+    float *u;  // where the norm's pass leaves the update, or NULL: it is formed again
     int64_t grad_ld;
     int n_grads;
     double n;
     float momentum;
     int nesterov;
-    __device__ __forceinline__ float mean(int64_t e) const
+    template <int N>
+    __device__ __forceinline__ void mean(int64_t e, float (&v)[N]) const
     {
-        if (n_grads == 1) return (float)grads[e];
-        double s = 0;
-        for (int i = 0; i < n_grads; ++i) s += (double)(float)grads[i * grad_ld + e];
-        return (float)(s / n);
+        load_vec(grads + e, v);
+        if (n_grads == 1) return;
+        double s[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) s[k] = (double)v[k];
+#pragma unroll 4
+        for (int i = 1; i < n_grads; ++i) {
+            load_vec(grads + i * grad_ld + e, v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) s[k] += (double)v[k];
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = (float)(s[k] / n);
     }
     // the update from the new momentum
-    __device__ __forceinline__ float value(int64_t e) const
+    template <int N>
+    __device__ __forceinline__ void value(int64_t e, int64_t e_u, float (&v)[N]) const
     {
-        return nesterov ? mean(e) + momentum * m[e] : m[e];
+        if (u) return load_vec(u + e_u, v);
+        float now[N];
+        load_vec(m + e, now);
+        if (nesterov) mean(e, v);
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = nesterov ? v[k] + momentum * now[k] : now[k];
     }
-    // ... which is formed and stored here, once for every element
-    __device__ __forceinline__ float first(int64_t e) const
+    // ... which is formed and stored here
+    template <int N>
+    __device__ __forceinline__ void first(int64_t e, int64_t e_u, float (&v)[N]) const
     {
-        const float g = mean(e), now = momentum * m[e] + g;
-        m[e] = now;
-        return nesterov ? g + momentum * now : now;
+        float now[N];
+        load_vec(m + e, now);
+        mean(e, v);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            now[k] = momentum * now[k] + v[k];
+            v[k] = nesterov ? v[k] + momentum * now[k] : now[k];
+        }
+        __builtin_memcpy(m + e, now, sizeof now);
+        if (u) __builtin_memcpy(u + e_u, v, sizeof v);
     }
 };
 
-// Sum of squares (64 bits) of kNormChunk elements of a matrix.
+// Sum of squares (64 bits) of `size` elements of a matrix: 8 per thread at a time
+// where the matrix is one run of memory, else one.
 template <class S>
 __global__ __launch_bounds__(256) void k_norm(const Mat *__restrict__ mats,
-                                              const Item *__restrict__ items, S src,
+                                              const Item *__restrict__ items, int size, S src,
                                               double *__restrict__ norm)
 {
     __shared__ double scratch[4];
     const Item it = items[blockIdx.x];
     const Mat &mt = mats[it.mat];
     const uint32_t cols = mt.cols, total = (uint32_t)mt.rows * cols;
-    const int64_t off = mt.off, ld = mt.ld;
+    const int64_t off = mt.off, ld = mt.ld, at_u = mt.ex;
     const uint32_t chunk = (uint32_t)it.i << 16 | it.j;
-    const uint32_t begin = chunk * kNormChunk, end = min(begin + kNormChunk, total);
+    const uint32_t begin = chunk * size, end = min(begin + size, total);
     double sum = 0;
-    for (uint32_t e = begin + threadIdx.x; e < end; e += 256) {
-        const uint32_t r = e / cols;
-        const float v = src.first(off + r * ld + (e - r * cols));
-        sum += (double)v * (double)v;
+    if (ld == cols) {
+        uint32_t e = begin + threadIdx.x * 8;
+#pragma unroll 2
+        for (; e + 8 <= end; e += 2048) {
+            float v[8];
+            src.first(off + e, at_u + e, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += (double)v[k] * (double)v[k];
+        }
+        for (; e < end; ++e) {  // the last thread's few, where 8 are no longer left
+            float v[1];
+            src.first(off + e, at_u + e, v);
+            sum += (double)v[0] * (double)v[0];
+        }
+    } else {
+        for (uint32_t e = begin + threadIdx.x; e < end; e += 256) {
+            const uint32_t r = e / cols;
+            float v[1];
+            src.first(off + r * ld + (e - r * cols), at_u + e, v);
+            sum += (double)v[0] * (double)v[0];
+        }
     }
     sum = block_sum(sum, scratch);
     if (threadIdx.x == 0) norm[mt.norm_first + chunk] = sum;
@@ -206,24 +270,38 @@ __device__ __forceinline__ int column(int k)
     return PAIRS ? (k >> 5) * 64 + (k & 31) : k;
 }
 
-__device__ __forceinline__ uint32_t pack(float v)
-{
-    _Float16 hi, lo;
-    split(v, hi, lo);
-    return (uint32_t)__builtin_bit_cast(uint16_t, hi) |
-           (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16;
-}
-
-// First iterate, X = u / (||u||_F + eps), padding zeroed.
+// First iterate, X = u / (||u||_F + eps), padding zeroed: 64 x 64 of the matrix
+// for a workgroup, 8 of a row for a thread, turned in LDS where X is the transpose.
 template <bool PAIRS, class S>
 __global__ __launch_bounds__(256) void k_first(const Mat *__restrict__ mats,
                                                const Item *__restrict__ items, S src, double eps,
                                                Areas w)
 {
     __shared__ double scratch[4];
-    __shared__ uint32_t tile[kPrep][kPrep + 1];
+    __shared__ float tile[kPrep][kPrep + 1];
     const Item it = items[blockIdx.x];
     const Mat &mt = mats[it.mat];
+    const int r0 = it.i * kPrep, c0 = it.j * kPrep;
+    const int line = threadIdx.x >> 3, eight = (threadIdx.x & 7) * 8;
+    float v[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int r = r0 + h * 32 + line, c = c0 + eight;
+        const int64_t e = mt.off + r * mt.ld + c, e_u = mt.ex + (int64_t)r * mt.cols + c;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[h][k] = 0.f;
+        if (r < mt.rows && c + 8 <= mt.cols) {
+            src.value(e, e_u, v[h]);
+        } else if (r < mt.rows) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c + k < mt.cols) {
+                    float one[1];
+                    src.value(e + k, e_u + k, one);
+                    v[h][k] = one[0];
+                }
+        }
+    }
     double sum = 0;
     for (int k = threadIdx.x; k < mt.norm_count; k += 256) sum += w.norm[mt.norm_first + k];
     sum = block_sum(sum, scratch);
@@ -232,36 +310,35 @@ __global__ __launch_bounds__(256) void k_first(const Mat *__restrict__ mats,
     const double gamma = size > 0 && size <= 0.5 ? exp2(fmin(-ceil(log2(size)), 120.0)) : 1.0;
     if (it.i == 0 && it.j == 0 && threadIdx.x == 0) w.gamma[it.mat] = (float)gamma;
     const double factor = (double)kScale * gamma / (sqrt(sum) + eps);
-    const int r0 = it.i * kPrep, c0 = it.j * kPrep;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll 4
-    for (int k = 0; k < kPrep / 4; ++k) {
-        const int r = r0 + wave * (kPrep / 4) + k, c = c0 + lane;
-        float v = 0.f;
-        if (r < mt.rows && c < mt.cols)
-            v = (float)((double)src.value(mt.off + r * mt.ld + c) * factor);
-        tile[r - r0][lane] = pack(v);
-    }
-    __syncthreads();
-    // rows of X: the matrix's rows, or its columns where X is the transpose
-    const int line = threadIdx.x >> 2, part = (threadIdx.x & 3) * 16;
-    uint32_t u[16];
+    if (mt.flip) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) u[k] = mt.flip ? tile[part + k][line] : tile[line][part + k];
-    const int row = (mt.flip ? c0 : r0) + line, col = (mt.flip ? r0 : c0) + part;
-    constexpr int kind = PAIRS ? 2 : 1;
-    _Float16 *hi_at = w.x + mt.ex * kind + (int64_t)row * mt.np * kind + column<PAIRS>(col);
-    _Float16 *lo_at = PAIRS ? hi_at + 32 : w.x_lo + mt.ex + (int64_t)row * mt.np + col;
-    uint32_t hi[8], lo[8];
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        hi[q] = (u[2 * q] & 0xffffu) | u[2 * q + 1] << 16;
-        lo[q] = u[2 * q] >> 16 | (u[2 * q + 1] & 0xffff0000u);
+            for (int k = 0; k < 8; ++k) tile[h * 32 + line][eight + k] = v[h][k];
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[h][k] = tile[eight + k][h * 32 + line];
     }
 #pragma unroll
-    for (int q = 0; q < 8; q += 4) {
-        *(v4u *)(hi_at + 2 * q) = v4u{hi[q], hi[q + 1], hi[q + 2], hi[q + 3]};
-        *(v4u *)(lo_at + 2 * q) = v4u{lo[q], lo[q + 1], lo[q + 2], lo[q + 3]};
+    for (int h = 0; h < 2; ++h) {
+        const int row = (mt.flip ? c0 : r0) + h * 32 + line, col = (mt.flip ? r0 : c0) + eight;
+        half8 hi, lo;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            // padding stays zero beside a NaN or an infinite norm too
+            const bool real = row < mt.m && col + k < mt.n;
+            _Float16 a, b;
+            split(real ? (float)((double)v[h][k] * factor) : 0.f, a, b);
+            hi[k] = a;
+            lo[k] = b;
+        }
+        constexpr int kind = PAIRS ? 2 : 1;
+        _Float16 *to = w.x + mt.ex * kind + (int64_t)row * mt.np * kind + column<PAIRS>(col);
+        *(half8 *)to = hi;
+        if constexpr (PAIRS) *(half8 *)(to + 32) = lo;
+        else *(half8 *)(w.x_lo + mt.ex + (int64_t)row * mt.np + col) = lo;
     }
 }
 
@@ -823,7 +900,7 @@ struct onebit_matrices_s {
     int device = 0;
     int32_t count = 0;
     int64_t extent = 0, ex = 0, em = 0;
-    int tile = 128;
+    int tile = 128, norm_size = 0;  // side of a tile; elements per workgroup of the norm
     int64_t norms = 0, firsts = 0, parts = 0;
     int64_t sym_blocks = 0, next_blocks = 0;  // workgroups of the products' launches
     std::vector<int64_t> offset;
@@ -935,6 +1012,10 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
     p->offset.resize(count);
     int64_t at = 0;
     const int tile = p->tile = tile_for(rows, cols, count);
+    // 2,048 elements are one load per thread; four where that still makes many workgroups
+    double elements = 0;
+    for (int32_t k = 0; k < count; ++k) elements += (double)rows[k] * (double)cols[k];
+    const int size = p->norm_size = elements <= (1 << 23) ? 2048 : 8192;
     constexpr int64_t kSide = 1 << 20, kMost = (int64_t)1 << 40, kItems = 1 << 23;
     for (int32_t k = 0; k < count; ++k) {
         const int64_t r = rows[k], c = cols[k];
@@ -974,7 +1055,7 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
         p->em += (int64_t)m.mp * m.mp;
         const int tm = m.mp / tile, tn = m.np / tile;
         m.norm_first = (int32_t)norm.size();
-        m.norm_count = (int32_t)((r * c + kNormChunk - 1) / kNormChunk);
+        m.norm_count = (int32_t)((r * c + size - 1) / size);
         m.part_first = (int32_t)next.size();
         m.part_count = tm * tn;
         const int rp = (m.flip ? m.np : m.mp) / kPrep, cp = (m.flip ? m.mp : m.np) / kPrep;
@@ -1133,7 +1214,7 @@ int run(const onebit_matrices_s *p, const S &src, const O &out, int scale_mode, 
             (_Float16 *)(ws + l.d), (_Float16 *)(ws + l.b),
             (double *)(ws + l.norm), (float *)(ws + l.part), (float *)(ws + l.t),
             (float *)(ws + l.gamma)};
-    k_norm<S><<<(int)p->norms, 256, 0, st>>>(p->mats, p->norm_items, src, w.norm);
+    k_norm<S><<<(int)p->norms, 256, 0, st>>>(p->mats, p->norm_items, p->norm_size, src, w.norm);
     k_first<PAIRS, S><<<(int)p->firsts, 256, 0, st>>>(p->mats, p->first_items, src, (double)eps, w);
     if (p->tile == 256)
         products<PAIRS, 256, 4, 2, 1>(p, w, out, scale_mode, steps, co, st);
@@ -1255,7 +1336,12 @@ int onebit_muon_step(onebit_matrices mats, float *x, float *m, const void *grads
     if (mats->ex == 0) return ONEBIT_OK;
     return with_type(grad_dtype, [&](auto *g) {
         using G = std::remove_pointer_t<decltype(g)>;
-        const FromMuon<G> src{(const G *)grads, m, grad_ld, n_grads, (double)n_grads, momentum,
+        // From three gradient rows on, reading them again costs more than the update's
+        // own way through memory; the second iterate's place, 4 bytes an element for
+        // pairs, is free until the first step's last product.
+        float *u = products == ONEBIT_PRODUCTS_F32 && nesterov && n_grads >= 3
+                       ? (float *)((char *)workspace + layout_of(mats, true).x1) : nullptr;
+        const FromMuon<G> src{(const G *)grads, m, u, grad_ld, n_grads, (double)n_grads, momentum,
                               nesterov};
         const ToMuon dst{x, 1.f - lr * weight_decay, lr};
         return products == ONEBIT_PRODUCTS_F32
