@@ -294,7 +294,7 @@ __global__ __launch_bounds__(256) void k_sort_move(const void *__restrict__ src,
     __shared__ uint32_t s_sums[4];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     uint32_t before = 0, total = 0;
-#pragma unroll 8
+#pragma unroll 32
     for (int b = 0; b < blocks; ++b) {
         const uint32_t n = counts[b * kDigits + tid];
         total += n;
@@ -374,7 +374,28 @@ __device__ __forceinline__ float *partial_at(const Sums &s, int64_t piece, int s
 }
 
 constexpr int kAhead = 8;  // rows whose loads are in flight together
+constexpr int kJoin = 8;   // threads that share a crossing row's partial sums
 
+// kCols elements as they lie in memory, `left` of which exist.
+template <class T>
+struct Raw {
+    T v[kCols];
+};
+
+template <class T>
+__device__ __forceinline__ void load_raw(const T *p, Raw<T> &r, int left)
+{
+    if (left >= kCols) {
+        __builtin_memcpy(&r, p, sizeof r);
+    } else {
+#pragma unroll
+        for (int k = 0; k < kCols; ++k) r.v[k] = k < left ? p[k] : (T)0.f;
+    }
+}
+
+// A thread's work is a chain: the list's entries, the rows they name, their sums.
+// Each part runs a batch ahead of the next: while a batch is added, the next one's
+// rows and the entries of the one after are under way.
 template <class D, class G>
 __global__ __launch_bounds__(256) void k_grad_sum(Sums s, const D *__restrict__ dout,
                                                   G *__restrict__ grad)
@@ -384,76 +405,112 @@ __global__ __launch_bounds__(256) void k_grad_sum(Sums s, const D *__restrict__ 
     if (piece >= s.pieces) return;
     c *= kCols;
     const int64_t begin = piece * s.piece, end = min(begin + s.piece, s.tokens);
-    uint32_t row = s.keys[begin];
-    if (row >= s.vocab) return;  // places that add nothing, as all that follow
-    bool before = begin > 0 && s.keys[begin - 1] == row;
+    const uint32_t none = (uint32_t)s.vocab;
+    const int left = s.width - c;
+    struct Batch {
+        uint32_t key[kAhead], at[kAhead];
+    };
+    // (the list's areas reach to a whole piece; entries past its end are not used)
+    auto entries = [&](int64_t at, Batch &b) {
+        __builtin_memcpy(b.key, __builtin_assume_aligned(s.keys + at, 16), sizeof b.key);
+        __builtin_memcpy(b.at, __builtin_assume_aligned(s.order + at, 16), sizeof b.at);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (at + u >= end || b.key[u] >= none) b.key[u] = none;
+    };
+    auto rows = [&](const Batch &b, Raw<D> (&r)[kAhead]) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (b.key[u] != none) load_raw(dout + (int64_t)b.at[u] * s.dout_ld + c, r[u], left);
+    };
+    Batch now, next;
+    Raw<D> r[kAhead];
+    entries(begin, now);
+    const uint32_t previous = begin > 0 ? s.keys[begin - 1] : none;
+    const uint32_t following = end < s.tokens ? s.keys[end] : none;
+    if (begin + kAhead < end) entries(begin + kAhead, next);
+    rows(now, r);
+    uint32_t row = now.key[0];
+    if (row == none) return;  // places that add nothing, as all that follow
+    bool before = previous == row;
     float acc[kCols] = {};
     for (int64_t at = begin; at < end; at += kAhead) {
-        uint32_t k[kAhead];
-        float v[kAhead][kCols];
+        Raw<D> r2[kAhead];
+        Batch after;
+        if (at + kAhead < end) rows(next, r2);
+        if (at + 2 * kAhead < end) entries(at + 2 * kAhead, after);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const bool on = at + u < end;
-            k[u] = on ? s.keys[at + u] : (uint32_t)s.vocab;
-            const int64_t t = on && k[u] < s.vocab ? s.order[at + u] : s.order[begin];
-            load_some(dout + t * s.dout_ld + c, v[u], s.width - c);
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (k[u] >= s.vocab) break;
-            if (k[u] != row) {  // the row ends here
+            if (now.key[u] == none) break;
+            if (now.key[u] != row) {  // the row ends here
                 if (before)
                     store_vec(partial_at(s, piece, 0, c), acc);
                 else
                     finish_row(s, grad, row, c, acc);
-                row = k[u];
+                row = now.key[u];
                 before = false;
 #pragma unroll
                 for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
             }
 #pragma unroll
-            for (int i = 0; i < kCols; ++i) acc[i] += v[u][i];
+            for (int i = 0; i < kCols; ++i) acc[i] += (float)r[u].v[i];
         }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) r[u] = r2[u];
+        now = next;
+        next = after;
     }
-    const bool after = end < s.tokens && s.keys[end] == row;
     if (before)
         store_vec(partial_at(s, piece, 0, c), acc);
-    else if (after)
+    else if (following == row)
         store_vec(partial_at(s, piece, 1, c), acc);
     else
         finish_row(s, grad, row, c, acc);
 }
 
-// Rows that cross pieces, by the piece they begin in.
+// Rows that cross pieces, by the piece they begin in: of the pieces that follow,
+// each of kJoin threads adds every kJoin-th, and their sums are added in order.
 template <class G>
 __global__ __launch_bounds__(256) void k_grad_join(Sums s, G *__restrict__ grad)
 {
-    int c;
-    const int64_t piece = row_of((int64_t)blockIdx.x * 256, s.per_row, c);
-    c *= kCols;
+    __shared__ float part[kJoin][256 / kJoin][kCols + 1];
+    const int groups = (s.per_row + 256 / kJoin - 1) / (256 / kJoin);  // of columns
+    const int64_t piece = blockIdx.x / groups;
     const int64_t begin = piece * s.piece, end = begin + s.piece;
-    if (piece >= s.pieces || end >= s.tokens) return;
+    if (end >= s.tokens) return;
     const uint32_t row = s.keys[end];
     if (row >= s.vocab || s.keys[end - 1] != row) return;
-    if (begin > 0 && s.keys[begin - 1] == row) return;  // it began earlier
-    float acc[kCols];
-    load_vec(partial_at(s, piece, 1, c), acc);
-    for (int64_t q = piece + 1;; q += kAhead) {
-        float v[kAhead][kCols];
-        bool on[kAhead];
+    if (begin > 0 && s.keys[begin] == row && s.keys[begin - 1] == row) return;  // it began earlier
+    const int lane = threadIdx.x % (256 / kJoin), turn = threadIdx.x / (256 / kJoin);
+    const int c = ((int)(blockIdx.x % groups) * (256 / kJoin) + lane) * kCols;
+    const bool mine = c < s.per_row * kCols;
+    float acc[kCols] = {};
+    if (turn == 0 && mine) load_vec(partial_at(s, piece, 1, c), acc);
+    constexpr int kBatch = 4;
+    for (int64_t q = piece + 1 + turn; q < s.pieces; q += kBatch * kJoin) {
+        float v[kBatch][kCols];
+        bool on[kBatch];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int64_t p = q + u < s.pieces ? q + u : q;
-            on[u] = q + u < s.pieces && s.keys[p * s.piece] == row;
-            load_vec(partial_at(s, p, 0, c), v[u]);
+        for (int u = 0; u < kBatch; ++u) {
+            const int64_t p = min(q + u * kJoin, s.pieces - 1);
+            on[u] = q + u * kJoin < s.pieces && s.keys[p * s.piece] == row;
+            if (mine) load_vec(partial_at(s, p, 0, c), v[u]);
         }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
+        for (int u = 0; u < kBatch; ++u)
             if (on[u])
 #pragma unroll
                 for (int i = 0; i < kCols; ++i) acc[i] += v[u][i];
-        if (!on[kAhead - 1] || q + kAhead >= s.pieces) break;
+        if (!on[kBatch - 1]) break;
     }
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) part[turn][lane][i] = acc[i];
+    __syncthreads();
+    if (turn > 0 || !mine) return;
+#pragma unroll
+    for (int t = 1; t < kJoin; ++t)
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) acc[i] += part[t][lane][i];
     finish_row(s, grad, row, c, acc);
 }
 
@@ -493,8 +550,8 @@ GradLayout grad_layout(int64_t tokens, int64_t width)
         return here;
     };
     for (int k = 0; k < 2; ++k) {
-        l.keys[k] = take((size_t)tokens * 4);
-        l.order[k] = take((size_t)tokens * 4);
+        l.keys[k] = take((size_t)l.pieces * l.piece * 4);
+        l.order[k] = take((size_t)l.pieces * l.piece * 4);
     }
     l.counts = take((size_t)kSortBlocks * kDigits * 4);
     l.partial = take((size_t)l.pieces * 2 * l.per_row * kCols * 4);
@@ -621,7 +678,8 @@ int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld,
     hipStream_t st = (hipStream_t)stream;
     const GradLayout l = grad_layout(tokens, width);
     const int64_t blocks = (l.pieces * l.per_row + 255) / 256;
-    if (blocks > (1 << 23))
+    const int64_t joins = (l.per_row + 256 / kJoin - 1) / (256 / kJoin);  // workgroups of a piece
+    if (blocks > (1 << 23) || l.pieces * joins > (1 << 23))
         return fail(ONEBIT_EINVAL, "%lld places of %lld columns are too many for one call",
                     (long long)tokens, (long long)width);
     char *ws = (char *)workspace;
@@ -682,7 +740,7 @@ int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld,
             using D = std::remove_pointer_t<decltype(d)>;
             k_grad_sum<D, G><<<blocks, 256, 0, st>>>(s, (const D *)dout, (G *)grad);
         });
-        if (l.pieces > 1) k_grad_join<G><<<blocks, 256, 0, st>>>(s, (G *)grad);
+        if (l.pieces > 1) k_grad_join<G><<<l.pieces * joins, 256, 0, st>>>(s, (G *)grad);
     });
     return launched("embedding gradient launch");
 }

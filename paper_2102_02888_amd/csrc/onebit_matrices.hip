@@ -621,6 +621,75 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
             all(f.a_lo, f.b);
         }
     };
+    // The first two slabs are under way before anything else is waited for.
+    char *const ours[2] = {buffer0 + group * 2 * kOperand, buffer1 + group * 2 * kOperand};
+    const int own = (slabs - group + KG - 1) / KG;  // slabs of this group
+    if (own > 0) stage(group, ours[0]);
+    if (own > 1) stage(KG + group, ours[1]);
+
+    // The shift, and the step's coefficients around it.
+    auto sum_over = [&](float v) {  // the workgroup's, the same in every thread
+        for (int k = 32; k > 0; k /= 2) v += __shfl_xor(v, k);
+        __syncthreads();
+        if (lane == 0) scratch[wave_number()] = v;
+        __syncthreads();
+        float total = 0.f;
+#pragma unroll
+        for (int k = 0; k < KG * kWaves; ++k) total += scratch[k];
+        return total;
+    };
+    const float gamma0 = w.gamma[it.mat], gamma = fmaxf(gamma0 * faded, 1.f);
+    const float inv2 = 1.f / (gamma * gamma);
+    float t;
+    if (STEP == kGram) {
+        if (faded == 1.f) {  // the first step
+            t = 1.f / (float)mt.m;
+        } else {
+            float sum = 0.f;
+            for (int k = threadIdx.x; k < mt.part_count; k += THREADS) sum += w.part[mt.part_first + k];
+            t = sum_over(sum) / (float)mt.m;
+            t = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, t)));
+        }
+        if (it.i == 0 && it.j == 0 && threadIdx.x == 0) w.t[it.mat] = t;
+    } else {
+        t = w.t[it.mat];
+    }
+    const float tx = t * inv2;  // of X, where t is of gamma X
+    // to the next step's gamma; the last product's value is X itself
+    const float change = STEP == kLast ? 1.f / gamma
+                         : STEP == kNext ? fmaxf(gamma0 * (faded * co.fade), 1.f) / gamma : 1.f;
+    const float linear = STEP == kPoly ? co.b + 2.f * co.c * tx
+                                       : (co.a + (co.b + co.c * tx) * tx) * change;
+    const float square = STEP == kPoly ? co.c * inv2 : inv2 * change;
+    constexpr float unscale = 1.f / kScale;
+    const float shift = STEP == kGram ? t * kScale : 0.f;
+    const float factor = STEP == kGram ? unscale : square * unscale;
+
+    // The old values of the linear term, 8 of a row per lane, are read a block of 32 x 64
+    // ahead of their use, but where the registers are full (pairs, tiles of 256).
+    constexpr bool kAhead = !(PAIRS && BT == 256);
+    const int line = lane >> 3, eight = (lane & 7) * 8;  // of 8 rows, and 8 numbers of one
+    constexpr int kRounds = 4 / KG, kBlocks = WR * WC / 2;
+    struct Old {
+        half8 hi[kRounds], lo[kRounds];
+    } old[2];
+    auto row_in_block = [&](int k) { return (KG > 1 ? group : k) * 8 + line; };
+    auto read_old = [&](int i1, int j1, Old &o) {
+        if constexpr (STEP != kGram) {
+#pragma unroll
+            for (int k = 0; k < kRounds; ++k) {
+                const int i = i1 + row_in_block(k), j = j1 + eight;
+                const _Float16 *from = (STEP == kPoly ? d + i * d_pitch : x + i * x_pitch) + column<PAIRS>(j);
+                o.hi[k] = *(const half8 *)from;
+                if constexpr (PAIRS) o.lo[k] = *(const half8 *)(from + 32);
+                else if constexpr (STEP != kPoly) o.lo[k] = *(const half8 *)(w.x_lo + ex + i * x_pitch + j);
+            }
+        }
+    };
+    auto block_row = [&](int n) { return i0 + wr + n / (WC / 2) * 32; };
+    auto block_col = [&](int n) { return j0 + wc + n % (WC / 2) * 64; };
+    if constexpr (KG > 1) read_old(block_row(0), block_col(0), old[0]);
+
     if constexpr (KG == 1) {
         // Each step's products run while the next step's fragments are read: two reads,
         // then one or two products, so that the reads are done well before the step is.
@@ -648,8 +717,6 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
         // takes the slab after the next, and the next one, a slab's time under way, is
         // waited for.  The loop begins there, so that nothing is under way where it
         // closes: the compiler would wait for all of it.
-        stage(0, buffer0);
-        stage(1, buffer1);
         staged_sync();
         load(buffer0, 0, f[0]);
         inner(buffer0, 0);
@@ -671,8 +738,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
         multiply(f[1]);
         staged_sync();
     } else {
-        char *const mine[2] = {buffer0 + group * 2 * kOperand, buffer1 + group * 2 * kOperand};
-        const int rounds = (slabs + KG - 1) / KG, own = (slabs - group + KG - 1) / KG;
+        const int rounds = (slabs + KG - 1) / KG;
         auto whole = [&](const char *from) {
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) {
@@ -695,51 +761,12 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
             if (s + 2 < own) stage((s + 2) * KG + group, from);
         };
         static_assert(kLoads < 16, "the counter's low bits");
-        if (own > 0) stage(group, mine[0]);
-        if (own > 1) stage(KG + group, mine[1]);
         for (int s = 0; s < rounds; s += 2) {
-            round(s, mine[0]);
-            if (s + 1 < rounds) round(s + 1, mine[1]);
+            round(s, ours[0]);
+            if (s + 1 < rounds) round(s + 1, ours[1]);
         }
         __syncthreads();
     }
-
-    // The shift, and the step's coefficients around it.
-    auto sum_over = [&](float v) {  // the workgroup's, the same in every thread
-        for (int k = 32; k > 0; k /= 2) v += __shfl_xor(v, k);
-        __syncthreads();
-        if (lane == 0) scratch[wave_number()] = v;
-        __syncthreads();
-        float total = 0.f;
-#pragma unroll
-        for (int k = 0; k < KG * kWaves; ++k) total += scratch[k];
-        return total;
-    };
-    const float gamma0 = w.gamma[it.mat], gamma = fmaxf(gamma0 * faded, 1.f);
-    const float inv2 = 1.f / (gamma * gamma);
-    float t;
-    if (STEP == kGram) {
-        if (faded == 1.f) {  // the first step
-            t = 1.f / (float)mt.m;
-        } else {
-            float sum = 0.f;
-            for (int k = threadIdx.x; k < mt.part_count; k += THREADS) sum += w.part[mt.part_first + k];
-            t = sum_over(sum) / (float)mt.m;
-        }
-        if (it.i == 0 && it.j == 0 && threadIdx.x == 0) w.t[it.mat] = t;
-    } else {
-        t = w.t[it.mat];
-    }
-    const float tx = t * inv2;  // of X, where t is of gamma X
-    // to the next step's gamma; the last product's value is X itself
-    const float change = STEP == kLast ? 1.f / gamma
-                         : STEP == kNext ? fmaxf(gamma0 * (faded * co.fade), 1.f) / gamma : 1.f;
-    const float linear = STEP == kPoly ? co.b + 2.f * co.c * tx
-                                       : (co.a + (co.b + co.c * tx) * tx) * change;
-    const float square = STEP == kPoly ? co.c * inv2 : inv2 * change;
-    constexpr float unscale = 1.f / kScale;
-    const float shift = STEP == kGram ? t * kScale : 0.f;
-    const float factor = STEP == kGram ? unscale : square * unscale;
 
     // The tile's values go through LDS, 32 x 64 of them at a time in a part of each
     // wave's own, to be read back 8 in a row: what is read and written in memory
@@ -756,7 +783,6 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
         else wave_sync();
     };
     const int col = lane & 31, quad = (lane >> 5) * 4;
-    const int line = lane >> 3, eight = (lane & 7) * 8;  // of 8 rows, and 8 numbers of one
     auto place = [&](int r, int c) { return r * 64 + (((c >> 2) ^ r) & 15) * 4 + (c & 3); };
     auto take = [&](int r, float (&v)[8]) {
         f32x4 lo = *(const f32x4 *)(sums + place(r, eight));
@@ -774,7 +800,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     };
     float squares = 0.f;
     // the values of 8 numbers of the output's row i from column j on, from their sums
-    auto value = [&](int i, int j, float (&v)[8]) {
+    auto value = [&](int i, int j, const Old &o, int k8, float (&v)[8]) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= factor;
         if constexpr (STEP == kGram) {
@@ -782,13 +808,10 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
             for (int k = 0; k < 8; ++k)
                 if (i == j + k && i < mt.m) v[k] -= shift;
         } else {
-            const _Float16 *from = STEP == kPoly ? d + i * d_pitch : x + i * x_pitch;
-            const half8 hi = *(const half8 *)(from + column<PAIRS>(j));
-            half8 lo = {};
-            if constexpr (PAIRS) lo = *(const half8 *)(from + column<PAIRS>(j) + 32);
-            else if constexpr (STEP != kPoly) lo = *(const half8 *)(w.x_lo + ex + i * x_pitch + j);
+            constexpr bool kLo = PAIRS || STEP != kPoly;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] += linear * ((float)hi[k] + (float)lo[k]);
+            for (int k = 0; k < 8; ++k)
+                v[k] += linear * (kLo ? (float)o.hi[k8][k] + (float)o.lo[k8][k] : (float)o.hi[k8][k]);
         }
     };
     auto store = [&](int i, int j, const float (&v)[8]) {
@@ -806,88 +829,93 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
         if constexpr (PAIRS) *(half8 *)(to + column<PAIRS>(j) + 32) = lo;
         else if constexpr (STEP == kNext) *(half8 *)(w.x_lo + ex + i * x_pitch + j) = lo;
     };
+    if constexpr (KG == 1) read_old(block_row(0), block_col(0), old[0]);
 #pragma unroll
-    for (int p = 0; p < WR; ++p)
+    for (int n = 0; n < kBlocks; ++n) {  // 32 rows x 64 columns
+        const int p = n / (WC / 2), qq = n % (WC / 2) * 2;
+        if (kAhead && n + 1 < kBlocks) read_old(block_row(n + 1), block_col(n + 1), old[(n + 1) & 1]);
+        if (!kAhead && n > 0) read_old(block_row(n), block_col(n), old[n & 1]);
 #pragma unroll
-        for (int qq = 0; qq < WC; qq += 2) {  // 32 rows x 64 columns
+        for (int q = 0; q < 2; ++q)
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+            for (int r = 0; r < 16; ++r)
+                mine[place((r >> 2) * 8 + quad + (r & 3), q * 32 + col)] = acc[p][qq + q][r];
+        part_sync();
+        const int i1 = block_row(n), j1 = block_col(n);
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    mine[place((r >> 2) * 8 + quad + (r & 3), q * 32 + col)] = acc[p][qq + q][r];
-            part_sync();
-            const int i1 = i0 + wr + p * 32, j1 = j0 + wc + qq * 32;
-#pragma unroll
-            for (int k0 = 0; k0 < 4 / KG; ++k0) {
-                const int k = KG > 1 ? group : k0;
-                const int r = k * 8 + line, i = i1 + r, j = j1 + eight;
-                float v[8];
-                take(r, v);
-                value(i, j, v);
-                if constexpr (STEP == kLast) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] *= unscale;
-                    if (!mt.flip) {
-                        if (i < mt.m && j < mt.n)
-                            out.put(mt.off + i * mt.ld + j, v, mt.n - j,
-                                    muon_scale(scale_mode, mt.rows, mt.cols));
-                    } else {  // back, to be read along the columns
-                        *(f32x4 *)(sums + place(r, eight)) = f32x4{v[0], v[1], v[2], v[3]};
-                        *(f32x4 *)(sums + place(r, eight + 4)) = f32x4{v[4], v[5], v[6], v[7]};
-                    }
-                } else {
-                    if constexpr (STEP == kNext)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) squares += (v[e] * unscale) * (v[e] * unscale);
-                    store(i, j, v);
-                }
-            }
-            part_sync();
+        for (int k = 0; k < kRounds; ++k) {
+            const int r = row_in_block(k), i = i1 + r, j = j1 + eight;
+            float v[8];
+            take(r, v);
+            value(i, j, old[n & 1], k, v);
             if constexpr (STEP == kLast) {
-                if (mt.flip) {
 #pragma unroll
-                    for (int k0 = 0; k0 < 4 / KG; ++k0) {
-                        const int k = KG > 1 ? group : k0;
-                        const int c = k * 16 + (lane >> 2), r = (lane & 3) * 8;
-                        float v[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = sums[place(r + e, c)];
-                        if (i1 + r < mt.m && j1 + c < mt.n)
-                            out.put(mt.off + (j1 + c) * mt.ld + i1 + r, v, mt.m - (i1 + r),
-                                    muon_scale(scale_mode, mt.rows, mt.cols));
-                    }
-                    part_sync();
+                for (int e = 0; e < 8; ++e) v[e] *= unscale;
+                if (!mt.flip) {
+                    if (i < mt.m && j < mt.n)
+                        out.put(mt.off + i * mt.ld + j, v, mt.n - j,
+                                muon_scale(scale_mode, mt.rows, mt.cols));
+                } else {  // back, to be read along the columns
+                    *(f32x4 *)(sums + place(r, eight)) = f32x4{v[0], v[1], v[2], v[3]};
+                    *(f32x4 *)(sums + place(r, eight + 4)) = f32x4{v[4], v[5], v[6], v[7]};
                 }
+            } else {
+                if constexpr (STEP == kNext)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) squares += (v[e] * unscale) * (v[e] * unscale);
+                store(i, j, v);
             }
         }
+        part_sync();
+        if constexpr (STEP == kLast) {
+            if (mt.flip) {
+#pragma unroll
+                for (int k = 0; k < kRounds; ++k) {
+                    const int c = (KG > 1 ? group : k) * 16 + (lane >> 2), r = (lane & 3) * 8;
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = sums[place(r + e, c)];
+                    if (i1 + r < mt.m && j1 + c < mt.n)
+                        out.put(mt.off + (j1 + c) * mt.ld + i1 + r, v, mt.m - (i1 + r),
+                                muon_scale(scale_mode, mt.rows, mt.cols));
+                }
+                part_sync();
+            }
+        }
+    }
     if constexpr (STEP == kNext) {
         const float sum = sum_over(squares);
         if (threadIdx.x == 0) w.part[mt.part_first + it.i * (mt.np / BT) + it.j] = sum;
     }
     if constexpr ((STEP == kGram || STEP == kPoly) && KG == 1) {
         if (it.i == it.j) return;  // a diagonal tile is its own transpose
+        constexpr int kTurned = WC * WR / 2;  // of 32 columns x 64 rows
+        auto turned_row = [&](int n) { return j0 + wc + n / (WR / 2) * 32; };
+        auto turned_col = [&](int n) { return i0 + wr + n % (WR / 2) * 64; };
+        read_old(turned_row(0), turned_col(0), old[0]);
 #pragma unroll
-        for (int q = 0; q < WC; ++q)
+        for (int n = 0; n < kTurned; ++n) {
+            const int q = n / (WR / 2), pp = n % (WR / 2) * 2;
+            if (kAhead && n + 1 < kTurned) read_old(turned_row(n + 1), turned_col(n + 1), old[(n + 1) & 1]);
+            if (!kAhead && n > 0) read_old(turned_row(n), turned_col(n), old[n & 1]);
 #pragma unroll
-            for (int pp = 0; pp < WR; pp += 2) {  // 32 columns x 64 rows
+            for (int p = 0; p < 2; ++p)
 #pragma unroll
-                for (int p = 0; p < 2; ++p)
+                for (int g = 0; g < 4; ++g)
+                    *(f32x4 *)(mine + place(col, p * 32 + g * 8 + quad)) =
+                        f32x4{acc[pp + p][q][g * 4], acc[pp + p][q][g * 4 + 1],
+                              acc[pp + p][q][g * 4 + 2], acc[pp + p][q][g * 4 + 3]};
+            wave_sync();
 #pragma unroll
-                    for (int g = 0; g < 4; ++g)
-                        *(f32x4 *)(mine + place(col, p * 32 + g * 8 + quad)) =
-                            f32x4{acc[pp + p][q][g * 4], acc[pp + p][q][g * 4 + 1],
-                                  acc[pp + p][q][g * 4 + 2], acc[pp + p][q][g * 4 + 3]};
-                wave_sync();
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int r = k * 8 + line, i = j0 + wc + q * 32 + r, j = i0 + wr + pp * 32 + eight;
-                    float v[8];
-                    take(r, v);
-                    value(i, j, v);
-                    store(i, j, v);
-                }
-                wave_sync();
+            for (int k = 0; k < kRounds; ++k) {
+                const int r = row_in_block(k), i = turned_row(n) + r, j = turned_col(n) + eight;
+                float v[8];
+                take(r, v);
+                value(i, j, old[n & 1], k, v);
+                store(i, j, v);
             }
+            wave_sync();
+        }
     }
 }
 
