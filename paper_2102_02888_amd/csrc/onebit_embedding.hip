@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/onebit.h"
 #include "onebit_internal.h"
@@ -107,6 +108,7 @@ __global__ __launch_bounds__(256) void k_embedding(const T *__restrict__ table, 
 constexpr int kDigits = 256;
 constexpr int kSmallTokens = 4096;   // sorted by one workgroup, in LDS
 constexpr int kSmallThreads = 1024;
+constexpr int kSmallRows = 1 << 18;  // rows that the sorting workgroup has bits for
 constexpr int kSortBlocks = 128;     // workgroups of a pass over more
 constexpr int kFillBlocks = 512;
 
@@ -118,9 +120,9 @@ struct Key {
     }
 };
 
-// Zeros rows [begin, end) of the gradient, by workgroup `part` of `parts`.
-// These run beside the sort, which keeps few CUs busy and no memory; rows with
-// places are then written a second time.
+// Zeros rows [begin, end) of the gradient, by workgroup `part` of `parts`: those
+// without a place, once the list is sorted; all of them beside the sort of a short
+// list, which keeps few CUs busy and no memory.
 struct Fill {
     void *grad;
     int64_t ld;
@@ -128,25 +130,73 @@ struct Fill {
     int width, elem;     // elem: bytes of an element
 };
 
+// Zeros `len` bytes, an even number from an even address on, by `threads` threads.
+__device__ __forceinline__ void fill_bytes(char *at, int64_t len, int thread, int threads)
+{
+    char *stop = at + len;
+    char *first = (char *)(((uintptr_t)at + 15) & ~(uintptr_t)15);
+    char *last = (char *)((uintptr_t)stop & ~(uintptr_t)15);
+    if (first > last) first = last = stop;  // a short run that crosses no 16 bytes
+    for (char *q = at + thread * 2; q < first && q < stop; q += threads * 2) *(uint16_t *)q = 0;
+    for (char *q = first + thread * 16; q < last; q += threads * 16) *(uint4 *)q = uint4{0, 0, 0, 0};
+    for (char *q = last + thread * 2; q < stop; q += threads * 2) *(uint16_t *)q = 0;
+}
+
+__device__ __forceinline__ void fill_range(const Fill &f, int part, int parts, int64_t &r0,
+                                           int64_t &r1)
+{
+    r0 = f.begin + (f.end - f.begin) * part / parts;
+    r1 = f.begin + (f.end - f.begin) * (part + 1) / parts;
+}
+
 __device__ void fill_rows(const Fill &f, int part, int parts)
 {
-    const int64_t rows = f.end - f.begin;
-    const int64_t r0 = f.begin + rows * part / parts, r1 = f.begin + rows * (part + 1) / parts;
-    if (r0 >= r1) return;
-    const int64_t row_bytes = (int64_t)f.width * f.elem;
-    char *base = (char *)f.grad + r0 * f.ld * f.elem;
-    int64_t pieces = r1 - r0, len = row_bytes, pitch = f.ld * f.elem;
-    if (f.ld == f.width) len *= pieces, pieces = 1;  // one run of bytes
-    for (int64_t p = 0; p < pieces; ++p) {
-        char *at = base + p * pitch, *stop = at + len;
-        char *first = (char *)(((uintptr_t)at + 15) & ~(uintptr_t)15);
-        char *last = (char *)((uintptr_t)stop & ~(uintptr_t)15);
-        if (first > last) first = last = stop;  // a short run that crosses no 16 bytes
-        for (char *q = at + threadIdx.x * 2; q < first && q < stop; q += blockDim.x * 2)
-            *(uint16_t *)q = 0;
-        for (char *q = first + threadIdx.x * 16; q < last; q += blockDim.x * 16)
-            *(uint4 *)q = uint4{0, 0, 0, 0};
-        for (char *q = last + threadIdx.x * 2; q < stop; q += blockDim.x * 2) *(uint16_t *)q = 0;
+    int64_t r0, r1;
+    fill_range(f, part, parts, r0, r1);
+    const int64_t bytes = (int64_t)f.width * f.elem, pitch = f.ld * f.elem;
+    char *base = (char *)f.grad + r0 * pitch;
+    if (r0 < r1 && f.ld == f.width)
+        fill_bytes(base, bytes * (r1 - r0), threadIdx.x, blockDim.x);  // one run
+    else
+        for (int64_t r = r0; r < r1; ++r, base += pitch)
+            fill_bytes(base, bytes, threadIdx.x, blockDim.x);
+}
+
+// The rows that have no bit, a wave for each.
+__device__ void fill_unmarked(const Fill &f, const uint32_t *__restrict__ present, int part,
+                              int parts)
+{
+    int64_t r0, r1;
+    fill_range(f, part, parts, r0, r1);
+    for (int64_t r = r0 + (threadIdx.x >> 6); r < r1; r += blockDim.x >> 6)
+        if (!(present[r >> 5] >> (r & 31) & 1))
+            fill_bytes((char *)f.grad + r * f.ld * f.elem, (int64_t)f.width * f.elem,
+                       threadIdx.x & 63, 64);
+}
+
+// The rows without a place: a thread looks its row up in the sorted keys, and a
+// wave zeros a row.
+__device__ void fill_absent(const Fill &f, const uint32_t *__restrict__ keys, int64_t tokens,
+                            int part, int parts)
+{
+    __shared__ bool absent[256];
+    int64_t r0, r1;
+    fill_range(f, part, parts, r0, r1);
+    for (int64_t r = r0; r < r1; r += 256) {
+        const uint32_t row = (uint32_t)(r + threadIdx.x);
+        int64_t lo = 0, hi = tokens;  // the first key that is not below the row's
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) / 2;
+            if (keys[mid] < row) lo = mid + 1;
+            else hi = mid;
+        }
+        __syncthreads();
+        absent[threadIdx.x] = r + threadIdx.x < r1 && (lo == tokens || keys[lo] != row);
+        __syncthreads();
+        for (int k = threadIdx.x >> 6; k < 256; k += 4)
+            if (absent[k])
+                fill_bytes((char *)f.grad + (r + k) * f.ld * f.elem, (int64_t)f.width * f.elem,
+                           threadIdx.x & 63, 64);
     }
 }
 
@@ -187,20 +237,28 @@ __device__ __forceinline__ uint32_t scan256(uint32_t v, uint32_t *wave_sums)
     return x - v;
 }
 
-// Up to kSmallTokens places: workgroup 0 sorts them whole, the others zero the
-// gradient.  Every wave owns consecutive keys, so that ranks within a wave and
-// waves in order keep the sort stable.
+// Up to kSmallTokens places: workgroup 0 sorts them whole, the others zero rows of
+// the gradient.  Every wave owns consecutive keys, so that ranks within a wave and
+// waves in order keep the sort stable.  It also leaves where every row's places
+// begin (begins[k] for the k-th row that has any, behind them the number of places;
+// *rows is their number) and a bit for every row that has any.
 __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const void *__restrict__ ids,
                                                               int ids_bytes, int tokens, Key key,
                                                               int bits, uint32_t *keys,
-                                                              uint32_t *order, Fill fill)
+                                                              uint32_t *order,
+                                                              uint32_t *begins, uint32_t *rows,
+                                                              uint32_t *present, int words,
+                                                              Fill fill)
 {
     if (blockIdx.x > 0) return fill_rows(fill, blockIdx.x - 1, gridDim.x - 1);
     constexpr int kWaves = kSmallThreads / 64;
     __shared__ uint32_t s_key[2][kSmallTokens], s_at[2][kSmallTokens];
     __shared__ uint32_t s_count[kWaves][kDigits];
     __shared__ uint32_t s_sums[4];
+    __shared__ uint32_t s_present[kSmallRows / 32], s_heads[kWaves], s_valid;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    for (int k = tid; k < words; k += kSmallThreads) s_present[k] = 0;
+    if (tid == 0) s_valid = 0;
     const int per_wave = (tokens + kWaves * 64 - 1) / (kWaves * 64) * 64;
     const int begin = min(wave * per_wave, tokens), end = min(begin + per_wave, tokens);
     for (int t = tid; t < tokens; t += kSmallThreads) {
@@ -245,10 +303,46 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const void *__rest
         }
         __syncthreads();
     }
+    // heads: places where another row begins
+    auto head = [&](int t) {
+        const uint32_t k = s_key[from][t];
+        return k < key.vocab && (t == 0 || s_key[from][t - 1] != k);
+    };
+    uint32_t heads = 0, valid = 0;
+    for (int t0 = begin; t0 < end; t0 += 64) {
+        const int t = t0 + lane;
+        const bool on = t < end;
+        heads += __popcll(__ballot(on && head(t)));
+        valid += __popcll(__ballot(on && s_key[from][t] < key.vocab));
+    }
+    if (lane == 0) {
+        s_heads[wave] = heads;
+        atomicAdd(&s_valid, valid);
+    }
+    __syncthreads();
+    uint32_t at = 0;
+    for (int w = 0; w < wave; ++w) at += s_heads[w];
+    for (int t0 = begin; t0 < end; t0 += 64) {
+        const int t = t0 + lane;
+        const bool on = t < end && head(t);
+        const uint64_t all = __ballot(on);
+        if (on) {
+            begins[at + __popcll(all & ((1ull << lane) - 1))] = t;
+            const uint32_t k = s_key[from][t];
+            if (words > 0) atomicOr(&s_present[k >> 5], 1u << (k & 31));
+        }
+        at += __popcll(all);
+    }
+    if (wave == kWaves - 1 && lane == 0) {
+        begins[at] = s_valid;
+        *rows = at;
+    }
     for (int t = tid; t < tokens; t += kSmallThreads) {
         keys[t] = s_key[from][t];
         order[t] = s_at[from][t];
     }
+    __syncthreads();
+    for (int k = tid; k < words; k += kSmallThreads) present[k] = s_present[k];
 }
 
 // One digit's counts per workgroup.  FIRST: keys come from the ids.
@@ -262,11 +356,8 @@ __device__ __forceinline__ uint32_t key_at(const void *src, int ids_bytes, const
 template <bool FIRST>
 __global__ __launch_bounds__(256) void k_sort_count(const void *__restrict__ src, int ids_bytes,
                                                     int64_t tokens, int64_t per_block, int blocks,
-                                                    Key key, int shift, uint32_t *counts,
-                                                    Fill fill)
+                                                    Key key, int shift, uint32_t *counts)
 {
-    if ((int)blockIdx.x >= blocks)
-        return fill_rows(fill, blockIdx.x - blocks, gridDim.x - blocks);
     __shared__ uint32_t s_count[kDigits];
     s_count[threadIdx.x] = 0;
     __syncthreads();
@@ -286,10 +377,8 @@ __global__ __launch_bounds__(256) void k_sort_move(const void *__restrict__ src,
                                                    int shift, int width,
                                                    const uint32_t *__restrict__ counts,
                                                    uint32_t *__restrict__ keys,
-                                                   uint32_t *__restrict__ order, Fill fill)
+                                                   uint32_t *__restrict__ order)
 {
-    if ((int)blockIdx.x >= blocks)
-        return fill_rows(fill, blockIdx.x - blocks, gridDim.x - blocks);
     __shared__ uint32_t s_count[4][kDigits];
     __shared__ uint32_t s_sums[4];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -306,6 +395,7 @@ __global__ __launch_bounds__(256) void k_sort_move(const void *__restrict__ src,
     const int64_t block_end = min((blockIdx.x + 1) * per_block, tokens);
     const int64_t begin = min(blockIdx.x * per_block + wave * per_wave, block_end);
     const int64_t end = min(begin + per_wave, block_end);
+#pragma unroll 4
     for (int64_t t = begin + lane; t < end; t += 64)
         atomicAdd(&s_count[wave][(key_at<FIRST>(src, ids_bytes, key, t) >> shift) & 255], 1u);
     __syncthreads();
@@ -316,21 +406,30 @@ __global__ __launch_bounds__(256) void k_sort_move(const void *__restrict__ src,
         at += n;
     }
     __syncthreads();
-    for (int64_t t0 = begin; t0 < end; t0 += 64) {
-        const int64_t t = t0 + lane;
-        const bool on = t < end;
-        const uint32_t k = on ? key_at<FIRST>(src, ids_bytes, key, t) : 0;
-        const uint32_t digit = (k >> shift) & 255;
-        const uint64_t same = same_digit(digit, width, on);
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        if (on) {
-            const uint32_t pos = s_count[wave][digit] + rank;
-            keys[pos] = k;
-            order[pos] = FIRST ? (uint32_t)t : src_at[t];
+    constexpr int kBatch = 4;  // rounds of 64 whose keys are loaded together
+    for (int64_t t0 = begin; t0 < end; t0 += 64 * kBatch) {
+        uint32_t k[kBatch], from[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int64_t t = min(t0 + u * 64 + lane, end - 1);
+            k[u] = key_at<FIRST>(src, ids_bytes, key, t);
+            from[u] = FIRST ? (uint32_t)t : src_at[t];
         }
-        wave_sync();
-        if (on && rank == 0) s_count[wave][digit] += (uint32_t)__popcll(same);
-        wave_sync();
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const bool on = t0 + u * 64 + lane < end;
+            const uint32_t digit = (k[u] >> shift) & 255;
+            const uint64_t same = same_digit(digit, width, on);
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            if (on) {
+                const uint32_t pos = s_count[wave][digit] + rank;
+                keys[pos] = k[u];
+                order[pos] = from[u];
+            }
+            wave_sync();
+            if (on && rank == 0) s_count[wave][digit] += (uint32_t)__popcll(same);
+            wave_sync();
+        }
     }
 }
 
@@ -340,140 +439,157 @@ __global__ __launch_bounds__(256) void k_sort_move(const void *__restrict__ src,
 
 // The sorted list is cut into pieces of `piece` places, whatever rows they
 // belong to, so that a frequent token costs what its places do.  A thread adds
-// kCols columns of a piece's places in order.  A row that lies inside a piece is
+// V columns of a piece's places in order.  A row that lies inside a piece is
 // finished there; a row that crosses a piece's end leaves one partial sum per
 // piece it touches (slot 0: it began in an earlier piece, slot 1: it begins
-// here), which k_grad_join adds in order.
+// here), which k_grad_join adds.
 struct Sums {
     const uint32_t *keys, *order;
     int64_t tokens, vocab;
-    int width, per_row, piece;
+    int width, per_row, piece;  // per_row: threads that share a row
     int64_t pieces;
     float scale;
     int accumulate;
     int64_t dout_ld, grad_ld;
-    float *partial;  // [pieces][2][per_row * kCols]
+    float *partial;  // [pieces][2][per_row * V]
 };
 
-template <class G>
+// Columns of a row's thread number n: V from n V on, or, so that every load is a
+// whole one, the row's last V.  skip: those that the thread before has too.
+template <int V>
+struct Columns {
+    int first, skip;
+    __device__ __forceinline__ Columns(int n, int width)
+        : first(V == 1 ? n : min(n * V, width - V)), skip(n * V - first) {}
+};
+
+template <int V, class G>
 __device__ __forceinline__ void finish_row(const Sums &s, G *__restrict__ grad, uint32_t row,
-                                           int c, const float (&acc)[kCols])
+                                           const Columns<V> &c, const float (&acc)[V])
 {
-    G *p = grad + (int64_t)row * s.grad_ld + c;
-    float v[kCols] = {};
-    if (s.accumulate) load_some(p, v, s.width - c);
+    G *p = grad + (int64_t)row * s.grad_ld + c.first;
+    float v[V];
 #pragma unroll
-    for (int k = 0; k < kCols; ++k)
-        v[k] = s.accumulate ? v[k] + s.scale * acc[k] : s.scale * acc[k];
-    store_some(p, v, s.width - c);
-}
-
-__device__ __forceinline__ float *partial_at(const Sums &s, int64_t piece, int slot, int c)
-{
-    return s.partial + ((piece * 2 + slot) * s.per_row) * kCols + c;
-}
-
-constexpr int kAhead = 8;  // rows whose loads are in flight together
-constexpr int kJoin = 8;   // threads that share a crossing row's partial sums
-
-// kCols elements as they lie in memory, `left` of which exist.
-template <class T>
-struct Raw {
-    T v[kCols];
-};
-
-template <class T>
-__device__ __forceinline__ void load_raw(const T *p, Raw<T> &r, int left)
-{
-    if (left >= kCols) {
-        __builtin_memcpy(&r, p, sizeof r);
+    for (int k = 0; k < V; ++k) v[k] = s.scale * acc[k];
+    if (c.skip == 0) {
+        if (s.accumulate) {
+            float old[V];
+            load_vec(p, old);
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] += old[k];
+        }
+        store_vec(p, v);
     } else {
 #pragma unroll
-        for (int k = 0; k < kCols; ++k) r.v[k] = k < left ? p[k] : (T)0.f;
+        for (int k = 0; k < V; ++k)
+            if (k >= c.skip) p[k] = (G)(s.accumulate ? v[k] + (float)p[k] : v[k]);
     }
 }
 
+template <int V>
+__device__ __forceinline__ float *partial_at(const Sums &s, int64_t piece, int slot, int n)
+{
+    return s.partial + ((piece * 2 + slot) * s.per_row + n) * V;
+}
+
+constexpr int kAhead = 4;  // rows whose loads are in flight together
+constexpr int kJoin = 8;   // threads that share a crossing row's partial sums
+
+template <class T, int V>
+struct Raw {  // elements as they lie in memory
+    T v[V];
+};
+
 // A thread's work is a chain: the list's entries, the rows they name, their sums.
 // Each part runs a batch ahead of the next: while a batch is added, the next one's
-// rows and the entries of the one after are under way.
-template <class D, class G>
+// rows and the entries of the one after are under way.  The loads stand outside of
+// every branch (an entry that adds nothing reads row 0 instead): where their
+// number is not known the compiler waits for all of them.
+template <class D, class G, int V>
 __global__ __launch_bounds__(256) void k_grad_sum(Sums s, const D *__restrict__ dout,
-                                                  G *__restrict__ grad)
+                                                  G *__restrict__ grad, int blocks, Fill fill)
 {
-    int c;
-    const int64_t piece = row_of((int64_t)blockIdx.x * 256, s.per_row, c);
+    if ((int)blockIdx.x >= blocks)
+        return fill_absent(fill, s.keys, s.tokens, blockIdx.x - blocks, gridDim.x - blocks);
+    int n;
+    const int64_t piece = row_of((int64_t)blockIdx.x * 256, s.per_row, n);
     if (piece >= s.pieces) return;
-    c *= kCols;
+    const Columns<V> c(n, s.width);
     const int64_t begin = piece * s.piece, end = min(begin + s.piece, s.tokens);
     const uint32_t none = (uint32_t)s.vocab;
-    const int left = s.width - c;
+    const D *from = dout + c.first;
     struct Batch {
         uint32_t key[kAhead], at[kAhead];
     };
-    // (the list's areas reach to a whole piece; entries past its end are not used)
+    // (the list's areas reach four batches past the last piece)
     auto entries = [&](int64_t at, Batch &b) {
         __builtin_memcpy(b.key, __builtin_assume_aligned(s.keys + at, 16), sizeof b.key);
         __builtin_memcpy(b.at, __builtin_assume_aligned(s.order + at, 16), sizeof b.at);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (at + u >= end || b.key[u] >= none) b.key[u] = none;
+        for (int u = 0; u < kAhead; ++u) {
+            const bool on = at + u < end && b.key[u] < none;
+            b.key[u] = on ? b.key[u] : none;
+            b.at[u] = on ? b.at[u] : 0;
+        }
     };
-    auto rows = [&](const Batch &b, Raw<D> (&r)[kAhead]) {
+    auto rows = [&](const Batch &b, Raw<D, V> (&r)[kAhead]) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (b.key[u] != none) load_raw(dout + (int64_t)b.at[u] * s.dout_ld + c, r[u], left);
+            __builtin_memcpy(&r[u], from + (int64_t)b.at[u] * s.dout_ld, sizeof r[u]);
     };
-    Batch now, next;
-    Raw<D> r[kAhead];
-    entries(begin, now);
+    Batch entry[2];
+    Raw<D, V> r[2][kAhead];
+    entries(begin, entry[0]);
+    entries(begin + kAhead, entry[1]);
     const uint32_t previous = begin > 0 ? s.keys[begin - 1] : none;
     const uint32_t following = end < s.tokens ? s.keys[end] : none;
-    if (begin + kAhead < end) entries(begin + kAhead, next);
-    rows(now, r);
-    uint32_t row = now.key[0];
+    rows(entry[0], r[0]);
+    uint32_t row = entry[0].key[0];
     if (row == none) return;  // places that add nothing, as all that follow
     bool before = previous == row;
-    float acc[kCols] = {};
-    for (int64_t at = begin; at < end; at += kAhead) {
-        Raw<D> r2[kAhead];
+    float acc[V] = {};
+    // (two batches by turns, with no copies from one to the other: a copy would wait)
+    auto batch = [&](int64_t at, Batch &now, const Raw<D, V> (&mine)[kAhead], const Batch &next,
+                     Raw<D, V> (&theirs)[kAhead]) {
         Batch after;
-        if (at + kAhead < end) rows(next, r2);
-        if (at + 2 * kAhead < end) entries(at + 2 * kAhead, after);
+        entries(at + 2 * kAhead, after);
+        rows(next, theirs);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (now.key[u] == none) break;
             if (now.key[u] != row) {  // the row ends here
+                if (now.key[u] == none) break;
                 if (before)
-                    store_vec(partial_at(s, piece, 0, c), acc);
+                    store_vec(partial_at<V>(s, piece, 0, n), acc);
                 else
-                    finish_row(s, grad, row, c, acc);
+                    finish_row<V>(s, grad, row, c, acc);
                 row = now.key[u];
                 before = false;
 #pragma unroll
-                for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
+                for (int i = 0; i < V; ++i) acc[i] = 0.f;
             }
 #pragma unroll
-            for (int i = 0; i < kCols; ++i) acc[i] += (float)r[u].v[i];
+            for (int i = 0; i < V; ++i) acc[i] += (float)mine[u].v[i];
         }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) r[u] = r2[u];
-        now = next;
-        next = after;
+        now = after;
+    };
+    for (int64_t at = begin; at < end; at += 2 * kAhead) {
+        batch(at, entry[0], r[0], entry[1], r[1]);
+        batch(at + kAhead, entry[1], r[1], entry[0], r[0]);
     }
     if (before)
-        store_vec(partial_at(s, piece, 0, c), acc);
+        store_vec(partial_at<V>(s, piece, 0, n), acc);
     else if (following == row)
-        store_vec(partial_at(s, piece, 1, c), acc);
+        store_vec(partial_at<V>(s, piece, 1, n), acc);
     else
-        finish_row(s, grad, row, c, acc);
+        finish_row<V>(s, grad, row, c, acc);
 }
 
 // Rows that cross pieces, by the piece they begin in: of the pieces that follow,
 // each of kJoin threads adds every kJoin-th, and their sums are added in order.
-template <class G>
+template <class G, int V>
 __global__ __launch_bounds__(256) void k_grad_join(Sums s, G *__restrict__ grad)
 {
-    __shared__ float part[kJoin][256 / kJoin][kCols + 1];
+    __shared__ float part[kJoin][256 / kJoin][V + 1];
     const int groups = (s.per_row + 256 / kJoin - 1) / (256 / kJoin);  // of columns
     const int64_t piece = blockIdx.x / groups;
     const int64_t begin = piece * s.piece, end = begin + s.piece;
@@ -482,36 +598,89 @@ __global__ __launch_bounds__(256) void k_grad_join(Sums s, G *__restrict__ grad)
     if (row >= s.vocab || s.keys[end - 1] != row) return;
     if (begin > 0 && s.keys[begin] == row && s.keys[begin - 1] == row) return;  // it began earlier
     const int lane = threadIdx.x % (256 / kJoin), turn = threadIdx.x / (256 / kJoin);
-    const int c = ((int)(blockIdx.x % groups) * (256 / kJoin) + lane) * kCols;
-    const bool mine = c < s.per_row * kCols;
-    float acc[kCols] = {};
-    if (turn == 0 && mine) load_vec(partial_at(s, piece, 1, c), acc);
+    const int n = (int)(blockIdx.x % groups) * (256 / kJoin) + lane;
+    const bool mine = n < s.per_row;
+    float acc[V] = {};
+    if (turn == 0 && mine) load_vec(partial_at<V>(s, piece, 1, n), acc);
     constexpr int kBatch = 4;
     for (int64_t q = piece + 1 + turn; q < s.pieces; q += kBatch * kJoin) {
-        float v[kBatch][kCols];
+        float v[kBatch][V];
         bool on[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             const int64_t p = min(q + u * kJoin, s.pieces - 1);
             on[u] = q + u * kJoin < s.pieces && s.keys[p * s.piece] == row;
-            if (mine) load_vec(partial_at(s, p, 0, c), v[u]);
+            if (mine) load_vec(partial_at<V>(s, p, 0, n), v[u]);
         }
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
             if (on[u])
 #pragma unroll
-                for (int i = 0; i < kCols; ++i) acc[i] += v[u][i];
+                for (int i = 0; i < V; ++i) acc[i] += v[u][i];
         if (!on[kBatch - 1]) break;
     }
 #pragma unroll
-    for (int i = 0; i < kCols; ++i) part[turn][lane][i] = acc[i];
+    for (int i = 0; i < V; ++i) part[turn][lane][i] = acc[i];
     __syncthreads();
     if (turn > 0 || !mine) return;
 #pragma unroll
     for (int t = 1; t < kJoin; ++t)
 #pragma unroll
-        for (int i = 0; i < kCols; ++i) acc[i] += part[t][lane][i];
-    finish_row(s, grad, row, c, acc);
+        for (int i = 0; i < V; ++i) acc[i] += part[t][lane][i];
+    finish_row<V>(s, grad, row, Columns<V>(n, s.width), acc);
+}
+
+// Sums of a short list: a workgroup takes one row's places, or up to `across`
+// threads' columns of them, with kSmallThreads / across threads per column that add
+// every so manieth place; their sums are added in order.  The workgroups behind the
+// rows' zero the rows without a place.
+template <class D, class G, int V>
+__global__ __launch_bounds__(kSmallThreads) void k_grad_rows(Sums s, const D *__restrict__ dout,
+                                                             G *__restrict__ grad, int across,
+                                                             int groups,
+                                                             const uint32_t *__restrict__ begins,
+                                                             const uint32_t *__restrict__ rows,
+                                                             const uint32_t *__restrict__ present,
+                                                             Fill fill)
+{
+    __shared__ float part[kSmallThreads * V];
+    const int blocks = (int)s.tokens * groups;
+    if ((int)blockIdx.x >= blocks)
+        return fill_unmarked(fill, present, blockIdx.x - blocks, gridDim.x - blocks);
+    const int index = blockIdx.x / groups;
+    if (index >= (int)*rows) return;
+    const int begin = begins[index], end = begins[index + 1];
+    const int turns = kSmallThreads / across, turn = threadIdx.x / across;
+    const int n = blockIdx.x % groups * across + threadIdx.x % across;
+    const bool mine = n < s.per_row && turn < turns;
+    const Columns<V> c(min(n, s.per_row - 1), s.width);
+    const D *from = dout + c.first;
+    float acc[V] = {};
+    if (mine)
+        for (int at = begin + turn; at < end; at += turns * kAhead) {
+            Raw<D, V> r[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)  // (past the end: the last place again)
+                __builtin_memcpy(&r[u], from + (int64_t)s.order[min(at + u * turns, end - 1)] * s.dout_ld,
+                                 sizeof r[u]);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (at + u * turns < end)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[i] += (float)r[u].v[i];
+        }
+    const int used = min(turns, end - begin);
+    if (used > 1) {
+        if (turn > 0 && turn < used)
+#pragma unroll
+            for (int i = 0; i < V; ++i) part[threadIdx.x * V + i] = acc[i];
+        __syncthreads();
+    }
+    if (turn > 0 || !mine) return;
+    for (int t = 1; t < used; ++t)
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] += part[(t * across + threadIdx.x) * V + i];
+    finish_row<V>(s, grad, s.keys[begin], c, acc);
 }
 
 // ---------------------------------------------------------------------------
@@ -521,28 +690,26 @@ __global__ __launch_bounds__(256) void k_grad_join(Sums s, G *__restrict__ grad)
 constexpr int64_t kSizeLimit = (int64_t)1 << 31;
 
 struct GradLayout {
-    int piece;
+    int piece, columns;  // columns: of a thread
     int64_t pieces, per_row;
-    size_t keys[2], order[2], counts, partial, total;  // byte offsets
+    size_t keys[2], order[2], counts, partial, begins, rows, present, total;  // byte offsets
 };
 
 size_t round_up(size_t a, size_t m) { return (a + m - 1) / m * m; }
 
-// Places per piece: enough pieces to fill the GPU, and up to 128 places where
-// there are many, which bounds the partial sums and the join's chains.
-int piece_of(int64_t tokens)
-{
-    int p = 8;
-    while (p < 128 && tokens / p > 1024) p *= 2;
-    return p;
-}
-
-GradLayout grad_layout(int64_t tokens, int64_t width)
+// Columns of a thread: 16 bytes of dout, or one where a row is shorter than that.
+// Places per piece: as many as still leave 2^18 threads, up to 128, which bounds
+// the partial sums and the join's chains.  us, pieces of 16 / 32 / 64 / 128:
+// 131,072 bf16 places of 1,024 columns 187 / 165 / 159 / 156, 33,333 fp32 ones of
+// 771 68 / 78 / 100 / 100 (97 threads a row).
+GradLayout grad_layout(int64_t tokens, int64_t width, int elem)
 {
     GradLayout l{};
-    l.piece = piece_of(tokens);
+    l.columns = width >= 16 / elem ? 16 / elem : 1;
+    l.per_row = (width + l.columns - 1) / l.columns;
+    l.piece = 8;
+    while (l.piece < 128 && tokens / (2 * l.piece) * l.per_row >= (1 << 18)) l.piece *= 2;
     l.pieces = (tokens + l.piece - 1) / l.piece;
-    l.per_row = (width + kCols - 1) / kCols;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -550,11 +717,14 @@ GradLayout grad_layout(int64_t tokens, int64_t width)
         return here;
     };
     for (int k = 0; k < 2; ++k) {
-        l.keys[k] = take((size_t)l.pieces * l.piece * 4);
-        l.order[k] = take((size_t)l.pieces * l.piece * 4);
+        l.keys[k] = take(((size_t)l.pieces * l.piece + 4 * kAhead) * 4);
+        l.order[k] = take(((size_t)l.pieces * l.piece + 4 * kAhead) * 4);
     }
+    l.begins = take(((size_t)std::min<int64_t>(tokens, kSmallTokens) + 1) * 4);
+    l.rows = take(4);
+    l.present = take(kSmallRows / 8);
     l.counts = take((size_t)kSortBlocks * kDigits * 4);
-    l.partial = take((size_t)l.pieces * 2 * l.per_row * kCols * 4);
+    l.partial = take((size_t)l.pieces * 2 * l.per_row * l.columns * 4);
     l.total = at;
     return l;
 }
@@ -656,7 +826,7 @@ int onebit_embedding_grad_workspace(int64_t tokens, int64_t vocab, int64_t width
     TRY(check_size(tokens, "tokens"));
     TRY(check_size(vocab, "vocab"));
     TRY(check_size(width, "width"));
-    *bytes = grad_layout(tokens, width).total;
+    *bytes = std::max(grad_layout(tokens, width, 2).total, grad_layout(tokens, width, 4).total);
     return ONEBIT_OK;
 }
 
@@ -676,7 +846,7 @@ int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld,
     if ((uintptr_t)workspace % 16) return fail(ONEBIT_EALIGN, "workspace is not 16-byte aligned");
     if (vocab == 0 || width == 0 || (tokens == 0 && accumulate)) return ONEBIT_OK;
     hipStream_t st = (hipStream_t)stream;
-    const GradLayout l = grad_layout(tokens, width);
+    const GradLayout l = grad_layout(tokens, width, elem_bytes(dout_dtype));
     const int64_t blocks = (l.pieces * l.per_row + 255) / 256;
     const int64_t joins = (l.per_row + 256 / kJoin - 1) / (256 / kJoin);  // workgroups of a piece
     if (blocks > (1 << 23) || l.pieces * joins > (1 << 23))
@@ -689,10 +859,18 @@ int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld,
               elem_bytes(grad_dtype)};
     const int fills = accumulate ? 0 : (int)std::min<int64_t>(kFillBlocks, vocab);
     int now = 0;
-    if (tokens <= kSmallTokens) {
+    // Half of the rows are zeroed beside the sort of a short list, all of them where
+    // there are too many for its bits; the others beside the sums.
+    const bool small = tokens <= kSmallTokens;
+    const int words = small && vocab <= kSmallRows ? (int)((vocab + 31) / 32) : 0;
+    Fill rest = fill;
+    if (small) {
+        rest.begin = tokens == 0 || words == 0 ? fill.end : fill.end / 2;
+        fill.end = rest.begin;
         k_sort_small<<<1 + fills, kSmallThreads, 0, st>>>(
             ids, ids_bytes, (int)tokens, key, bits, (uint32_t *)(ws + l.keys[0]),
-            (uint32_t *)(ws + l.order[0]), fill);
+            (uint32_t *)(ws + l.order[0]), (uint32_t *)(ws + l.begins), (uint32_t *)(ws + l.rows),
+            (uint32_t *)(ws + l.present), words, fill);
     } else {
         const int sorters = (int)std::min<int64_t>(kSortBlocks, (tokens + 1023) / 1024);
         const int64_t per_block = ((tokens + sorters - 1) / sorters + 255) / 256 * 256;
@@ -701,28 +879,21 @@ int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld,
         const void *src = ids;
         const uint32_t *src_at = nullptr;
         for (int p = 0; p < passes; ++p) {
-            // the rows are zeroed in equal parts beside every launch of the sort
-            auto part = [&](int k) {
-                Fill f = fill;
-                f.begin = fill.end * k / (2 * passes);
-                f.end = fill.end * (k + 1) / (2 * passes);
-                return f;
-            };
             const int shift = 8 * p, width_bits = std::min(8, bits - shift);
             uint32_t *keys = (uint32_t *)(ws + l.keys[p & 1]);
             uint32_t *order = (uint32_t *)(ws + l.order[p & 1]);
             if (p == 0) {
-                k_sort_count<true><<<sorters + fills, 256, 0, st>>>(
-                    src, ids_bytes, tokens, per_block, sorters, key, shift, counts, part(0));
-                k_sort_move<true><<<sorters + fills, 256, 0, st>>>(
+                k_sort_count<true><<<sorters, 256, 0, st>>>(
+                    src, ids_bytes, tokens, per_block, sorters, key, shift, counts);
+                k_sort_move<true><<<sorters, 256, 0, st>>>(
                     src, src_at, ids_bytes, tokens, per_block, sorters, key, shift, width_bits,
-                    counts, keys, order, part(1));
+                    counts, keys, order);
             } else {
-                k_sort_count<false><<<sorters + fills, 256, 0, st>>>(
-                    src, ids_bytes, tokens, per_block, sorters, key, shift, counts, part(2 * p));
-                k_sort_move<false><<<sorters + fills, 256, 0, st>>>(
+                k_sort_count<false><<<sorters, 256, 0, st>>>(
+                    src, ids_bytes, tokens, per_block, sorters, key, shift, counts);
+                k_sort_move<false><<<sorters, 256, 0, st>>>(
                     src, src_at, ids_bytes, tokens, per_block, sorters, key, shift, width_bits,
-                    counts, keys, order, part(2 * p + 1));
+                    counts, keys, order);
             }
             src = keys;
             src_at = order;
@@ -734,13 +905,29 @@ int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld,
     Sums s{(const uint32_t *)(ws + l.keys[now]), (const uint32_t *)(ws + l.order[now]), tokens,
            vocab, (int)width, (int)l.per_row, l.piece, l.pieces, scale, accumulate, dout_ld,
            grad_ld, (float *)(ws + l.partial)};
-    with_type(grad_dtype, [&](auto *g) {
+    const int absent = accumulate ? 0 : (int)std::min<int64_t>(4 * kFillBlocks, (rest.end - rest.begin + 31) / 32);
+    const int across = (int)std::min<int64_t>(l.per_row, 128);
+    const int groups = (int)((l.per_row + across - 1) / across);
+    auto sums = [&](auto columns, auto *d, auto *g) {
+        using D = std::remove_pointer_t<decltype(d)>;
         using G = std::remove_pointer_t<decltype(g)>;
+        constexpr int V = decltype(columns)::value;
+        if (small) {
+            k_grad_rows<D, G, V><<<(int)tokens * groups + absent, kSmallThreads, 0, st>>>(
+                s, (const D *)dout, (G *)grad, across, groups, (const uint32_t *)(ws + l.begins),
+                (const uint32_t *)(ws + l.rows), (const uint32_t *)(ws + l.present), rest);
+            return;
+        }
+        k_grad_sum<D, G, V><<<blocks + absent, 256, 0, st>>>(s, (const D *)dout, (G *)grad,
+                                                             (int)blocks, rest);
+        if (l.pieces > 1) k_grad_join<G, V><<<l.pieces * joins, 256, 0, st>>>(s, (G *)grad);
+    };
+    with_type(grad_dtype, [&](auto *g) {
         with_type(dout_dtype, [&](auto *d) {
-            using D = std::remove_pointer_t<decltype(d)>;
-            k_grad_sum<D, G><<<blocks, 256, 0, st>>>(s, (const D *)dout, (G *)grad);
+            constexpr int kWide = 16 / sizeof(*d);
+            if (l.columns == 1) sums(std::integral_constant<int, 1>{}, d, g);
+            else sums(std::integral_constant<int, kWide>{}, d, g);
         });
-        if (l.pieces > 1) k_grad_join<G><<<l.pieces * joins, 256, 0, st>>>(s, (G *)grad);
     });
     return launched("embedding gradient launch");
 }
