@@ -37,6 +37,28 @@ __device__ __forceinline__ void store_vec(T *p, const float (&v)[N])
     __builtin_memcpy(p, t, sizeof t);
 }
 
+// ... past the caches: what a call writes once and does not read again leaves the
+// rows that it reads in them (131,072 rows of 1,024 bf16 numbers from an fp32 table:
+// 118 us with plain stores, 76 so).
+template <class T, int N>
+__device__ __forceinline__ void stream_vec(T *p, const float (&v)[N])
+{
+    constexpr int kBytes = sizeof(T) * N;
+    if constexpr (kBytes < 4) {
+        store_vec(p, v);
+    } else {
+        constexpr int kWords = kBytes % 16 == 0 ? 4 : kBytes % 8 == 0 ? 2 : 1, kPieces = kBytes / (4 * kWords);
+        typedef uint32_t words __attribute__((ext_vector_type(kWords), aligned(sizeof(T))));
+        T t[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) t[k] = (T)v[k];
+        words w[kPieces];
+        __builtin_memcpy(w, t, kBytes);
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) __builtin_nontemporal_store(w[k], (words *)p + k);
+    }
+}
+
 // The first `left` of N elements (a row's end); the others are 0 or not stored.
 template <class T, int N>
 __device__ __forceinline__ void load_some(const T *p, float (&v)[N], int left)
@@ -49,7 +71,7 @@ __device__ __forceinline__ void load_some(const T *p, float (&v)[N], int left)
 template <class T, int N>
 __device__ __forceinline__ void store_some(T *p, const float (&v)[N], int left)
 {
-    if (left >= N) return store_vec(p, v);
+    if (left >= N) return stream_vec(p, v);
 #pragma unroll
     for (int k = 0; k < N; ++k)
         if (k < left) p[k] = (T)v[k];
@@ -138,7 +160,9 @@ __device__ __forceinline__ void fill_bytes(char *at, int64_t len, int thread, in
     char *last = (char *)((uintptr_t)stop & ~(uintptr_t)15);
     if (first > last) first = last = stop;  // a short run that crosses no 16 bytes
     for (char *q = at + thread * 2; q < first && q < stop; q += threads * 2) *(uint16_t *)q = 0;
-    for (char *q = first + thread * 16; q < last; q += threads * 16) *(uint4 *)q = uint4{0, 0, 0, 0};
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    for (char *q = first + thread * 16; q < last; q += threads * 16)
+        __builtin_nontemporal_store(words{0, 0, 0, 0}, (words *)q);
     for (char *q = last + thread * 2; q < stop; q += threads * 2) *(uint16_t *)q = 0;
 }
 
@@ -478,7 +502,7 @@ __device__ __forceinline__ void finish_row(const Sums &s, G *__restrict__ grad, 
 #pragma unroll
             for (int k = 0; k < V; ++k) v[k] += old[k];
         }
-        store_vec(p, v);
+        stream_vec(p, v);
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -498,6 +522,19 @@ constexpr int kJoin = 8;   // threads that share a crossing row's partial sums
 template <class T, int V>
 struct Raw {  // elements as they lie in memory
     T v[V];
+    // every row is read once, so that it need not stay in the caches
+    __device__ __forceinline__ void load(const T *p)
+    {
+        constexpr int kBytes = sizeof(T) * V;
+        if constexpr (kBytes < 4) {
+            __builtin_memcpy(v, p, kBytes);
+        } else {
+            static_assert(kBytes == 4 || kBytes == 16, "one load");
+            typedef uint32_t words __attribute__((ext_vector_type(kBytes / 4), aligned(sizeof(T))));
+            const words w = __builtin_nontemporal_load((const words *)p);
+            __builtin_memcpy(v, &w, kBytes);
+        }
+    }
 };
 
 // A thread's work is a chain: the list's entries, the rows they name, their sums.
@@ -535,7 +572,7 @@ __global__ __launch_bounds__(256) void k_grad_sum(Sums s, const D *__restrict__ 
     auto rows = [&](const Batch &b, Raw<D, V> (&r)[kAhead]) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            __builtin_memcpy(&r[u], from + (int64_t)b.at[u] * s.dout_ld, sizeof r[u]);
+            r[u].load(from + (int64_t)b.at[u] * s.dout_ld);
     };
     Batch entry[2];
     Raw<D, V> r[2][kAhead];
@@ -661,8 +698,7 @@ __global__ __launch_bounds__(kSmallThreads) void k_grad_rows(Sums s, const D *__
             Raw<D, V> r[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)  // (past the end: the last place again)
-                __builtin_memcpy(&r[u], from + (int64_t)s.order[min(at + u * turns, end - 1)] * s.dout_ld,
-                                 sizeof r[u]);
+                r[u].load(from + (int64_t)s.order[min(at + u * turns, end - 1)] * s.dout_ld);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
                 if (at + u * turns < end)

@@ -19,8 +19,8 @@ _ID_BYTES = {torch.int32: 4, torch.int64: 8}
 
 
 def _matrix(t, name, rows=None, cols=None):
-    """(pointer, type code, leading dimension) of a 2-D GPU tensor with unit
-    stride in its rows; a contiguous tensor of more dimensions counts as rows
+    """(pointer, type code, leading dimension, rows, columns) of a 2-D GPU
+    tensor with unit stride in its rows; a contiguous tensor of more dimensions counts as rows
     of its last one."""
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
@@ -31,8 +31,9 @@ def _matrix(t, name, rows=None, cols=None):
         raise ValueError("%s must be a GPU tensor" % name)
     shape = t.shape
     if len(shape) == 2:
-        have, width, ld = shape[0], shape[1], t.stride(0)
-        if width > 1 and t.stride(1) != 1:
+        have, width = shape
+        ld, unit = t.stride()
+        if width > 1 and unit != 1:
             raise ValueError("%s must have unit stride in its last dimension" % name)
         if have > 1 and ld < width:
             raise ValueError("%s has overlapping rows" % name)
@@ -44,7 +45,7 @@ def _matrix(t, name, rows=None, cols=None):
     if (rows is not None and have != rows and shape[-1]) or (cols is not None and width != cols):
         raise ValueError("%s is %s; the call needs %s row(s) of %s elements"
                          % (name, tuple(shape), "any number of" if rows is None else rows, cols))
-    return t.data_ptr(), code, max(ld, width)
+    return t.data_ptr(), code, ld if ld > width else width, have, width
 
 
 def _ids(ids):
@@ -70,10 +71,8 @@ def onebit_embedding_forward(table, ids, out, scale=1.0, stream=None):
     """out[t] = scale * table[ids[t]]; an id outside the table gives a row of
     zeros.  out: one row per id."""
     ip, ib, tokens = _ids(ids)
-    tp, tcode, tld = _matrix(table, "table")
-    vocab, width = table.shape[-2:] if table.dim() == 2 else (table.numel() // table.shape[-1],
-                                                             table.shape[-1])
-    op, ocode, old = _matrix(out, "out", tokens, width)
+    tp, tcode, tld, vocab, width = _matrix(table, "table")
+    op, ocode, old, _, _ = _matrix(out, "out", tokens, width)
     _one_device(table, ids, out)
     call("onebit_embedding_forward", tp, tcode, tld, vocab, width, ip, ib, tokens, float(scale),
          op, ocode, old, _stream(stream))
@@ -92,11 +91,10 @@ def onebit_embedding_grad(grad_out, ids, grad_table, workspace, scale=1.0, paddi
     row v (accumulate: added to it); ids outside the table and equal to
     padding_idx add nothing."""
     ip, ib, tokens = _ids(ids)
-    gp, gcode, gld = _matrix(grad_table, "grad_table")
+    gp, gcode, gld, vocab, width = _matrix(grad_table, "grad_table")
     if grad_table.dim() != 2:
         raise ValueError("grad_table must be 2-D")
-    vocab, width = grad_table.shape
-    dp, dcode, dld = _matrix(grad_out, "grad_out", tokens, width)
+    dp, dcode, dld, _, _ = _matrix(grad_out, "grad_out", tokens, width)
     if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda \
             or not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous GPU tensor")
