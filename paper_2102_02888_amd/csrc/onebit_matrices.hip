@@ -35,6 +35,7 @@
 #include <memory>
 #include <new>
 #include <type_traits>
+#include <utility>
 #include <vector>
 
 #include "../../include/onebit.h"
@@ -66,8 +67,20 @@ struct Mat {
     int32_t flip;                // 1: X is the matrix transposed
     int32_t norm_first, norm_count;  // partial sums of the norm
     int32_t part_first, part_count;  // partial sums of the iterate's squares
-    int32_t pad;
+    int32_t slot_first, slot_count;  // counters of its tiles that several workgroups form
+    int32_t parts;               // of a Gram tile's summed index
     int64_t ex, em;              // elements of X and of D before this matrix's
+    int64_t sums;                // where the parts' sums are
+};
+
+// A tile of a product.  (16 bytes, beside a matrix's record that its tiles share: a
+// record of its own for every tile, 160 bytes, would be one load less to wait for
+// but a miss for every workgroup, and costs up to 18%.)
+struct MatTile {
+    int32_t mat;     // < 0: none
+    uint16_t i, j;
+    int32_t part;    // of Mat::parts, of the summed index
+    int32_t slot;    // of several parts: the counter
 };
 
 struct Item {
@@ -84,6 +97,8 @@ struct Areas {
     float *part;    // per tile of the iterate
     float *t;       // per matrix
     float *gamma;   // per matrix, of the first iterate
+    uint32_t *counter;  // per tile in parts: parts that are done
+    float *sums;        // their sums
 };
 
 struct Coefficients {
@@ -308,7 +323,10 @@ __global__ __launch_bounds__(256) void k_first(const Mat *__restrict__ mats,
     const double size = sqrt(sum) / (sqrt(sum) + eps);
     // a NaN, zero or infinite norm, and every norm above eps: 1
     const double gamma = size > 0 && size <= 0.5 ? exp2(fmin(-ceil(log2(size)), 120.0)) : 1.0;
-    if (it.i == 0 && it.j == 0 && threadIdx.x == 0) w.gamma[it.mat] = (float)gamma;
+    if (it.i == 0 && it.j == 0) {
+        if (threadIdx.x == 0) w.gamma[it.mat] = (float)gamma;
+        for (int k = threadIdx.x; k < mt.slot_count; k += 256) w.counter[mt.slot_first + k] = 0;
+    }
     const double factor = (double)kScale * gamma / (sqrt(sum) + eps);
     if (mt.flip) {
 #pragma unroll
@@ -539,7 +557,7 @@ __device__ __forceinline__ int deep_place(int byte)
 // the wait for a slab is what counts.
 template <bool PAIRS, int STEP, int BT, int WR, int WC, int KG, int THREADS, class O>
 __global__ __launch_bounds__(THREADS, 2) void k_product(
-    const Mat *__restrict__ mats, const Item *__restrict__ items, Areas w, Coefficients co,
+    const Mat *__restrict__ mats, const MatTile *__restrict__ tiles, Areas w, Coefficients co,
     float faded, O out, int scale_mode)
 {
     constexpr int kWaves = BT * BT / (1024 * WR * WC);
@@ -549,7 +567,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     __shared__ __attribute__((aligned(1024))) char buffer0[KG * 2 * kOperand],
         buffer1[KG * 2 * kOperand];
     __shared__ float scratch[KG * kWaves];
-    const Item it = items[(blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds];
+    const MatTile it = tiles[(blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds];
     if (it.mat < 0) return;
     const Mat mt = mats[it.mat];
     constexpr int kind = PAIRS ? 2 : 1;
@@ -565,15 +583,19 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     const _Float16 *x = w.x + ex, *d = w.d + em, *b = w.b + em;
     const _Float16 *pa = (STEP == kGram ? x : STEP == kPoly ? d : b) + i0 * pitch;
     const _Float16 *pb = kDeep ? x + j0 * kind : (STEP == kGram ? x : d) + j0 * pitch;
-    const int slabs = (int)(pitch / kSlab);  // even, but for tiles of 64
+    // Slabs: all of them, an even number but for tiles of 64, or this part's.
+    constexpr bool kInParts = STEP == kGram && KG > 1;
+    const int all_slabs = (int)(pitch / kSlab);
+    const int slab0 = kInParts ? (int)((int64_t)all_slabs * it.part / mt.parts) : 0;
+    const int slabs = kInParts ? (int)((int64_t)all_slabs * (it.part + 1) / mt.parts) - slab0 : all_slabs;
 
     f32x16 acc[WR][WC] = {};
     const RowStager<BT, kWaves> stage_a(pa, pitch, wave);
     const std::conditional_t<kDeep, DeepStager<PAIRS, BT, kWaves>, RowStager<BT, kWaves>> stage_b(
         pb, kDeep ? x_pitch : pitch, wave);
     auto stage = [&](int s, char *to) {
-        stage_a(s, to);
-        stage_b(s, to + kOperand);
+        stage_a(slab0 + s, to);
+        stage_b(slab0 + s, to + kOperand);
     };
     // Fragments of 16 numbers of the summed index: of a slab's kSteps, the k-th.
     constexpr int kSteps = PAIRS ? 2 : 4, kDeepBytes = BT * 2 * kind;
@@ -673,7 +695,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     struct Old {
         half8 hi[kRounds], lo[kRounds];
     } old[2];
-    auto row_in_block = [&](int k) { return (KG > 1 ? group : k) * 8 + line; };
+    auto row_in_block = [&](int k) { return (group * kRounds + k) * 8 + line; };
     auto read_old = [&](int i1, int j1, Old &o) {
         if constexpr (STEP != kGram) {
 #pragma unroll
@@ -774,7 +796,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     // 8 (r / 4) + 4 (lane / 32) + r % 4 of a 32 x 32 product.
     // With several groups every wave leaves its sums there, and adds and finishes the
     // KG-th part of the rows that its group has.
-    static_assert(KG == 1 || (KG == 4 && WR == 1 && WC == 2), "a quarter of 32 rows for a group");
+    static_assert(KG == 1 || (4 % KG == 0 && WR == 1 && WC == 2), "some of 32 rows for a group");
     static_assert(kWaves * 2048 * 4 <= 2 * kOperand, "the epilogue's LDS");
     float *const mine = (float *)buffer0 + wave_number() * 2048;
     float *const sums = (float *)buffer0 + wave * 2048;  // the first group's
@@ -842,6 +864,50 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
                 mine[place((r >> 2) * 8 + quad + (r & 3), q * 32 + col)] = acc[p][qq + q][r];
         part_sync();
         const int i1 = block_row(n), j1 = block_col(n);
+        // A tile in parts: every workgroup leaves its sums, and the last one to have done
+        // so (the counter, which it sets back) adds all of them in order and goes on.
+        if constexpr (kInParts) {
+            if (mt.parts > 1) {
+                auto at = [&](int part, int k) {
+                    return w.sums + mt.sums +
+                           ((int64_t)(it.slot - mt.slot_first) * mt.parts + part) * (BT * BT) +
+                           (wr + row_in_block(k)) * BT + wc + eight;
+                };
+#pragma unroll
+                for (int k = 0; k < kRounds; ++k) {
+                    float v[8];
+                    take(row_in_block(k), v);
+                    __builtin_memcpy(at(it.part, k), v, sizeof v);
+                }
+                __threadfence();
+                __syncthreads();
+                if (threadIdx.x == 0) {
+                    const uint32_t before = __hip_atomic_fetch_add(
+                        w.counter + it.slot, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+                    scratch[0] = before + 1 == (uint32_t)mt.parts ? 1.f : 0.f;
+                    if (before + 1 == (uint32_t)mt.parts)
+                        __hip_atomic_store(w.counter + it.slot, 0u, __ATOMIC_RELAXED,
+                                           __HIP_MEMORY_SCOPE_AGENT);
+                }
+                __syncthreads();
+                if (scratch[0] == 0.f) return;
+                __threadfence();
+#pragma unroll
+                for (int k = 0; k < kRounds; ++k) {
+                    float v[8] = {};
+                    for (int q = 0; q < mt.parts; ++q) {
+                        float one[8];
+                        __builtin_memcpy(one, at(q, k), sizeof one);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] += one[e];
+                    }
+                    const int i = i1 + row_in_block(k), j = j1 + eight;
+                    value(i, j, old[0], k, v);
+                    store(i, j, v);
+                }
+                return;
+            }
+        }
 #pragma unroll
         for (int k = 0; k < kRounds; ++k) {
             const int r = row_in_block(k), i = i1 + r, j = j1 + eight;
@@ -871,7 +937,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
             if (mt.flip) {
 #pragma unroll
                 for (int k = 0; k < kRounds; ++k) {
-                    const int c = (KG > 1 ? group : k) * 16 + (lane >> 2), r = (lane & 3) * 8;
+                    const int c = (group * kRounds + k) * 16 + (lane >> 2), r = (lane & 3) * 8;
                     float v[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = sums[place(r + e, c)];
@@ -924,18 +990,31 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
 
 using namespace onebit;
 
+// The tiles of one of a step's products and the kernel that forms them.
+struct Product {
+    int side = 0, groups = 1;  // of a tile; of waves (k_product's KG)
+    int64_t blocks = 0;
+    const MatTile *tiles = nullptr;
+};
+
+// What a call needs for one kind of products.
+struct Side {
+    int64_t ex = 0, em = 0, firsts = 0, parts = 0, slots = 0, sums = 0;
+    const Mat *mats = nullptr;
+    const Item *first_items = nullptr;
+    Product gram, poly, next;
+};
+
 struct onebit_matrices_s {
     int device = 0;
     int32_t count = 0;
-    int64_t extent = 0, ex = 0, em = 0;
-    int tile = 128, norm_size = 0;  // side of a tile; elements per workgroup of the norm
-    int64_t norms = 0, firsts = 0, parts = 0;
-    int64_t sym_blocks = 0, next_blocks = 0;  // workgroups of the products' launches
+    int64_t extent = 0, norms = 0;
+    int norm_size = 0;  // elements per workgroup of the norm
+    bool empty = true;
     std::vector<int64_t> offset;
     char *dev = nullptr;
-    const Mat *mats = nullptr;
-    const Item *norm_items = nullptr, *first_items = nullptr, *sym_items = nullptr,
-               *next_items = nullptr;
+    const Item *norm_items = nullptr;
+    Side side[2];  // by ONEBIT_PRODUCTS_*
 };
 
 namespace {
@@ -949,11 +1028,12 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
     } while (0)
 
 struct WorkspaceLayout {
-    size_t x0, x1, x_lo, d, b, norm, part, t, gamma, total;
+    size_t x0, x1, x_lo, d, b, norm, part, t, gamma, counter, sums, total;
 };
 
 WorkspaceLayout layout_of(const onebit_matrices_s *p, bool pairs)
 {
+    const Side &s = p->side[pairs ? ONEBIT_PRODUCTS_F32 : ONEBIT_PRODUCTS_F16];
     WorkspaceLayout l{};
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -962,69 +1042,237 @@ WorkspaceLayout layout_of(const onebit_matrices_s *p, bool pairs)
         return here;
     };
     const size_t half = pairs ? 4 : 2;
-    l.x0 = take(half * p->ex);
-    l.x1 = take(half * p->ex);
-    l.x_lo = take(pairs ? 0 : 2 * p->ex);
-    l.d = take(half * p->em);
-    l.b = take(half * p->em);
+    l.x0 = take(half * s.ex);
+    l.x1 = take(half * s.ex);
+    l.x_lo = take(pairs ? 0 : 2 * s.ex);
+    l.d = take(half * s.em);
+    l.b = take(half * s.em);
     l.norm = take(8 * (size_t)p->norms);
-    l.part = take(4 * (size_t)p->parts);
+    l.part = take(4 * (size_t)s.parts);
     l.t = take(4 * (size_t)p->count);
     l.gamma = take(4 * (size_t)p->count);
+    l.counter = take(4 * (size_t)s.slots);
+    l.sums = take(4 * (size_t)s.sums);
     l.total = at;
     return l;
 }
 
-// Side of the products' tiles for a list: 256, which reads half as much for each
-// product, where such tiles are enough to fill the GPU; 64, with the summed index
-// split over four groups of waves, where larger ones would leave CUs without work.
-int tile_for(const int64_t *rows, const int64_t *cols, int32_t count)
-{
-    auto tiles = [&](int64_t side) {
-        int64_t n = 0;
-        for (int32_t k = 0; k < count; ++k)
-            n += std::max<int64_t>(0, (rows[k] + side - 1) / side) *
-                 std::max<int64_t>(0, (cols[k] + side - 1) / side);
-        return n;
-    };
-    return tiles(256) >= 1024 ? 256 : tiles(128) >= 256 ? 128 : 64;
-}
-
 // Workgroups go to the XCDs round-robin, and each XCD has an L2 of its own: a
-// matrix's tiles go to one XCD as far as that keeps the XCDs' work even.  Items
+// matrix's tiles go to one XCD as far as that keeps the XCDs' work even.  Tiles
 // (with what one costs, the dearest first) are dealt out in runs of one matrix, each
 // to the XCD with the least so far; entry x * length + k is XCD x's k-th.
 struct Costed {
-    Item item;
-    int64_t cost;
+    MatTile tile;
+    double cost;
 };
 
-std::vector<Item> deal(std::vector<Costed> all)
+std::vector<MatTile> deal(std::vector<Costed> &all)
 {
     std::stable_sort(all.begin(), all.end(),
                      [](const Costed &a, const Costed &b) { return a.cost > b.cost; });
-    int64_t total = 0;
+    double total = 0;
     for (const Costed &c : all) total += c.cost;
-    const int64_t most = total / (kXcds * 8);  // of a run
-    std::vector<Item> lists[kXcds];
-    int64_t load[kXcds] = {};
+    const double most = total / (kXcds * 8) * (1 + 1e-9);  // of a run
+    std::vector<MatTile> lists[kXcds];
+    double load[kXcds] = {};
     for (size_t k = 0; k < all.size();) {
         const int to = (int)(std::min_element(load, load + kXcds) - load);
-        int64_t run = 0;
-        const int32_t mat = all[k].item.mat;
+        double run = 0;
+        const int32_t mat = all[k].tile.mat;
         do {
-            lists[to].push_back(all[k].item);
+            lists[to].push_back(all[k].tile);
             run += all[k].cost;
             ++k;
-        } while (k < all.size() && all[k].item.mat == mat && run + all[k].cost <= most);
+        } while (k < all.size() && all[k].tile.mat == mat && run + all[k].cost <= most);
         load[to] += run;
     }
     size_t length = 0;
     for (const auto &l : lists) length = std::max(length, l.size());
-    std::vector<Item> out(length * kXcds, Item{-1, 0, 0});
+    MatTile none{};
+    none.mat = -1;
+    std::vector<MatTile> out(length * kXcds, none);
     for (int x = 0; x < kXcds; ++x)
         std::copy(lists[x].begin(), lists[x].end(), out.begin() + x * length);
     return out;
+}
+
+// The kernels' shapes, and what a tile of each costs: us for a tile and for each of
+// its slabs, for pairs and for halves, on a CU that has as many of them as fit
+// (measured from lists of 1 to 96 matrices, 17 x 4,000 to 4,096 x 4,096).
+struct Shape {
+    int side, groups;
+    double tile[2], slab[2];
+};
+constexpr Shape kShapes[] = {
+    {64, 4, {4.0, 4.0}, {0.26, 0.23}},
+    {64, 2, {2.5, 2.5}, {0.24, 0.21}},
+    {128, 1, {3.0, 3.0}, {0.72, 0.65}},
+    {256, 1, {10.0, 10.0}, {2.7, 2.25}},
+};
+constexpr int kCus = 256;
+constexpr int kPartSlabs = 16;  // least slabs of a part
+
+struct Sizes {
+    int64_t m, n;
+};
+
+int64_t pad_to(int64_t v, int64_t side) { return (v + side - 1) / side * side; }
+
+// Tiles of a product of one matrix (rows of tiles, and per row r their number).
+int64_t tiles_of(const Sizes &z, const Shape &h, int pad, bool symmetric)
+{
+    const int64_t tm = pad_to(z.m, pad) / h.side, tn = pad_to(z.n, pad) / h.side;
+    return !symmetric ? tm * tn : h.groups > 1 ? tm * tm : tm * (tm + 1) / 2;
+}
+
+// Parts of the summed index of a Gram tile: as many as leave every CU one workgroup.
+int parts_of(const Sizes &z, const Shape &h, int pad, int64_t all_tiles, int kind)
+{
+    const int64_t slabs = pad_to(z.n, pad) * kind / kSlab;
+    return h.groups < 4 ? 1 : (int)std::max<int64_t>(1, std::min(kCus / std::max<int64_t>(all_tiles, 1),
+                                                                 slabs / kPartSlabs));
+}
+
+// Estimated us of a launch: every tile goes to the CU that is free first, the dearest
+// first; for long lists the mean and half of a tile.
+enum Which { kIsGram, kIsPoly, kIsNext };
+double launch_cost(const std::vector<Sizes> &all, const Shape &h, int pad, Which which, int kind)
+{
+    const int p = kind == 2 ? 0 : 1;
+    int64_t tiles = 0;
+    for (const Sizes &z : all) tiles += tiles_of(z, h, pad, which != kIsNext);
+    std::vector<std::pair<double, int64_t>> work;  // cost, how many
+    double total = 0, dearest = 0;
+    for (const Sizes &z : all) {
+        int64_t count = tiles_of(z, h, pad, which != kIsNext);
+        double slabs = (double)(pad_to(which == kIsGram ? z.n : z.m, pad) * kind / kSlab);
+        if (which == kIsGram) {
+            const int parts = parts_of(z, h, pad, tiles, kind);
+            count *= parts;
+            slabs = slabs / parts + (parts > 1 ? 8 : 0);  // and the wait for the others
+        }
+        const double cost = h.tile[p] + h.slab[p] * slabs;
+        work.push_back({cost, count});
+        total += cost * (double)count;
+        dearest = std::max(dearest, cost);
+    }
+    if (total > 64.0 * kCus * dearest) return total / kCus + dearest / 2;
+    std::sort(work.rbegin(), work.rend());
+    std::vector<double> cus(kCus, 0.0);  // a heap, the earliest on top
+    auto later = [](double a, double b) { return a > b; };
+    double last = 0;
+    for (const auto &[cost, count] : work)
+        for (int64_t k = 0; k < count; ++k) {
+            std::pop_heap(cus.begin(), cus.end(), later);
+            last = std::max(last, cus.back() += cost);
+            std::push_heap(cus.begin(), cus.end(), later);
+        }
+    return last;
+}
+
+// Chooses the three products' kernels: the last one's tile sets the padding, and the
+// other two take no larger one.
+void choose(const std::vector<Sizes> &all, int kind, Shape (&best)[3])
+{
+    double least = INFINITY;
+    for (const Shape &next : kShapes) {
+        double cost = launch_cost(all, next, next.side, kIsNext, kind);
+        Shape pick[3] = {next, next, next};
+        for (int which = 0; which < 2; ++which) {
+            double lowest = INFINITY;
+            for (const Shape &h : kShapes) {
+                if (h.side > next.side) continue;
+                const double c = launch_cost(all, h, next.side, (Which)which, kind);
+                if (c < lowest) {
+                    lowest = c;
+                    pick[which] = h;
+                }
+            }
+            cost += lowest;
+        }
+        if (cost < least) {
+            least = cost;
+            std::copy(pick, pick + 3, best);
+        }
+    }
+}
+
+// Tables of one side, on the host.
+struct Built {
+    std::vector<Mat> mats;
+    std::vector<Item> first;
+    std::vector<MatTile> gram, poly, next;
+};
+
+int build_side(std::vector<Mat> mats, int kind, Side &side, Built &out)
+{
+    constexpr int64_t kItems = 1 << 22;
+    std::vector<Sizes> sizes;
+    for (const Mat &m : mats)
+        if (m.m > 0) sizes.push_back(Sizes{m.m, m.n});
+    if (sizes.empty()) {
+        out.mats = std::move(mats);
+        return ONEBIT_OK;
+    }
+    Shape shape[3];
+    choose(sizes, kind, shape);
+    const int pad = shape[kIsNext].side, p = kind == 2 ? 0 : 1;
+    int64_t gram_tiles = 0;
+    for (const Sizes &z : sizes) gram_tiles += tiles_of(z, shape[kIsGram], pad, true);
+    std::vector<Costed> lists[3];
+    int64_t tiles = 0;
+    for (size_t k = 0; k < mats.size(); ++k) {
+        Mat &m = mats[k];
+        if (m.m == 0) continue;
+        const Sizes z{m.m, m.n};
+        m.mp = (int32_t)pad_to(m.m, pad);
+        m.np = (int32_t)pad_to(m.n, pad);
+        m.ex = side.ex;
+        m.em = side.em;
+        side.ex += (int64_t)m.mp * m.np;
+        side.em += (int64_t)m.mp * m.mp;
+        m.part_first = (int32_t)side.parts;
+        m.part_count = (int32_t)tiles_of(z, shape[kIsNext], pad, false);
+        side.parts += m.part_count;
+        m.slot_first = (int32_t)side.slots;
+        const int parts = m.parts = parts_of(z, shape[kIsGram], pad, gram_tiles, kind);
+        m.sums = side.sums;
+        if (parts > 1) m.slot_count = (int32_t)tiles_of(z, shape[kIsGram], pad, true);
+        side.slots += m.slot_count;
+        side.sums += (int64_t)m.slot_count * parts * shape[kIsGram].side * shape[kIsGram].side;
+        const int rp = (m.flip ? m.np : m.mp) / kPrep, cp = (m.flip ? m.mp : m.np) / kPrep;
+        for (int which = 0; which < 3; ++which) tiles += tiles_of(z, shape[which], pad, which != kIsNext);
+        if (tiles > kItems || (int64_t)out.first.size() + (int64_t)rp * cp > kItems)
+            return fail(ONEBIT_EINVAL, "too many tiles (matrix %d)", (int)k);
+        for (int i = 0; i < rp; ++i)
+            for (int j = 0; j < cp; ++j) out.first.push_back(Item{(int32_t)k, (uint16_t)i, (uint16_t)j});
+        int32_t slot = m.slot_first;
+        for (int which = 0; which < 3; ++which) {
+            const Shape &h = shape[which];
+            const int tm = m.mp / h.side, tn = which == kIsNext ? m.np / h.side : tm;
+            const int split = which == kIsGram ? parts : 1;
+            const double slabs = (double)((which == kIsGram ? m.np : m.mp) * kind / kSlab) / split;
+            for (int i = 0; i < tm; ++i)
+                for (int j = 0; j < (which == kIsNext || h.groups > 1 ? tn : i + 1); ++j) {
+                    MatTile t{};
+                    t.mat = (int32_t)k;
+                    t.i = (uint16_t)i;
+                    t.j = (uint16_t)j;
+                    t.slot = split > 1 ? slot++ : 0;
+                    for (t.part = 0; t.part < split; ++t.part)
+                        lists[which].push_back(Costed{t, h.tile[p] + h.slab[p] * slabs});
+                }
+        }
+    }
+    out.gram = deal(lists[kIsGram]);
+    out.poly = deal(lists[kIsPoly]);
+    out.next = deal(lists[kIsNext]);
+    side.firsts = (int64_t)out.first.size();
+    side.gram = Product{shape[kIsGram].side, shape[kIsGram].groups, (int64_t)out.gram.size(), nullptr};
+    side.poly = Product{shape[kIsPoly].side, shape[kIsPoly].groups, (int64_t)out.poly.size(), nullptr};
+    side.next = Product{shape[kIsNext].side, shape[kIsNext].groups, (int64_t)out.next.size(), nullptr};
+    out.mats = std::move(mats);
+    return ONEBIT_OK;
 }
 
 int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
@@ -1034,12 +1282,10 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
     hipError_t e = hipGetDevice(&p->device);
     if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
     std::vector<Mat> mats(count);
-    std::vector<Item> norm, first;
-    std::vector<Costed> sym, next;
+    std::vector<Item> norm;
     p->count = count;
     p->offset.resize(count);
     int64_t at = 0;
-    const int tile = p->tile = tile_for(rows, cols, count);
     // 2,048 elements are one load per thread; four where that still makes many workgroups
     double elements = 0;
     for (int32_t k = 0; k < count; ++k) elements += (double)rows[k] * (double)cols[k];
@@ -1059,8 +1305,9 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
                         (long long)c);
         if (off < 0 || off > kMost)
             return fail(ONEBIT_EINVAL, "offset[%d] = %lld", k, (long long)off);
+        // (r - 1) * pitch < 2^60
         const int64_t span = r > 0 && c > 0 ? (r - 1) * pitch + c : 0;
-        if (off + span > kMost || span > kMost)
+        if (off + span > kMost)
             return fail(ONEBIT_EINVAL, "matrix %d ends above 2^40 elements", k);
         p->offset[k] = off;
         at = off + (span + 63) / 64 * 64;
@@ -1075,72 +1322,54 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
         m.m = (int32_t)std::min(r, c);
         m.n = (int32_t)std::max(r, c);
         if (m.m == 0) continue;
-        m.mp = (m.m + tile - 1) / tile * tile;
-        m.np = (m.n + tile - 1) / tile * tile;
-        m.ex = p->ex;
-        m.em = p->em;
-        p->ex += (int64_t)m.mp * m.np;
-        p->em += (int64_t)m.mp * m.mp;
-        const int tm = m.mp / tile, tn = m.np / tile;
+        p->empty = false;
         m.norm_first = (int32_t)norm.size();
         m.norm_count = (int32_t)((r * c + size - 1) / size);
-        m.part_first = (int32_t)next.size();
-        m.part_count = tm * tn;
-        const int rp = (m.flip ? m.np : m.mp) / kPrep, cp = (m.flip ? m.mp : m.np) / kPrep;
-        if ((int64_t)norm.size() + m.norm_count > kItems || (int64_t)first.size() + (int64_t)rp * cp > kItems)
-            return fail(ONEBIT_EINVAL, "too many tiles (matrix %d)", k);
+        if ((int64_t)norm.size() + m.norm_count > kItems)
+            return fail(ONEBIT_EINVAL, "too many elements (matrix %d)", k);
         for (int32_t q = 0; q < m.norm_count; ++q)
             norm.push_back(Item{k, (uint16_t)(q >> 16), (uint16_t)q});
-        for (int i = 0; i < rp; ++i)
-            for (int j = 0; j < cp; ++j) first.push_back(Item{k, (uint16_t)i, (uint16_t)j});
-        for (int i = 0; i < tm; ++i)
-            for (int j = 0; j < (tile == 64 ? tm : i + 1); ++j)
-                sym.push_back(Costed{{k, (uint16_t)i, (uint16_t)j}, m.np + m.mp});
-        for (int i = 0; i < tm; ++i)
-            for (int j = 0; j < tn; ++j)
-                next.push_back(Costed{{k, (uint16_t)i, (uint16_t)j}, m.mp});
     }
     p->norms = (int64_t)norm.size();
-    p->firsts = (int64_t)first.size();
-    p->parts = (int64_t)next.size();
-    const std::vector<Item> sym_dealt = deal(std::move(sym)), next_dealt = deal(std::move(next));
-    p->sym_blocks = (int64_t)sym_dealt.size();
-    p->next_blocks = (int64_t)next_dealt.size();
+    Built built[2];
+    TRY(build_side(mats, 2, p->side[ONEBIT_PRODUCTS_F32], built[ONEBIT_PRODUCTS_F32]));
+    TRY(build_side(mats, 1, p->side[ONEBIT_PRODUCTS_F16], built[ONEBIT_PRODUCTS_F16]));
     // one host buffer in the layout of the device allocation
-    size_t total = 0;
-    auto take = [&](size_t bytes) {
-        const size_t here = total;
-        total += up256(bytes);
+    std::vector<char> host;
+    auto put = [&](const auto &v) {
+        const size_t here = host.size();
+        host.resize(here + up256(std::max<size_t>(v.size() * sizeof(v[0]), 1)));
+        if (!v.empty()) std::memcpy(host.data() + here, v.data(), v.size() * sizeof(v[0]));
         return here;
     };
-    const size_t o_mats = take(mats.size() * sizeof(Mat));
-    const size_t o_norm = take(norm.size() * sizeof(Item)), o_first = take(first.size() * sizeof(Item));
-    const size_t o_sym = take(sym_dealt.size() * sizeof(Item));
-    const size_t o_next = take(next_dealt.size() * sizeof(Item));
-    std::vector<char> host(total);
-    auto copy = [&](size_t to, const auto &v) {
-        if (!v.empty()) std::memcpy(host.data() + to, v.data(), v.size() * sizeof(v[0]));
-    };
-    copy(o_mats, mats);
-    copy(o_norm, norm);
-    copy(o_first, first);
-    copy(o_sym, sym_dealt);
-    copy(o_next, next_dealt);
+    const size_t o_norm = put(norm);
+    size_t o[2][5];
+    for (int k = 0; k < 2; ++k) {
+        o[k][0] = put(built[k].mats);
+        o[k][1] = put(built[k].first);
+        o[k][2] = put(built[k].gram);
+        o[k][3] = put(built[k].poly);
+        o[k][4] = put(built[k].next);
+    }
     void *dev = nullptr;
-    e = hipMalloc(&dev, total);
+    e = hipMalloc(&dev, host.size());
     if (e == hipErrorOutOfMemory) return fail(ONEBIT_ENOMEM, "hipMalloc of the matrix tables");
     if (e != hipSuccess) return hip_fail(e, "hipMalloc");
-    e = hipMemcpy(dev, host.data(), total, hipMemcpyHostToDevice);
+    e = hipMemcpy(dev, host.data(), host.size(), hipMemcpyHostToDevice);
     if (e != hipSuccess) {
         (void)hipFree(dev);
         return hip_fail(e, "copy of the matrix tables");
     }
     p->dev = (char *)dev;
-    p->mats = (const Mat *)(p->dev + o_mats);
     p->norm_items = (const Item *)(p->dev + o_norm);
-    p->first_items = (const Item *)(p->dev + o_first);
-    p->sym_items = (const Item *)(p->dev + o_sym);
-    p->next_items = (const Item *)(p->dev + o_next);
+    for (int k = 0; k < 2; ++k) {
+        Side &s = p->side[k];
+        s.mats = (const Mat *)(p->dev + o[k][0]);
+        s.first_items = (const Item *)(p->dev + o[k][1]);
+        s.gram.tiles = (const MatTile *)(p->dev + o[k][2]);
+        s.poly.tiles = (const MatTile *)(p->dev + o[k][3]);
+        s.next.tiles = (const MatTile *)(p->dev + o[k][4]);
+    }
     *out = p.release();
     return ONEBIT_OK;
 }
@@ -1210,25 +1439,29 @@ int check_coefficients(Coefficients &k, int steps)
     return ONEBIT_OK;
 }
 
-template <bool PAIRS, int BT, int WR, int WC, int KG, class O>
-void products(const onebit_matrices_s *p, Areas w, const O &out, int scale_mode, int steps,
-              const Coefficients &co, hipStream_t st)
+template <bool PAIRS, int STEP, class O>
+void launch(const Mat *mats, const Product &p, const Areas &w, const Coefficients &co, float faded, const O &out,
+            int scale_mode, hipStream_t st)
 {
-    constexpr int kThreads = KG * BT * BT / (16 * WR * WC);
-    float faded = 1.f;
-    for (int k = 0; k < steps; ++k, faded *= co.fade) {
-        k_product<PAIRS, kGram, BT, WR, WC, KG, kThreads, NoOut><<<p->sym_blocks, kThreads, 0, st>>>(
-            p->mats, p->sym_items, w, co, faded, NoOut{}, 0);
-        k_product<PAIRS, kPoly, BT, WR, WC, KG, kThreads, NoOut><<<p->sym_blocks, kThreads, 0, st>>>(
-            p->mats, p->sym_items, w, co, faded, NoOut{}, 0);
-        if (k + 1 < steps)
-            k_product<PAIRS, kNext, BT, WR, WC, KG, kThreads, NoOut><<<p->next_blocks, kThreads, 0, st>>>(
-                p->mats, p->next_items, w, co, faded, NoOut{}, 0);
-        else
-            k_product<PAIRS, kLast, BT, WR, WC, KG, kThreads, O><<<p->next_blocks, kThreads, 0, st>>>(
-                p->mats, p->next_items, w, co, faded, out, scale_mode);
-        std::swap(w.x, w.x_next);
-    }
+    auto run = [&](auto side, auto wr, auto wc, auto groups) {
+        constexpr int BT = decltype(side)::value, WR = decltype(wr)::value, WC = decltype(wc)::value;
+        constexpr int KG = decltype(groups)::value, kThreads = KG * BT * BT / (16 * WR * WC);
+        k_product<PAIRS, STEP, BT, WR, WC, KG, kThreads, O><<<p.blocks, kThreads, 0, st>>>(
+            mats, p.tiles, w, co, faded, out, scale_mode);
+    };
+    using std::integral_constant;
+    if (p.side == 256)
+        run(integral_constant<int, 256>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{},
+            integral_constant<int, 1>{});
+    else if (p.side == 128)
+        run(integral_constant<int, 128>{}, integral_constant<int, 2>{}, integral_constant<int, 2>{},
+            integral_constant<int, 1>{});
+    else if (p.groups == 4)
+        run(integral_constant<int, 64>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{},
+            integral_constant<int, 4>{});
+    else
+        run(integral_constant<int, 64>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{},
+            integral_constant<int, 2>{});
 }
 
 // Everything after the arguments' checks: `src` is what is orthogonalised.
@@ -1236,20 +1469,24 @@ template <bool PAIRS, class S, class O>
 int run(const onebit_matrices_s *p, const S &src, const O &out, int scale_mode, int steps,
         const Coefficients &co, float eps, void *workspace, hipStream_t st)
 {
+    const Side &side = p->side[PAIRS ? ONEBIT_PRODUCTS_F32 : ONEBIT_PRODUCTS_F16];
     const WorkspaceLayout l = layout_of(p, PAIRS);
     char *ws = (char *)workspace;
     Areas w{(_Float16 *)(ws + l.x0), (_Float16 *)(ws + l.x1), (_Float16 *)(ws + l.x_lo),
             (_Float16 *)(ws + l.d), (_Float16 *)(ws + l.b),
             (double *)(ws + l.norm), (float *)(ws + l.part), (float *)(ws + l.t),
-            (float *)(ws + l.gamma)};
-    k_norm<S><<<(int)p->norms, 256, 0, st>>>(p->mats, p->norm_items, p->norm_size, src, w.norm);
-    k_first<PAIRS, S><<<(int)p->firsts, 256, 0, st>>>(p->mats, p->first_items, src, (double)eps, w);
-    if (p->tile == 256)
-        products<PAIRS, 256, 4, 2, 1>(p, w, out, scale_mode, steps, co, st);
-    else if (p->tile == 128)
-        products<PAIRS, 128, 2, 2, 1>(p, w, out, scale_mode, steps, co, st);
-    else
-        products<PAIRS, 64, 1, 2, 4>(p, w, out, scale_mode, steps, co, st);
+            (float *)(ws + l.gamma), (uint32_t *)(ws + l.counter), (float *)(ws + l.sums)};
+    k_norm<S><<<(int)p->norms, 256, 0, st>>>(side.mats, p->norm_items, p->norm_size, src, w.norm);
+    k_first<PAIRS, S><<<(int)side.firsts, 256, 0, st>>>(side.mats, side.first_items, src,
+                                                        (double)eps, w);
+    float faded = 1.f;
+    for (int k = 0; k < steps; ++k, faded *= co.fade) {
+        launch<PAIRS, kGram>(side.mats, side.gram, w, co, faded, NoOut{}, 0, st);
+        launch<PAIRS, kPoly>(side.mats, side.poly, w, co, faded, NoOut{}, 0, st);
+        if (k + 1 < steps) launch<PAIRS, kNext>(side.mats, side.next, w, co, faded, NoOut{}, 0, st);
+        else launch<PAIRS, kLast>(side.mats, side.next, w, co, faded, out, scale_mode, st);
+        std::swap(w.x, w.x_next);
+    }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? ONEBIT_OK : hip_fail(e, "matrix kernel launch");
 }
@@ -1264,7 +1501,7 @@ int check_common(const onebit_matrices_s *p, int32_t products, int32_t steps,
     co = coefficients ? Coefficients{coefficients[0], coefficients[1], coefficients[2], 1.f}
                       : Coefficients{3.4445f, -4.7750f, 2.0315f, 1.f};
     TRY(check_coefficients(co, steps));
-    if (!workspace && p->ex > 0) return fail(ONEBIT_EINVAL, "workspace is NULL");
+    if (!workspace && !p->empty) return fail(ONEBIT_EINVAL, "workspace is NULL");
     if ((uintptr_t)workspace % 256) return fail(ONEBIT_EALIGN, "workspace is not 256-byte aligned");
     return ONEBIT_OK;
 }
@@ -1329,7 +1566,7 @@ int onebit_orthogonalize(onebit_matrices mats, const void *in, int32_t in_dtype,
         return fail(ONEBIT_EINVAL, "in place, but in and out have different types");
     Coefficients co;
     TRY(check_common(mats, products, steps, coefficients, eps, workspace, co));
-    if (mats->ex == 0) return ONEBIT_OK;
+    if (mats->empty) return ONEBIT_OK;
     return with_type(in_dtype, [&](auto *i) {
         using I = std::remove_pointer_t<decltype(i)>;
         return with_type(out_dtype, [&](auto *o) {
@@ -1361,7 +1598,7 @@ int onebit_muon_step(onebit_matrices mats, float *x, float *m, const void *grads
         return fail(ONEBIT_EINVAL, "scale %d is not one of ONEBIT_MUON_SCALE_*", scale);
     Coefficients co;
     TRY(check_common(mats, products, steps, coefficients, eps, workspace, co));
-    if (mats->ex == 0) return ONEBIT_OK;
+    if (mats->empty) return ONEBIT_OK;
     return with_type(grad_dtype, [&](auto *g) {
         using G = std::remove_pointer_t<decltype(g)>;
         // From three gradient rows on, reading them again costs more than the update's
