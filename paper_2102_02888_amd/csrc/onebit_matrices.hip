@@ -879,7 +879,9 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
                     take(row_in_block(k), v);
                     __builtin_memcpy(at(it.part, k), v, sizeof v);
                 }
-                __threadfence();
+                // One thread's release and acquire stand for the workgroup's: the barriers
+                // order the others' accesses with it.  (A fence writes the whole L2 back:
+                // one in every wave took 86 us where the products take 30.)
                 __syncthreads();
                 if (threadIdx.x == 0) {
                     const uint32_t before = __hip_atomic_fetch_add(
@@ -891,7 +893,6 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
                 }
                 __syncthreads();
                 if (scratch[0] == 0.f) return;
-                __threadfence();
 #pragma unroll
                 for (int k = 0; k < kRounds; ++k) {
                     float v[8] = {};
@@ -1097,20 +1098,22 @@ std::vector<MatTile> deal(std::vector<Costed> &all)
 }
 
 // The kernels' shapes, and what a tile of each costs: us for a tile and for each of
-// its slabs, for pairs and for halves, on a CU that has as many of them as fit
-// (measured from lists of 1 to 96 matrices, 17 x 4,000 to 4,096 x 4,096).
+// its slabs, for pairs and for halves, on a CU that has as many of them as fit;
+// and for each slab of a tile that has its CU to itself.  (Fitted to lists of 1 to
+// 96 matrices, 17 x 4,000 to 4,096 x 4,096.)
 struct Shape {
     int side, groups;
-    double tile[2], slab[2];
+    double tile[2], slab[2], alone[2];
 };
 constexpr Shape kShapes[] = {
-    {64, 4, {4.0, 4.0}, {0.26, 0.23}},
-    {64, 2, {2.5, 2.5}, {0.24, 0.21}},
-    {128, 1, {3.0, 3.0}, {0.72, 0.65}},
-    {256, 1, {10.0, 10.0}, {2.7, 2.25}},
+    {64, 4, {4.5, 4.5}, {0.26, 0.25}, {0.26, 0.25}},
+    {64, 2, {2.5, 2.5}, {0.21, 0.21}, {0.37, 0.39}},
+    {128, 1, {7.0, 5.0}, {0.64, 0.60}, {0.64, 0.60}},
+    {256, 1, {10.0, 12.0}, {2.65, 2.30}, {2.65, 2.30}},
 };
 constexpr int kCus = 256;
-constexpr int kPartSlabs = 16;  // least slabs of a part
+constexpr int kPartSlabs = 16;    // least slabs of a part
+constexpr double kPartCost = 6.0;  // us that a part's join adds
 
 struct Sizes {
     int64_t m, n;
@@ -1125,12 +1128,30 @@ int64_t tiles_of(const Sizes &z, const Shape &h, int pad, bool symmetric)
     return !symmetric ? tm * tn : h.groups > 1 ? tm * tm : tm * (tm + 1) / 2;
 }
 
-// Parts of the summed index of a Gram tile: as many as leave every CU one workgroup.
-int parts_of(const Sizes &z, const Shape &h, int pad, int64_t all_tiles, int kind)
+// Slabs of a part of a Gram tile's sum: the fewest, and at least kPartSlabs, with
+// which the workgroups are no more than the CUs, or than a quarter above the tiles.
+int64_t part_slabs(const std::vector<Sizes> &all, const Shape &h, int pad, int kind)
 {
-    const int64_t slabs = pad_to(z.n, pad) * kind / kSlab;
-    return h.groups < 4 ? 1 : (int)std::max<int64_t>(1, std::min(kCus / std::max<int64_t>(all_tiles, 1),
-                                                                 slabs / kPartSlabs));
+    constexpr int64_t kWhole = (int64_t)1 << 40;
+    if (h.groups < 4) return kWhole;
+    int64_t tiles = 0, longest = 0;
+    for (const Sizes &z : all) {
+        tiles += tiles_of(z, h, pad, true);
+        longest = std::max(longest, pad_to(z.n, pad) * kind / kSlab);
+    }
+    const int64_t most = std::max<int64_t>(kCus, tiles + tiles / 4);
+    for (int64_t slabs = kPartSlabs; slabs < longest; slabs += slabs / 4) {
+        int64_t parts = 0;
+        for (const Sizes &z : all)
+            parts += tiles_of(z, h, pad, true) * ((pad_to(z.n, pad) * kind / kSlab + slabs - 1) / slabs);
+        if (parts <= most) return slabs;
+    }
+    return kWhole;
+}
+
+int parts_of(const Sizes &z, int pad, int kind, int64_t part)
+{
+    return (int)((pad_to(z.n, pad) * kind / kSlab + part - 1) / part);
 }
 
 // Estimated us of a launch: every tile goes to the CU that is free first, the dearest
@@ -1139,28 +1160,30 @@ enum Which { kIsGram, kIsPoly, kIsNext };
 double launch_cost(const std::vector<Sizes> &all, const Shape &h, int pad, Which which, int kind)
 {
     const int p = kind == 2 ? 0 : 1;
-    int64_t tiles = 0;
-    for (const Sizes &z : all) tiles += tiles_of(z, h, pad, which != kIsNext);
+    const int64_t part = which == kIsGram ? part_slabs(all, h, pad, kind) : 0;
     std::vector<std::pair<double, int64_t>> work;  // cost, how many
-    double total = 0, dearest = 0;
+    double total = 0, dearest = 0, longest = 0;
     for (const Sizes &z : all) {
         int64_t count = tiles_of(z, h, pad, which != kIsNext);
         double slabs = (double)(pad_to(which == kIsGram ? z.n : z.m, pad) * kind / kSlab);
+        double join = 0;
         if (which == kIsGram) {
-            const int parts = parts_of(z, h, pad, tiles, kind);
+            const int parts = parts_of(z, pad, kind, part);
             count *= parts;
-            slabs = slabs / parts + (parts > 1 ? 8 : 0);  // and the wait for the others
+            slabs /= parts;
+            join = parts > 1 ? kPartCost : 0;
         }
-        const double cost = h.tile[p] + h.slab[p] * slabs;
+        const double cost = h.tile[p] + h.slab[p] * slabs + join;
+        longest = std::max(longest, h.tile[p] + h.alone[p] * slabs + join);
         work.push_back({cost, count});
         total += cost * (double)count;
         dearest = std::max(dearest, cost);
     }
-    if (total > 64.0 * kCus * dearest) return total / kCus + dearest / 2;
+    if (total > 64.0 * kCus * dearest) return std::max(total / kCus + dearest / 2, longest);
     std::sort(work.rbegin(), work.rend());
     std::vector<double> cus(kCus, 0.0);  // a heap, the earliest on top
     auto later = [](double a, double b) { return a > b; };
-    double last = 0;
+    double last = longest;
     for (const auto &[cost, count] : work)
         for (int64_t k = 0; k < count; ++k) {
             std::pop_heap(cus.begin(), cus.end(), later);
@@ -1217,8 +1240,7 @@ int build_side(std::vector<Mat> mats, int kind, Side &side, Built &out)
     Shape shape[3];
     choose(sizes, kind, shape);
     const int pad = shape[kIsNext].side, p = kind == 2 ? 0 : 1;
-    int64_t gram_tiles = 0;
-    for (const Sizes &z : sizes) gram_tiles += tiles_of(z, shape[kIsGram], pad, true);
+    const int64_t part = part_slabs(sizes, shape[kIsGram], pad, kind);
     std::vector<Costed> lists[3];
     int64_t tiles = 0;
     for (size_t k = 0; k < mats.size(); ++k) {
@@ -1235,7 +1257,7 @@ int build_side(std::vector<Mat> mats, int kind, Side &side, Built &out)
         m.part_count = (int32_t)tiles_of(z, shape[kIsNext], pad, false);
         side.parts += m.part_count;
         m.slot_first = (int32_t)side.slots;
-        const int parts = m.parts = parts_of(z, shape[kIsGram], pad, gram_tiles, kind);
+        const int parts = m.parts = parts_of(z, pad, kind, part);
         m.sums = side.sums;
         if (parts > 1) m.slot_count = (int32_t)tiles_of(z, shape[kIsGram], pad, true);
         side.slots += m.slot_count;
