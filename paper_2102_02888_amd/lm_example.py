@@ -1,0 +1,100 @@
+"""A small language model trained with both optimizers of this package:
+
+    python -m paper_2102_02888_amd.lm_example [steps]
+
+The token table (tied to the output) and a bias belong to OnebitAdam, in one
+flat buffer; the hidden matrices belong to Muon, in another.  n simulated
+workers see batches of their own.  A worker's table gradient is the output
+product's, to which onebit_embedding_grad adds the lookup's, both in the
+worker's row of OnebitAdam's gradients; the matrices' gradients go to Muon's
+rows.  The tokens are synthetic: each is followed by one of four others.
+"""
+import sys
+
+import torch
+import torch.nn.functional as F
+
+from .embedding import embedding_workspace, onebit_embedding_forward, onebit_embedding_grad
+from .muon import Matrices, Muon
+from .onebit import Plan
+from .optimizer import OnebitAdam
+
+
+class Model:
+    """Residual two-matrix layers between a tied embedding and its output."""
+
+    def __init__(self, device, vocab=1000, width=128, layers=2, n_workers=4, tokens=512, seed=0):
+        gen = torch.Generator(device=device).manual_seed(seed)
+        self.vocab, self.width, self.tokens, self.n = vocab, width, tokens, n_workers
+        self.plan = Plan([vocab * width, vocab], n_workers)
+        self.adam = OnebitAdam(self.plan, device, lr=3e-3, warmup_steps=40)
+        self.mats = Matrices([s for _ in range(layers) for s in ((width, 4 * width),
+                                                                 (4 * width, width))])
+        self.muon = Muon(self.mats, device, lr=0.02, n_workers=n_workers)
+        self.table = self._table(self.adam.x)
+        self.table.normal_(0.0, 0.05, generator=gen)
+        self.matrices = [self.mats.view(self.muon.x, k) for k in range(2 * layers)]
+        for m in self.matrices:
+            m.normal_(0.0, m.shape[0] ** -0.5, generator=gen)
+        self.workspace = embedding_workspace(tokens, vocab, width, device)
+        self.scale = width ** 0.5
+        self.next = torch.randint(vocab, (vocab, 4), device=device, generator=gen)
+        self.gen = gen
+
+    def _table(self, flat):
+        return flat[:self.vocab * self.width].view(self.vocab, self.width)
+
+    def _bias(self, flat):
+        at = int(self.plan.tensor_off[1])
+        return flat[at:at + self.vocab]
+
+    def batch(self):
+        """Tokens and what follows each of them."""
+        ids = torch.randint(self.vocab, (self.tokens,), device=self.table.device,
+                            generator=self.gen)
+        pick = torch.randint(4, (self.tokens, 1), device=ids.device, generator=self.gen)
+        return ids, self.next[ids].gather(1, pick)[:, 0]
+
+    def worker(self, i):
+        """Worker i's loss on a batch of its own, and its gradients."""
+        ids, target = self.batch()
+        hidden = torch.empty(self.tokens, self.width, device=ids.device)
+        onebit_embedding_forward(self.table, ids, hidden, scale=self.scale)
+        hidden.requires_grad_()
+        table, bias, *mats = (t.detach().requires_grad_() for t in
+                              (self.table, self._bias(self.adam.x), *self.matrices))
+        h = hidden
+        for a, b in zip(mats[::2], mats[1::2]):
+            h = h + F.relu(h @ a) @ b
+        h = h * torch.rsqrt(h.square().mean(1, keepdim=True) + 1e-6)
+        loss = F.cross_entropy(h @ table.t() + bias, target)
+        d_hidden, d_table, d_bias, *d_mats = torch.autograd.grad(loss, [hidden, table, bias, *mats])
+        row = self.adam.grads[i]
+        self._table(row).copy_(d_table)
+        onebit_embedding_grad(d_hidden, ids, self._table(row), self.workspace, scale=self.scale,
+                              accumulate=True)
+        self._bias(row).copy_(d_bias)
+        for k, d in enumerate(d_mats):
+            self.mats.view(self.muon.grads[i], k).copy_(d)
+        return loss.detach()
+
+    def step(self):
+        """One step of both optimizers; returns the workers' mean loss."""
+        loss = torch.stack([self.worker(i) for i in range(self.n)]).mean()
+        self.adam.step()
+        self.muon.step()
+        return loss
+
+
+def main(steps=200):
+    model = Model(torch.device("cuda", torch.cuda.current_device()))
+    for step in range(1, steps + 1):
+        loss = model.step()
+        if step == 1 or step % 20 == 0:
+            print("step %4d  loss %.4f  (%s)" % (step, float(loss), "warm-up"
+                                                 if model.adam.in_warmup else "compressed"))
+    return float(loss)
+
+
+if __name__ == "__main__":
+    main(int(sys.argv[1]) if len(sys.argv) > 1 else 200)

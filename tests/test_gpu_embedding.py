@@ -247,3 +247,43 @@ def test_refusals(dev):
                         ((p, 0, 8, 10, 8, ids.data_ptr() + 4, 8, 5, 1.0, p, 0, 8, None), -2),
                         ((None, 0, 8, 10, 8, ids.data_ptr(), 8, 5, 1.0, p, 0, 8, None), -1)):
         assert L.onebit_embedding_forward(*bad) == status
+
+
+def test_tables_past_32_bits(dev):
+    """A table of 70,000 rows of 32,768 (2^31 and more elements): its last rows
+    are read, written and zeroed at their places."""
+    import paper_2102_02888_amd as ob
+    vocab, width = 70000, 32768
+    table = torch.zeros(vocab, width, dtype=torch.bfloat16, device=dev)
+    last = torch.randn(16, width, device=dev, generator=_gen(dev, 1)).bfloat16()
+    table[-16:] = last
+    ids = torch.arange(vocab - 16, vocab, device=dev)
+    out = torch.empty(16, width, dtype=torch.bfloat16, device=dev)
+    ob.onebit_embedding_forward(table, ids, out)
+    assert torch.equal(out, last)
+    table.fill_(3.0)
+    work = ob.embedding_workspace(16, vocab, width, dev)
+    ob.onebit_embedding_grad(out, ids, table, work, scale=2.0)
+    assert torch.equal(table[-16:], (last.float() * 2).bfloat16())
+    assert not bool(table[:-16].any())
+    many = ids.repeat(300)  # 4,800 places: the long lists' kernels
+    dout = out.repeat(300, 1)
+    work = ob.embedding_workspace(4800, vocab, width, dev)
+    table.fill_(3.0)
+    ob.onebit_embedding_grad(dout, many, table, work)
+    assert torch.equal(table[-16:], (last.float() * 300).bfloat16())
+    assert not bool(table[:-16].any())
+
+
+@pytest.mark.parametrize("tokens", [100, 4096, 9000])
+@pytest.mark.parametrize("vocab", [40, 262144, 262145, 300001])
+def test_gradient_of_many_rows(dev, tokens, vocab):
+    """Both sides of the sorting workgroup's rows and places; rows of 2 bytes."""
+    import paper_2102_02888_amd as ob
+    ids = torch.randint(-1, vocab + 1, (tokens,), device=dev, generator=_gen(dev, 1))
+    dout = torch.ones(tokens, 1, device=dev, dtype=torch.bfloat16)
+    grad = torch.full((vocab, 1), 5.0, device=dev, dtype=torch.float16)
+    ob.onebit_embedding_grad(dout, ids, grad, ob.embedding_workspace(tokens, vocab, 1, dev))
+    on = (ids >= 0) & (ids < vocab)
+    want = torch.bincount(ids[on], minlength=vocab).to(torch.float16)
+    assert torch.equal(grad[:, 0], want)

@@ -298,3 +298,83 @@ def test_refusals(dev):
     mats.close()
     with pytest.raises(ValueError, match="closed"):
         ob.onebit_orthogonalize(mats, g, o, w)
+
+
+@pytest.mark.parametrize("shapes", [
+    [(17, 9000)],                                  # one tile row, the Gram sum in many parts
+    [(5, 4000), (64, 2100), (130, 2000)] * 2,      # parts of several tiles
+    [(700, 900), (900, 650)] * 8,                  # tiles of 128
+    [(1025, 1100)] * 30 + [(1500, 520)] * 30,      # tiles of 256
+    [(90, 200)] * 300,                             # tiles of 64 by two groups of waves
+])
+def test_every_kernel_shape(dev, shapes):
+    """Lists that take each of the products' kernels, twice on one workspace
+    (the parts' counters are left as a call finds them); some matrices against
+    the formula."""
+    import paper_2102_02888_amd as ob
+    mats = ob.Matrices(shapes)
+    grad, res = torch.empty(mats.extent, device=dev), torch.zeros(mats.extent, device=dev)
+    grad.normal_(0, 1e-3, generator=_gen(dev, 1))
+    for prod, tol in ((ob.PRODUCTS_F32, 1e-5), (ob.PRODUCTS_F16, 3e-3)):
+        work = mats.workspace(dev, prod)
+        work.fill_(255)
+        ob.onebit_orthogonalize(mats, grad, res, work, products=prod)
+        first = res.clone()
+        for _ in range(3):
+            ob.onebit_orthogonalize(mats, grad, res, work, products=prod)
+            assert torch.equal(first, res)  # bit for bit, whichever part ends last
+        for k in sorted({0, 1 % len(shapes), len(shapes) // 2, len(shapes) - 1}):
+            assert _rel(mats.view(res, k), _ortho64(mats.view(grad, k))) < tol, (k, shapes[k])
+    mats.close()
+
+
+def test_parts_in_a_graph(dev):
+    import paper_2102_02888_amd as ob
+    mats = ob.Matrices([(17, 6000), (40, 3000)])
+    grad = torch.empty(mats.extent, device=dev)
+    res, want = torch.zeros_like(grad), torch.zeros_like(grad)
+    work = mats.workspace(dev)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ob.onebit_orthogonalize(mats, grad, res, work)
+    for seed in range(4):
+        grad.normal_(0, 1e-3, generator=_gen(dev, seed))
+        ob.onebit_orthogonalize(mats, grad, want, work)
+        torch.cuda.synchronize()
+        graph.replay()
+        assert torch.equal(res, want), seed
+    mats.close()
+
+
+def test_offsets_past_32_bits(dev):
+    """A matrix that begins beyond 2^31 elements and 2^32 bytes of its buffers."""
+    import paper_2102_02888_amd as ob
+    at = (1 << 31) + 192
+    mats = ob.Matrices([(70, 100), (100, 70)], offsets=[at, 5])
+    grad = torch.zeros(mats.extent, dtype=torch.bfloat16, device=dev)
+    res = torch.zeros(mats.extent, dtype=torch.bfloat16, device=dev)
+    for k in range(2):
+        mats.view(grad, k).copy_(_values(dev, *mats.shapes[k], "noise", k))
+    ob.onebit_orthogonalize(mats, grad, res, mats.workspace(dev, ob.PRODUCTS_F16))
+    for k in range(2):
+        assert _rel(mats.view(res, k), _ortho64(mats.view(grad, k))) < 3e-3 + ROUND["bf16"]
+    assert not bool(res[5 + 7000:at].any())
+    mats.close()
+
+
+def test_creation_refusals(dev):
+    import paper_2102_02888_amd as ob
+    for bad, text in ((dict(shapes=[(3, -1)]), "side"), (dict(shapes=[(1 << 21, 1)]), "side"),
+                      (dict(shapes=[(1 << 16, 1 << 16)]), "2\\^31"),
+                      (dict(shapes=[(4, 5)], lds=[4]), "ld"),
+                      (dict(shapes=[(4, 5)], offsets=[-1]), "offset"),
+                      (dict(shapes=[(4, 5)], offsets=[1 << 41]), "offset"),
+                      (dict(shapes=[(1 << 20, 1)], lds=[1 << 40]), "ends above")):
+        with pytest.raises(ob.OnebitError, match=text):
+            ob.Matrices(**bad)
+    with pytest.raises(ValueError, match="one entry per matrix"):
+        ob.Matrices([(4, 5)], offsets=[0, 1])
+    mats = ob.Matrices([(0, 4), (7, 0)])  # nothing to do, nothing needed
+    x = torch.zeros(0, device=dev)
+    ob.onebit_orthogonalize(mats, x, x, mats.workspace(dev))
+    mats.close()
