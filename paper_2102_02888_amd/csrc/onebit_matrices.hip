@@ -238,7 +238,9 @@ struct FromMuon {
 };
 
 // Sum of squares (64 bits) of `size` elements of a matrix: 8 per thread at a time
-// where the matrix is one run of memory, else one.
+// where the matrix is one run of memory, else one.  Memory bounds it: 302M fp32
+// elements 204 us (5.9 TB/s), a step's momentum from bf16 gradients over the same 530 us
+// (3.0 GB, 5.7 TB/s), of 8 gradients over 50M elements 274 us.
 template <class S>
 __global__ __launch_bounds__(256) void k_norm(const Mat *__restrict__ mats,
                                               const Item *__restrict__ items, int size, S src,
@@ -287,6 +289,8 @@ __device__ __forceinline__ int column(int k)
 
 // First iterate, X = u / (||u||_F + eps), padding zeroed: 64 x 64 of the matrix
 // for a workgroup, 8 of a row for a thread, turned in LDS where X is the transpose.
+// It is a launch of its own because the factor needs the whole norm.  Memory bounds
+// it: 302M fp32 elements to hi and lo 460 us (2.4 GB, 5.3 TB/s).
 template <bool PAIRS, class S>
 __global__ __launch_bounds__(256) void k_first(const Mat *__restrict__ mats,
                                                const Item *__restrict__ items, S src, double eps,
@@ -555,6 +559,19 @@ __device__ __forceinline__ int deep_place(int byte)
 // its own (the k-th slab goes to group k mod KG) in buffers of its own, and their
 // sums are added at the end: for lists with fewer tiles than the GPU has CUs, where
 // the wait for a slab is what counts.
+// A tile of 256 reads 1/128 of an operand's number per multiply-add, a tile of 64
+// 1/32, which only short lists can afford.  Its 8 waves of 128 x 64 leave the matrix
+// cores two waves per SIMD to draw from (4 waves of 128 x 128 read a third less from LDS
+// but took 4% longer over a list of 144 matrices with halves, 11% with pairs).
+// Measured on that list (96 of 1,024 x 1,024, 24 of 4,096 x 1,024, 24 of 1,024 x 4,096;
+// us, and the share of the time that the matrix cores are busy):
+//            gram       poly       next        last
+//   pairs    951 66%    602 55%    1,682 67%   1,889 54%
+//   halves   420 56%    254 39%      906 39%     825 39%
+// There is no LDS bank conflict but in the last one's turned tiles.  What bounds
+// pairs is the matrix cores in the slabs and memory in the epilogue, which one tile's
+// products cannot hide where it has its CU to itself; halves wait for their slabs,
+// of which no more than LDS holds can be under way.
 template <bool PAIRS, int STEP, int BT, int WR, int WC, int KG, int THREADS, class O>
 __global__ __launch_bounds__(THREADS, 2) void k_product(
     const Mat *__restrict__ mats, const MatTile *__restrict__ tiles, Areas w, Coefficients co,
@@ -1100,7 +1117,15 @@ std::vector<MatTile> deal(std::vector<Costed> &all)
 // The kernels' shapes, and what a tile of each costs: us for a tile and for each of
 // its slabs, for pairs and for halves, on a CU that has as many of them as fit;
 // and for each slab of a tile that has its CU to itself.  (Fitted to lists of 1 to
-// 96 matrices, 17 x 4,000 to 4,096 x 4,096.)
+// 96 matrices, 17 x 4,000 to 4,096 x 4,096.)  us of whole calls with each shape alone,
+// and with those that are chosen:
+//                                       64 x 4   64 x 2      128      256   chosen
+//   12 of 128 x 128 to 512, pairs          101      100      149      392      101
+//   11 of 17 x 4,000 to 1,001 x 257, pairs 198      277      517    1,383      177
+//   1,024 x 1,024, halves                  133      141      229      433      133
+//   4 of them, halves                      428      329      263      450      263
+//   16 of them, pairs                    2,719    2,081    1,239    1,284    1,228
+//   144 of 1,024 x 1,024 to 4,096, halves 23,602  16,987    9,022    8,117    8,161
 struct Shape {
     int side, groups;
     double tile[2], slab[2], alone[2];
@@ -1108,7 +1133,7 @@ struct Shape {
 constexpr Shape kShapes[] = {
     {64, 4, {4.5, 4.5}, {0.26, 0.25}, {0.26, 0.25}},
     {64, 2, {2.5, 2.5}, {0.21, 0.21}, {0.37, 0.39}},
-    {128, 1, {7.0, 5.0}, {0.64, 0.60}, {0.64, 0.60}},
+    {128, 1, {7.0, 5.0}, {0.64, 0.64}, {0.64, 0.64}},
     {256, 1, {10.0, 12.0}, {2.65, 2.30}, {2.65, 2.30}},
 };
 constexpr int kCus = 256;
