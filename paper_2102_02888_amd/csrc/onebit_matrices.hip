@@ -498,13 +498,14 @@ struct RowStager {
 };
 
 // Stages a slab of an operand with the summed index along its rows: kSlab / kind
-// rows of BT numbers (pairs: of BT hi and BT lo).
-template <bool PAIRS, int BT, int WAVES>
+// rows of BT numbers (pairs: of BT hi and BT lo); or one of its PARTS parts.
+template <bool PAIRS, int BT, int WAVES, int PARTS>
 struct DeepStager {
-    static constexpr int kEach = BT / 8 / WAVES, kBytes = BT * (PAIRS ? 4 : 2);
+    static constexpr int kEach = BT / 8 / WAVES / PARTS, kBytes = BT * (PAIRS ? 4 : 2);
     static constexpr int kRows = 1024 / kBytes;  // of an instruction
-    static constexpr int kKinds = kRows < 4 ? 4 / kRows : 1;  // permutations of an instruction
-    static_assert(kEach % kKinds == 0, "rows of an instruction");
+    // permutations of a wave's instructions
+    static constexpr int kKinds = kRows >= 4 ? 1 : kEach < 4 / kRows ? kEach : 4 / kRows;
+    static_assert(kEach % kKinds == 0 && (kEach % 4 == 0 || kEach == kKinds), "rows of an instruction");
     const char *base;
     int pitch, wave, lane_at[kKinds];
     __device__ __forceinline__ DeepStager(const _Float16 *src, int64_t row_numbers, int wave_)
@@ -513,12 +514,13 @@ struct DeepStager {
         const int at = (threadIdx.x & 63) * 16, r = at / kBytes, p = at % kBytes / 16;
 #pragma unroll
         for (int k = 0; k < kKinds; ++k)
-            lane_at[k] = r * pitch + (((p >> 1) ^ deep_swizzle<kBytes>(k * kRows + r)) * 2 + (p & 1)) * 16;
+            lane_at[k] = r * pitch +
+                (((p >> 1) ^ deep_swizzle<kBytes>((wave * kEach + k) * kRows + r)) * 2 + (p & 1)) * 16;
     }
-    __device__ __forceinline__ void operator()(int slab, char *lds) const
+    __device__ __forceinline__ void operator()(int part, char *lds) const
     {
-        constexpr int kSlabRows = kSlab / (PAIRS ? 2 : 1);
-        const char *from = base + (int64_t)slab * kSlabRows * pitch;
+        constexpr int kPartRows = kSlab / (PAIRS ? 2 : 1) / PARTS;
+        const char *from = base + (int64_t)part * kPartRows * pitch;
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
             const int block = wave * kEach + k;
@@ -570,8 +572,8 @@ __device__ __forceinline__ int deep_place(int byte)
 //   halves   420 56%    254 39%      906 39%     825 39%
 // There is no LDS bank conflict but in the last one's turned tiles.  What bounds
 // pairs is the matrix cores in the slabs and memory in the epilogue, which one tile's
-// products cannot hide where it has its CU to itself; halves wait for their slabs,
-// of which no more than LDS holds can be under way.
+// products cannot hide where it has its CU to itself; for halves, with a third of the
+// products, the epilogue counts for more.
 template <bool PAIRS, int STEP, int BT, int WR, int WC, int KG, int THREADS, class O>
 __global__ __launch_bounds__(THREADS, 2) void k_product(
     const Mat *__restrict__ mats, const MatTile *__restrict__ tiles, Areas w, Coefficients co,
@@ -581,8 +583,12 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     static_assert(THREADS == KG * kWaves * 64, "a wave for every part of the tile");
     constexpr int kOperand = BT * kRowBytes;
     constexpr bool kDeep = STEP == kNext || STEP == kLast;
-    __shared__ __attribute__((aligned(1024))) char buffer0[KG * 2 * kOperand],
-        buffer1[KG * 2 * kOperand];
+    // Tiles of 256 of B X: X in buffers of its own, for half slabs.
+    constexpr bool kSplit = kDeep && BT == 256;
+    constexpr int kBuffer = (kSplit ? 1 : KG * 2) * kOperand, kHalfBuffer = kSplit ? kOperand / 2 : 16;
+    __shared__ __attribute__((aligned(1024))) char buffer0[kBuffer], buffer1[kBuffer];
+    __shared__ __attribute__((aligned(1024))) char x00[kHalfBuffer], x01[kHalfBuffer],
+        x10[kHalfBuffer], x11[kHalfBuffer];
     __shared__ float scratch[KG * kWaves];
     const MatTile it = tiles[(blockIdx.x % kXcds) * (gridDim.x / kXcds) + blockIdx.x / kXcds];
     if (it.mat < 0) return;
@@ -608,8 +614,8 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
 
     f32x16 acc[WR][WC] = {};
     const RowStager<BT, kWaves> stage_a(pa, pitch, wave);
-    const std::conditional_t<kDeep, DeepStager<PAIRS, BT, kWaves>, RowStager<BT, kWaves>> stage_b(
-        pb, kDeep ? x_pitch : pitch, wave);
+    const std::conditional_t<kDeep, DeepStager<PAIRS, BT, kWaves, kSplit ? 2 : 1>,
+                             RowStager<BT, kWaves>> stage_b(pb, kDeep ? x_pitch : pitch, wave);
     auto stage = [&](int s, char *to) {
         stage_a(slab0 + s, to);
         stage_b(slab0 + s, to + kOperand);
@@ -626,26 +632,30 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     for (int c = 0; c < 4; ++c) {
         place_a[c] = row_chunk(wr + row, c * 2 + up);
         if (!kDeep) place_b[c] = kOperand + row_chunk(wc + row, c * 2 + up);
-        else place_b[c] = kOperand + deep_place<kDeepBytes>((wc + c / kind * 32) * 2 * kind + c % kind * 64);
+        else place_b[c] = (kSplit ? 0 : kOperand) +
+                          deep_place<kDeepBytes>((wc + c / kind * 32) * 2 * kind + c % kind * 64);
     }
-    auto second = [&](const char *buffer, int k, int q, int lo) {
+    // b: where the second operand's slab begins, or its half with fragment k in it
+    auto second = [&](const char *b, int k, int q, int lo) {
         if (kDeep)
-            return deep_fragment<kDeepBytes>(buffer + place_b[q * kind + lo] + k * 16 * kDeepBytes);
-        return *(const half8 *)(buffer + place_b[k + lo * 2] + q * 32 * kRowBytes);
+            return deep_fragment<kDeepBytes>(b + place_b[q * kind + lo] +
+                                             (kSplit ? k % (kSteps / 2) : k) * 16 * kDeepBytes);
+        return *(const half8 *)(b + place_b[k + lo * 2] + q * 32 * kRowBytes);
     };
-    auto load = [&](const char *buffer, int k, Fragments &f) {
+    auto load_from = [&](const char *buffer, const char *b, int k, Fragments &f) {
 #pragma unroll
         for (int p = 0; p < WR; ++p) f.a[p] = *(const half8 *)(buffer + place_a[k] + p * 32 * kRowBytes);
 #pragma unroll
-        for (int q = 0; q < WC; ++q) f.b[q] = second(buffer, k, q, 0);
+        for (int q = 0; q < WC; ++q) f.b[q] = second(b, k, q, 0);
         if (PAIRS) {
 #pragma unroll
-            for (int q = 0; q < WC; ++q) f.b_lo[q] = second(buffer, k, q, 1);
+            for (int q = 0; q < WC; ++q) f.b_lo[q] = second(b, k, q, 1);
 #pragma unroll
             for (int p = 0; p < WR; ++p)
                 f.a_lo[p] = *(const half8 *)(buffer + place_a[k + 2] + p * 32 * kRowBytes);
         }
     };
+    auto load = [&](const char *buffer, int k, Fragments &f) { load_from(buffer, buffer, k, f); };
     auto multiply = [&](const Fragments &f) {
         auto all = [&](const half8 *fa, const half8 *fb) {
 #pragma unroll
@@ -663,8 +673,25 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     // The first two slabs are under way before anything else is waited for.
     char *const ours[2] = {buffer0 + group * 2 * kOperand, buffer1 + group * 2 * kOperand};
     const int own = (slabs - group + KG - 1) / KG;  // slabs of this group
-    if (own > 0) stage(group, ours[0]);
-    if (own > 1) stage(KG + group, ours[1]);
+    // (split: loads must start in the order in which they are waited for)
+    auto in_order = [] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto stage_x = [&](int part, char *to) {
+        in_order();
+        stage_b(part, to);
+        in_order();
+    };
+    if constexpr (kSplit) {
+        stage_x(0, x00);
+        stage_a(0, buffer0);
+        stage_x(1, x01);
+        stage_x(2, x10);
+    } else {
+        if (own > 0) stage(group, ours[0]);
+        if (own > 1) stage(KG + group, ours[1]);
+    }
 
     // The shift, and the step's coefficients around it.
     auto sum_over = [&](float v) {  // the workgroup's, the same in every thread
@@ -737,8 +764,8 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
         constexpr int kGroup = kReads * 2 <= kProducts ? 2 : 1;
         constexpr int kRest = kProducts - kReads / 2 * kGroup;
         Fragments f[2];
-        auto step = [&](const char *next, int k, int parity) {
-            load(next, k, f[parity ^ 1]);
+        auto step_from = [&](const char *next, const char *b, int k, int parity) {
+            load_from(next, b, k, f[parity ^ 1]);
             multiply(f[parity]);
 #pragma unroll
             for (int g = 0; g < kReads / 2; ++g) {
@@ -748,6 +775,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
             __builtin_amdgcn_sched_group_barrier(0x008, kRest, 0);
             __builtin_amdgcn_sched_barrier(0);
         };
+        auto step = [&](const char *next, int k, int parity) { step_from(next, next, k, parity); };
         auto inner = [&](const char *now, int parity) {  // all of a slab's steps but the last
 #pragma unroll
             for (int k = 0; k < kSteps - 1; ++k) step(now, k + 1, (parity + k) & 1);
@@ -756,24 +784,82 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
         // takes the slab after the next, and the next one, a slab's time under way, is
         // waited for.  The loop begins there, so that nothing is under way where it
         // closes: the compiler would wait for all of it.
-        staged_sync();
-        load(buffer0, 0, f[0]);
-        inner(buffer0, 0);
         constexpr int kLastParity = (kSteps - 1) & 1;
         static_assert(kLastParity == 1, "fragments change places an even number of times a slab");
-        for (int s = 2; s < slabs; s += 2) {
+        if constexpr (kSplit) {
+            // X comes from memory, B from the L2 as a rule: half a slab of X is loaded again
+            // as soon as it has been read, so that its loads have one and a half slab's
+            // time.  Started in turn: the second half and A of a slab when the slab
+            // before it begins, the first half of the slab after in its middle.  (A list of
+            // 144 matrices, one slab's time for all loads and so: halves 8,248 and 8,089 us,
+            // pairs 17,410 and 17,372.)
+            constexpr int kHalfLoads = BT / 16 / kWaves, kLoadsA = BT / 8 / kWaves;
+            static_assert(2 * kHalfLoads + kLoadsA < 16, "the counter's low bits");
+            auto sync = [&](auto left) {  // all loads are there but the last `left`
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_waitcnt(0x0070 | decltype(left)::value);  // and all LDS reads
+                bare_sync();
+            };
+            using std::integral_constant;
+            constexpr integral_constant<int, 2 * kHalfLoads> at_begin{};
+            constexpr integral_constant<int, 2 * kHalfLoads + kLoadsA> at_half{};
+            // a slab's steps but the last, whose fragments of step 0 are there
+            auto first_half = [&](const char *a, const char *x0) {
+#pragma unroll
+                for (int k = 1; k < kSteps / 2; ++k) step_from(a, x0, k, (k - 1) & 1);
+            };
+            auto second_half = [&](const char *a, const char *x1) {
+#pragma unroll
+                for (int k = kSteps / 2; k < kSteps; ++k) step_from(a, x1, k, (k - 1) & 1);
+            };
+            sync(at_begin);
+            stage_a(1, buffer1);
+            stage_x(3, x11);
+            load_from(buffer0, x00, 0, f[0]);
+            for (int s = 0; s + 2 < slabs; s += 2) {
+                first_half(buffer0, x00);
+                sync(at_half);
+                stage_x(2 * s + 4, x00);
+                second_half(buffer0, x01);
+                sync(at_begin);
+                stage_a(s + 2, buffer0);
+                stage_x(2 * s + 5, x01);
+                step_from(buffer1, x10, 0, 1);
+                first_half(buffer1, x10);
+                sync(at_half);
+                stage_x(2 * s + 6, x10);
+                second_half(buffer1, x11);
+                sync(at_begin);
+                stage_a(s + 3, buffer1);
+                stage_x(2 * s + 7, x11);
+                step_from(buffer0, x00, 0, 1);
+            }
+            first_half(buffer0, x00);
+            sync(at_half);
+            second_half(buffer0, x01);
+            sync(integral_constant<int, kHalfLoads>{});
+            step_from(buffer1, x10, 0, 1);
+            first_half(buffer1, x10);
             staged_sync();
-            stage(s, buffer0);
+            second_half(buffer1, x11);
+        } else {
+            staged_sync();
+            load(buffer0, 0, f[0]);
+            inner(buffer0, 0);
+            for (int s = 2; s < slabs; s += 2) {
+                staged_sync();
+                stage(s, buffer0);
+                step(buffer1, 0, 1);
+                inner(buffer1, 0);
+                staged_sync();
+                stage(s + 1, buffer1);
+                step(buffer0, 0, 1);
+                inner(buffer0, 0);
+            }
+            staged_sync();
             step(buffer1, 0, 1);
             inner(buffer1, 0);
-            staged_sync();
-            stage(s + 1, buffer1);
-            step(buffer0, 0, 1);
-            inner(buffer0, 0);
         }
-        staged_sync();
-        step(buffer1, 0, 1);
-        inner(buffer1, 0);
         multiply(f[1]);
         staged_sync();
     } else {
@@ -815,8 +901,11 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     // KG-th part of the rows that its group has.
     static_assert(KG == 1 || (4 % KG == 0 && WR == 1 && WC == 2), "some of 32 rows for a group");
     static_assert(kWaves * 2048 * 4 <= 2 * kOperand, "the epilogue's LDS");
-    float *const mine = (float *)buffer0 + wave_number() * 2048;
-    float *const sums = (float *)buffer0 + wave * 2048;  // the first group's
+    constexpr int kFit = kSplit ? kOperand / 8192 : KG * kWaves;  // waves in buffer0
+    float *const mine = wave_number() < kFit ? (float *)buffer0 + wave_number() * 2048
+                                             : (float *)buffer1 + (wave_number() - kFit) * 2048;
+    // the first group's
+    float *const sums = kSplit ? mine : (float *)buffer0 + wave * 2048;
     auto part_sync = [&] {
         if constexpr (KG > 1) __syncthreads();
         else wave_sync();
