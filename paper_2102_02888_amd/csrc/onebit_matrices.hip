@@ -568,8 +568,8 @@ __device__ __forceinline__ int deep_place(int byte)
 // Measured on that list (96 of 1,024 x 1,024, 24 of 4,096 x 1,024, 24 of 1,024 x 4,096;
 // us, and the share of the time that the matrix cores are busy):
 //            gram       poly       next        last
-//   pairs    951 66%    602 55%    1,682 67%   1,889 54%
-//   halves   420 56%    254 39%      906 39%     825 39%
+//   pairs    970 66%    607 55%    1,672 66%   1,952 56%
+//   halves   437 53%    268 44%      867 44%     836 45%
 // There is no LDS bank conflict but in the last one's turned tiles.  What bounds
 // pairs is the matrix cores in the slabs and memory in the epilogue, which one tile's
 // products cannot hide where it has its CU to itself; for halves, with a third of the
@@ -1214,7 +1214,7 @@ std::vector<MatTile> deal(std::vector<Costed> &all)
 //   1,024 x 1,024, halves                  133      141      229      433      133
 //   4 of them, halves                      428      329      263      450      263
 //   16 of them, pairs                    2,719    2,081    1,239    1,284    1,228
-//   144 of 1,024 x 1,024 to 4,096, halves 23,602  16,987    9,022    8,117    8,161
+//   144 of 1,024 x 1,024 to 4,096, halves 23,602  16,987    9,022    8,089    8,089
 struct Shape {
     int side, groups;
     double tile[2], slab[2], alone[2];
