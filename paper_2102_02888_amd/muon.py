@@ -26,10 +26,13 @@ MUON_SCALE_RMS = 2
 
 
 def products_for(out_dtype):
-    """The products an output of this type asks for by default: bfloat16
-    holds 8 bits, whose rounding (1.7e-3 as a whole) is above what
-    PRODUCTS_F16 adds (about 1e-3); float16 and float32 hold more."""
-    return PRODUCTS_F16 if out_dtype == torch.bfloat16 else PRODUCTS_F32
+    """The products of a call that names none: PRODUCTS_F32, whatever type the
+    output has, so that a result is off by the rounding to its type alone.
+    PRODUCTS_F16 takes about half as long over long lists and adds up to 1e-3
+    (bfloat16 results of gradients at the BERT-Large shape: 1.69e-3 from the
+    exact ones as a whole, where the type's rounding is 1.66e-3); it is the
+    caller's to ask for."""
+    return PRODUCTS_F32
 
 
 def _int64_array(values, count, name):
@@ -86,7 +89,10 @@ class Matrices:
         return self._bytes[products]
 
     def workspace(self, device, products=PRODUCTS_F32):
-        return torch.empty(max(self._bytes[products], 256), dtype=torch.uint8, device=device)
+        """A workspace for calls with these products, and with the other kind:
+        one serves calls that differ in them."""
+        most = max(self._bytes[products], *self._bytes.values(), 256)
+        return torch.empty(most, dtype=torch.uint8, device=device)
 
     def close(self):
         if self._h is not None:
@@ -139,8 +145,8 @@ def _coefficients(values):
 def onebit_orthogonalize(mats, grad, out, workspace, products=None, steps=5, eps=1e-7,
                          coefficients=None, stream=None):
     """out = the matrices of grad, orthogonalised by `steps` Newton-Schulz
-    steps; out may be grad itself.  products: PRODUCTS_F32 or PRODUCTS_F16
-    (default: products_for(out.dtype))."""
+    steps; out may be grad itself.  products: PRODUCTS_F32 (the default,
+    whatever out's type) or PRODUCTS_F16."""
     if products is None:
         products = products_for(out.dtype if isinstance(out, torch.Tensor) else None)
     gp, gcode = _flat(grad, mats, "grad")

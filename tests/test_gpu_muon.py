@@ -378,3 +378,20 @@ def test_creation_refusals(dev):
     x = torch.zeros(0, device=dev)
     ob.onebit_orthogonalize(mats, x, x, mats.workspace(dev))
     mats.close()
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16", "f16"])
+def test_default_products_are_those_of_fp32(dev, out):
+    """A call that names no products takes PRODUCTS_F32 for every output type: it is
+    off by that type's rounding alone.  One workspace serves both kinds."""
+    import paper_2102_02888_amd as ob
+    mats = ob.Matrices([(200, 300), (70, 64)])
+    grad = torch.empty(mats.extent, device=dev).normal_(0, 1e-3, generator=_gen(dev, 3))
+    work = mats.workspace(dev, ob.PRODUCTS_F16)
+    got = {}
+    for products in (None, ob.PRODUCTS_F32, ob.PRODUCTS_F16):
+        got[products] = torch.zeros(mats.extent, dtype=TYPES[out], device=dev)
+        ob.onebit_orthogonalize(mats, grad, got[products], work, products=products)
+    assert torch.equal(got[None], got[ob.PRODUCTS_F32])
+    assert not torch.equal(got[None], got[ob.PRODUCTS_F16])
+    mats.close()
