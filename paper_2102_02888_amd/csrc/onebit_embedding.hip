@@ -751,7 +751,7 @@ constexpr int64_t kSizeLimit = (int64_t)1 << 31;
 struct GradLayout {
     int piece, columns;  // columns: of a thread
     int64_t pieces, per_row;
-    size_t keys[2], order[2], counts, partial, begins, rows, present, total;  // byte offsets
+    size_t keys[2], order[2], counts, partial, begins, rows, present;  // byte offsets
 };
 
 size_t round_up(size_t a, size_t m) { return (a + m - 1) / m * m; }
@@ -761,13 +761,16 @@ size_t round_up(size_t a, size_t m) { return (a + m - 1) / m * m; }
 // the partial sums and the join's chains.  us, pieces of 16 / 32 / 64 / 128:
 // 131,072 bf16 places of 1,024 columns 187 / 165 / 159 / 156, 33,333 fp32 ones of
 // 771 68 / 78 / 100 / 100 (97 threads a row).
+constexpr int kLeastPiece = 8, kMostPiece = 128;
+constexpr int64_t kPieceThreads = 1 << 18;
+
 GradLayout grad_layout(int64_t tokens, int64_t width, int elem)
 {
     GradLayout l{};
     l.columns = width >= 16 / elem ? 16 / elem : 1;
     l.per_row = (width + l.columns - 1) / l.columns;
-    l.piece = 8;
-    while (l.piece < 128 && tokens / (2 * l.piece) * l.per_row >= (1 << 18)) l.piece *= 2;
+    l.piece = kLeastPiece;
+    while (l.piece < kMostPiece && tokens / (2 * l.piece) * l.per_row >= kPieceThreads) l.piece *= 2;
     l.pieces = (tokens + l.piece - 1) / l.piece;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -776,16 +779,32 @@ GradLayout grad_layout(int64_t tokens, int64_t width, int elem)
         return here;
     };
     for (int k = 0; k < 2; ++k) {
-        l.keys[k] = take(((size_t)l.pieces * l.piece + 4 * kAhead) * 4);
-        l.order[k] = take(((size_t)l.pieces * l.piece + 4 * kAhead) * 4);
+        l.keys[k] = take((round_up(tokens, kMostPiece) + 4 * kAhead) * 4);
+        l.order[k] = take((round_up(tokens, kMostPiece) + 4 * kAhead) * 4);
     }
     l.begins = take(((size_t)std::min<int64_t>(tokens, kSmallTokens) + 1) * 4);
     l.rows = take(4);
     l.present = take(kSmallRows / 8);
     l.counts = take((size_t)kSortBlocks * kDigits * 4);
-    l.partial = take((size_t)l.pieces * 2 * l.per_row * l.columns * 4);
-    l.total = at;
+    l.partial = at;
     return l;
+}
+
+// Bytes that serve every call of up to so many tokens and columns.  The areas before
+// the partial sums grow with the tokens, but there are fewer partial sums where a
+// longer piece begins: a call has pieces * 2 * (its columns, padded to its threads').
+// With the longest piece that is at most the first number below; with a shorter one
+// tokens / (2 piece) * per_row stayed below kPieceThreads, so that pieces * per_row is
+// below 2 kPieceThreads + 2 per_row, and pieces are at least kLeastPiece places.
+size_t grad_workspace(int64_t tokens, int64_t width, int elem)
+{
+    const GradLayout l = grad_layout(tokens, width, elem);
+    const size_t padded = (size_t)(l.per_row * l.columns);
+    auto pieces = [&](int piece) { return round_up(tokens, piece) / piece; };
+    const size_t longest = pieces(kMostPiece) * padded;
+    const size_t shorter = std::min(pieces(kLeastPiece) * padded,
+                                    2 * (size_t)kPieceThreads * (16 / elem) + 2 * padded);
+    return l.partial + round_up(std::max(longest, shorter) * 2 * 4, 256);
 }
 
 int check_size(int64_t v, const char *name)
@@ -885,7 +904,7 @@ int onebit_embedding_grad_workspace(int64_t tokens, int64_t vocab, int64_t width
     TRY(check_size(tokens, "tokens"));
     TRY(check_size(vocab, "vocab"));
     TRY(check_size(width, "width"));
-    *bytes = std::max(grad_layout(tokens, width, 2).total, grad_layout(tokens, width, 4).total);
+    *bytes = std::max(grad_workspace(tokens, width, 2), grad_workspace(tokens, width, 4));
     return ONEBIT_OK;
 }
 

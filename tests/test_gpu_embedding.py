@@ -287,3 +287,28 @@ def test_gradient_of_many_rows(dev, tokens, vocab):
     on = (ids >= 0) & (ids < vocab)
     want = torch.bincount(ids[on], minlength=vocab).to(torch.float16)
     assert torch.equal(grad[:, 0], want)
+
+
+@pytest.mark.parametrize("src", ["bf16", "f32"])
+def test_one_workspace_for_shorter_and_narrower_calls(dev, src):
+    """A workspace of exactly the size for the largest call serves the others, and
+    nothing behind it is touched: calls on both sides of where the pieces of the
+    list get longer (32,768 places of 1,024 bf16 columns, 16,384 of fp32)."""
+    import paper_2102_02888_amd as ob
+    vocab, most, wide = 500, 32768, 1024
+    n = ctypes.c_size_t()
+    assert ob.lib().onebit_embedding_grad_workspace(most, vocab, wide, ctypes.byref(n)) == 0
+    # as much again behind it as the largest need of any of these calls
+    whole = torch.full((n.value + (64 << 20),), 0xA5, dtype=torch.uint8, device=dev)
+    work, behind = whole[:n.value], whole[n.value:]
+    for tokens, width in ((most, wide), (most - 1, wide), (most, 1016), (16384, wide),
+                          (16383, wide), (16384, 1020), (4097, 1000), (4096, wide), (100, 7)):
+        dout = torch.randint(-4, 5, (tokens, width), device=dev, generator=_gen(dev, 1))
+        dout = dout.to(TYPES[src])
+        ids = torch.randint(-1, vocab, (tokens,), device=dev, generator=_gen(dev, 2))
+        grad = torch.full((vocab, width), 3.0, device=dev)
+        ob.onebit_embedding_grad(dout, ids, grad, work)
+        want = torch.zeros(vocab + 1, width, device=dev)  # small integers: exact in any order
+        want.index_add_(0, torch.where(ids < 0, vocab, ids), dout.float())
+        assert torch.equal(grad, want[:-1]), (tokens, width)
+        assert bool((behind == 0xA5).all()), (tokens, width)
