@@ -120,10 +120,12 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Workgroup barrier behind loads straight into LDS: every wave waits for its own
-// before it arrives (a plain barrier does not wait for them).
+// Workgroup barrier behind loads straight into LDS, or behind stores that are to be
+// there for other workgroups: every wave waits for its own before it arrives (a plain
+// barrier waits for neither).
 __device__ __forceinline__ void staged_sync()
 {
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0), the other counters at their most
     __syncthreads();
 }
@@ -985,13 +987,19 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
                     take(row_in_block(k), v);
                     __builtin_memcpy(at(it.part, k), v, sizeof v);
                 }
-                // One thread's release and acquire stand for the workgroup's: the barriers
-                // order the others' accesses with it.  (A fence writes the whole L2 back:
+                // One thread's release and acquire stand for the workgroup's: every wave's
+                // stores have reached the L2 before the barrier, and what they read after
+                // the next one comes from behind it.  (A fence writes the whole L2 back:
                 // one in every wave took 86 us where the products take 30.)
-                __syncthreads();
+                staged_sync();
                 if (threadIdx.x == 0) {
+                    // The wait for the write-back is stated: behind a wait for all stores
+                    // the compiler takes the release's own for done and leaves it out.
+                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                     const uint32_t before = __hip_atomic_fetch_add(
-                        w.counter + it.slot, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+                        w.counter + it.slot, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
                     scratch[0] = before + 1 == (uint32_t)mt.parts ? 1.f : 0.f;
                     if (before + 1 == (uint32_t)mt.parts)
                         __hip_atomic_store(w.counter + it.slot, 0u, __ATOMIC_RELAXED,

@@ -1,9 +1,17 @@
 """The language-model operators' host side, without a GPU."""
 import ctypes
+import glob
+import os
+import re
+import shutil
+import subprocess
 
 import pytest
 
 from paper_2102_02888_amd import _native
+from paper_2102_02888_amd.build import LIB
+
+OBJDUMP = "/opt/rocm/llvm/bin/llvm-objdump"
 
 
 @pytest.fixture(scope="module")
@@ -40,3 +48,49 @@ def test_gradient_workspace_serves_every_shorter_and_narrower_call(lib, vocab):
             assert size >= most, (t, w)
             assert size >= below[k], (t, w)
             most, below[k] = size, size
+
+
+def _kernels(tmp_path):
+    """{kernel symbol: its instructions} of the built library's gfx950 code."""
+    shutil.copy(LIB, tmp_path / "lib.so")
+    subprocess.run([OBJDUMP, "--offloading", "lib.so"], cwd=tmp_path, check=True,
+                   stdout=subprocess.DEVNULL)
+    out = {}
+    for part in glob.glob(str(tmp_path / "lib.so.*gfx950")):
+        text = subprocess.run([OBJDUMP, "-d", "--no-show-raw-insn", part], check=True,
+                              stdout=subprocess.PIPE, text=True).stdout
+        for line in text.splitlines():
+            name = re.match(r"[0-9a-f]+ <(.*)>:$", line)
+            if name:
+                now = out.setdefault(name.group(1), [])
+            elif line.startswith("\t"):
+                now.append(line.split("//")[0].strip())
+    return out
+
+
+@pytest.mark.skipif(not os.path.exists(OBJDUMP), reason="no disassembler for the built kernels")
+def test_every_wave_waits_for_its_stores_before_a_workgroup_publishes_them(tmp_path):
+    """Where one thread releases a whole workgroup's sums to other workgroups (the
+    write-back of the L2, then the counter's increment), every wave has to have
+    waited for its own stores before the barrier that the thread comes from, which
+    does not wait for them by itself; the thread has to wait for the write-back
+    before it counts, and for the count before it discards what its caches hold."""
+    found = 0
+
+    def waits(code):
+        return any(l.startswith("s_waitcnt") and "vmcnt(0)" in l for l in code)
+
+    for name, code in _kernels(tmp_path).items():
+        for k, line in enumerate(code):
+            if not line.startswith("buffer_wbl2"):
+                continue
+            found += 1
+            barrier = max(i for i in range(k) if code[i].startswith("s_barrier"))
+            store = max(i for i in range(barrier) if "global_store" in code[i])
+            count = min(i for i in range(k, len(code)) if "atomic_add" in code[i])
+            discard = min(i for i in range(count, len(code)) if code[i].startswith("buffer_inv"))
+            after = min(i for i in range(count, len(code)) if code[i].startswith("s_barrier"))
+            assert waits(code[store:barrier]), (name, code[store:barrier + 1])
+            assert waits(code[k:count]), (name, code[k:count + 1])
+            assert waits(code[count:discard]) and discard < after, (name, code[count:after + 1])
+    assert found  # the parts of a Gram sum
