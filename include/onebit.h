@@ -461,6 +461,17 @@ int onebit_matrices_destroy(onebit_matrices mats);
 int onebit_matrices_info(onebit_matrices mats, int32_t products, int64_t *extent,
                          int64_t *offset, size_t *workspace_bytes);
 
+/* Which kernels form the three products of a step (D, B, and X + B X) over a list of
+ * matrices of these sizes: side[k] of the k-th's square tiles, 64, 128 or 256, and
+ * groups[k] of waves that share a tile's summed index (1 but for tiles of 64).
+ * parts: the most parts that the sum of a tile of D is cut into.  They are chosen by the
+ * estimated time; results of another choice differ in the order of sums alone.  Needs
+ * no device.  Any output may be NULL; all are 0 where no matrix has elements.
+ * Errors: EINVAL (null, count < 1, a side below 0 or above 2^20, unknown products), ENOMEM. */
+int onebit_matrices_kernels(const int64_t *rows, const int64_t *cols, int32_t count,
+                            int32_t products, int32_t side[3], int32_t groups[3],
+                            int32_t *parts);
+
 /* out = O(in), matrix by matrix; elements outside the matrices are not
  * written.  in, out: flat buffers of `extent` elements of their types; out may
  * be the same buffer as in (same type).  workspace: 256-byte aligned.

@@ -15,7 +15,7 @@ from .embedding import (  # noqa: F401
 from .freeze import VarianceFreezeDetector  # noqa: F401
 from .muon import (  # noqa: F401
     Matrices, Muon, MUON_SCALE_NONE, MUON_SCALE_RMS, MUON_SCALE_SPECTRAL, PRODUCTS_F16,
-    PRODUCTS_F32, onebit_muon_step, onebit_orthogonalize, products_for,
+    PRODUCTS_F32, matrices_kernels, onebit_muon_step, onebit_orthogonalize, products_for,
 )
 from .optimizer import OnebitAdam  # noqa: F401
 from ._native import OnebitError, lib  # noqa: F401

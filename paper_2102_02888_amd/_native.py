@@ -61,6 +61,7 @@ SIGNATURES = {
     "onebit_matrices_create": [_vp, _vp, _vp, _vp, _i32, _vp],
     "onebit_matrices_destroy": [_vp],
     "onebit_matrices_info": [_vp, _i32, _vp, _vp, _vp],
+    "onebit_matrices_kernels": [_vp, _vp, _i32, _i32, _vp, _vp, _vp],
     "onebit_orthogonalize": [_vp, _vp, _i32, _vp, _i32, _i32, _i32, _vp, _f32, _vp, _vp],
     "onebit_muon_step": [_vp, _vp, _vp, _vp, _i32, _i64, _i32, _f32, _f32, _i32, _f32, _i32, _i32,
                          _i32, _vp, _f32, _vp, _vp],

@@ -1419,6 +1419,17 @@ int build_side(std::vector<Mat> mats, int kind, Side &side, Built &out)
     return ONEBIT_OK;
 }
 
+int check_sides(int k, int64_t r, int64_t c)
+{
+    constexpr int64_t kSide = 1 << 20;
+    if (r < 0 || c < 0 || r > kSide || c > kSide)
+        return fail(ONEBIT_EINVAL, "matrix %d is %lld x %lld: a side is at most 2^20", k,
+                    (long long)r, (long long)c);
+    if (r * c >= ((int64_t)1 << 31))
+        return fail(ONEBIT_EINVAL, "matrix %d has 2^31 elements or more", k);
+    return ONEBIT_OK;
+}
+
 int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
                 const int64_t *ld, int32_t count, onebit_matrices *out)
 {
@@ -1434,14 +1445,10 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
     double elements = 0;
     for (int32_t k = 0; k < count; ++k) elements += (double)rows[k] * (double)cols[k];
     const int size = p->norm_size = elements <= (1 << 23) ? 2048 : 8192;
-    constexpr int64_t kSide = 1 << 20, kMost = (int64_t)1 << 40, kItems = 1 << 23;
+    constexpr int64_t kMost = (int64_t)1 << 40, kItems = 1 << 23;
     for (int32_t k = 0; k < count; ++k) {
         const int64_t r = rows[k], c = cols[k];
-        if (r < 0 || c < 0 || r > kSide || c > kSide)
-            return fail(ONEBIT_EINVAL, "matrix %d is %lld x %lld: a side is at most 2^20", k,
-                        (long long)r, (long long)c);
-        if (r * c >= ((int64_t)1 << 31))
-            return fail(ONEBIT_EINVAL, "matrix %d has 2^31 elements or more", k);
+        TRY(check_sides(k, r, c));
         const int64_t pitch = ld ? ld[k] : c;
         const int64_t off = offset ? offset[k] : at;
         if (pitch < c || pitch > kMost)
@@ -1515,6 +1522,28 @@ int create_impl(const int64_t *rows, const int64_t *cols, const int64_t *offset,
         s.next.tiles = (const MatTile *)(p->dev + o[k][4]);
     }
     *out = p.release();
+    return ONEBIT_OK;
+}
+
+int kernels_impl(const int64_t *rows, const int64_t *cols, int32_t count, int kind,
+                 int32_t (&side)[3], int32_t (&groups)[3], int32_t &parts)
+{
+    std::vector<Sizes> sizes;
+    for (int32_t k = 0; k < count; ++k) {
+        TRY(check_sides(k, rows[k], cols[k]));
+        if (rows[k] > 0 && cols[k] > 0)
+            sizes.push_back(Sizes{std::min(rows[k], cols[k]), std::max(rows[k], cols[k])});
+    }
+    if (sizes.empty()) return ONEBIT_OK;
+    Shape shape[3];
+    choose(sizes, kind, shape);
+    for (int k = 0; k < 3; ++k) {
+        side[k] = shape[k].side;
+        groups[k] = shape[k].groups;
+    }
+    const int pad = shape[kIsNext].side;
+    const int64_t part = part_slabs(sizes, shape[kIsGram], pad, kind);
+    for (const Sizes &z : sizes) parts = std::max(parts, parts_of(z, pad, kind, part));
     return ONEBIT_OK;
 }
 
@@ -1695,6 +1724,25 @@ int onebit_matrices_info(onebit_matrices mats, int32_t products, int64_t *extent
     if (offset) std::copy(mats->offset.begin(), mats->offset.end(), offset);
     if (workspace_bytes)
         *workspace_bytes = layout_of(mats, products == ONEBIT_PRODUCTS_F32).total;
+    return ONEBIT_OK;
+}
+
+int onebit_matrices_kernels(const int64_t *rows, const int64_t *cols, int32_t count,
+                            int32_t products, int32_t side[3], int32_t groups[3], int32_t *parts)
+{
+    if (!rows || !cols) return fail(ONEBIT_EINVAL, "rows or cols is NULL");
+    if (count < 1) return fail(ONEBIT_EINVAL, "count < 1");
+    if (products != ONEBIT_PRODUCTS_F32 && products != ONEBIT_PRODUCTS_F16)
+        return fail(ONEBIT_EINVAL, "products %d is not one of ONEBIT_PRODUCTS_*", products);
+    int32_t s[3] = {}, g[3] = {}, p = 0;
+    try {
+        TRY(kernels_impl(rows, cols, count, products == ONEBIT_PRODUCTS_F32 ? 2 : 1, s, g, p));
+    } catch (const std::bad_alloc &) {
+        return fail(ONEBIT_ENOMEM, "host memory for the matrix tables");
+    }
+    if (side) std::copy(s, s + 3, side);
+    if (groups) std::copy(g, g + 3, groups);
+    if (parts) *parts = p;
     return ONEBIT_OK;
 }
 

@@ -15,7 +15,7 @@ from .onebit import _GRAD_DTYPES, _stream
 
 __all__ = ["Matrices", "Muon", "MUON_SCALE_NONE", "MUON_SCALE_SPECTRAL", "MUON_SCALE_RMS",
            "PRODUCTS_F32", "PRODUCTS_F16", "onebit_muon_step", "onebit_orthogonalize",
-           "products_for"]
+           "matrices_kernels", "products_for"]
 
 # The ONEBIT_PRODUCTS_* and ONEBIT_MUON_SCALE_* constants.
 PRODUCTS_F32 = 0
@@ -42,6 +42,22 @@ def _int64_array(values, count, name):
     if a.shape != (count,):
         raise ValueError("%s must have one entry per matrix" % name)
     return a, a.ctypes.data_as(ctypes.c_void_p)
+
+
+def matrices_kernels(shapes, products=PRODUCTS_F32):
+    """Which kernels the calls over matrices of these shapes take: the tiles'
+    side and the groups of waves that share a tile, of a step's three products
+    ("gram": D, "poly": B, "next": X + B X), and the most "parts" of a tile of D.
+    Needs no GPU."""
+    rows, rp = _int64_array([r for r, _ in shapes], len(shapes), "shapes")
+    cols, cp = _int64_array([c for _, c in shapes], len(shapes), "shapes")
+    side, groups = (ctypes.c_int32 * 3)(), (ctypes.c_int32 * 3)()
+    parts = ctypes.c_int32()
+    call("onebit_matrices_kernels", rp, cp, len(shapes), int(products), side, groups,
+         ctypes.byref(parts))
+    out = {name: (side[k], groups[k]) for k, name in enumerate(("gram", "poly", "next"))}
+    out["parts"] = parts.value
+    return out
 
 
 class Matrices:

@@ -16,6 +16,8 @@ import math
 import pytest
 import torch
 
+from matrix_lists import KERNEL_LISTS
+
 pytestmark = pytest.mark.gpu
 
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
@@ -394,4 +396,62 @@ def test_default_products_are_those_of_fp32(dev, out):
         ob.onebit_orthogonalize(mats, grad, got[products], work, products=products)
     assert torch.equal(got[None], got[ob.PRODUCTS_F32])
     assert not torch.equal(got[None], got[ob.PRODUCTS_F16])
+    mats.close()
+
+
+@pytest.mark.parametrize("name", list(KERNEL_LISTS))
+@pytest.mark.parametrize("products,tol", [("f32", 1e-5), ("f16", 3e-3)])
+def test_orthogonalize_by_every_kernel(dev, name, products, tol):
+    """The kernels that the list is meant for are those that its call takes; every
+    matrix against the formula; bit for bit the same in every call; nothing between
+    the matrices is written."""
+    import paper_2102_02888_amd as ob
+    shapes, pairs, halves = KERNEL_LISTS[name]
+    prod = ob.PRODUCTS_F32 if products == "f32" else ob.PRODUCTS_F16
+    assert ob.matrices_kernels(shapes, prod) == (pairs if products == "f32" else halves)
+    mats = ob.Matrices(shapes)
+    grad = torch.empty(mats.extent, device=dev).normal_(0, 1e-3, generator=_gen(dev, 1))
+    res = torch.full((mats.extent,), 7.0, device=dev)
+    work = mats.workspace(dev, prod)
+    work.fill_(255)
+    ob.onebit_orthogonalize(mats, grad, res, work, products=prod)
+    for k in range(len(shapes)):
+        assert _rel(mats.view(res, k), _ortho64(mats.view(grad, k))) < tol, (k, shapes[k])
+    between = torch.ones_like(res, dtype=torch.bool)
+    for k in range(len(shapes)):
+        mats.view(between, k).fill_(False)
+    assert bool((res[between] == 7.0).all())
+    again = torch.full_like(res, 7.0)
+    for _ in range(4):
+        ob.onebit_orthogonalize(mats, grad, again, work, products=prod)
+        assert torch.equal(again, res)
+    mats.close()
+
+
+@pytest.mark.parametrize("name", list(KERNEL_LISTS))
+@pytest.mark.parametrize("products,tol,n,grad", [("f32", 1e-5, 1, "bf16"), ("f32", 1e-5, 3, "f32"),
+                                                 ("f16", 3e-3, 2, "bf16")])
+def test_muon_step_by_every_kernel(dev, name, products, tol, n, grad):
+    """One step from a momentum that is not zero; tolerances as for one step of
+    test_muon_step, with the products' own."""
+    import paper_2102_02888_amd as ob
+    shapes = KERNEL_LISTS[name][0]
+    mats = ob.Matrices(shapes)
+    opt = ob.Muon(mats, dev, lr=0.02, momentum=0.9, weight_decay=0.1, scale=ob.MUON_SCALE_RMS,
+                  n_workers=n, grad_dtype=TYPES[grad],
+                  products=ob.PRODUCTS_F32 if products == "f32" else ob.PRODUCTS_F16)
+    opt.x.normal_(0, 0.02, generator=_gen(dev, 1))
+    opt.m.normal_(0, 2e-3, generator=_gen(dev, 2))
+    for i in range(n):
+        opt.grads[i].normal_(0, 1e-3, generator=_gen(dev, 3 + i))
+    x, m = opt.x.clone(), opt.m.clone()
+    opt.step()
+    for k in range(len(shapes)):
+        old = mats.view(x, k).double()
+        want_x, want_m = _muon64(old, mats.view(m, k), [mats.view(g, k) for g in opt.grads], 0.02,
+                                 0.9, True, 0.1, ob.MUON_SCALE_RMS)
+        assert _rel(mats.view(opt.m, k), want_m) < 3 * 2.0 ** -23
+        move = float((want_x - old).norm())
+        far = float((mats.view(opt.x, k).double() - want_x).norm())
+        assert far < tol * move + 2.0 ** -22 * float(want_x.norm()), (k, far, move)
     mats.close()

@@ -10,6 +10,8 @@ import pytest
 
 from paper_2102_02888_amd import _native
 from paper_2102_02888_amd.build import LIB
+from paper_2102_02888_amd.muon import PRODUCTS_F16, PRODUCTS_F32, matrices_kernels
+from matrix_lists import KERNEL_LISTS
 
 OBJDUMP = "/opt/rocm/llvm/bin/llvm-objdump"
 
@@ -94,3 +96,31 @@ def test_every_wave_waits_for_its_stores_before_a_workgroup_publishes_them(tmp_p
             assert waits(code[k:count]), (name, code[k:count + 1])
             assert waits(code[count:discard]) and discard < after, (name, code[count:after + 1])
     assert found  # the parts of a Gram sum
+
+
+def test_tested_lists_take_every_kernel():
+    """Each product (the last one is next's other epilogue) by each of the four
+    kernels, for both kinds of products; and sums in parts, for both."""
+    want = {(name, kernel) for name in ("gram", "poly", "next")
+            for kernel in ((64, 2), (64, 4), (128, 1), (256, 1))}
+    for products, at in ((PRODUCTS_F32, 1), (PRODUCTS_F16, 2)):
+        seen, parts = set(), 0
+        for case, entry in KERNEL_LISTS.items():
+            got = matrices_kernels(entry[0], products)
+            assert got == entry[at], case
+            parts = max(parts, got.pop("parts"))
+            seen |= set(got.items())
+        assert seen == want and parts > 1
+
+
+def test_matrices_kernels_refusals_and_empty_lists(lib):
+    empty = dict(gram=(0, 0), poly=(0, 0), next=(0, 0), parts=0)
+    assert matrices_kernels([(0, 5), (7, 0)]) == empty
+    one = (ctypes.c_int64 * 1)(4)
+    assert lib.onebit_matrices_kernels(one, one, 1, 0, None, None, None) == 0
+    assert lib.onebit_matrices_kernels(None, one, 1, 0, None, None, None) == -1
+    assert lib.onebit_matrices_kernels(one, one, 0, 0, None, None, None) == -1
+    assert lib.onebit_matrices_kernels(one, one, 1, 2, None, None, None) == -1
+    for bad in ((-1, 4), (4, (1 << 20) + 1), (1 << 16, 1 << 16)):
+        with pytest.raises(_native.OnebitError):
+            matrices_kernels([(4, 4), bad])
