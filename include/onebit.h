@@ -401,8 +401,10 @@ int onebit_embedding_grad_workspace(int64_t tokens, int64_t vocab, int64_t width
  * One rounding to the gradient's type, after the old value is added in fp32.
  * dout: `tokens` rows of `width` elements, dout_ld apart; grad: `vocab` rows,
  * grad_ld apart, in/out; workspace: onebit_embedding_grad_workspace() bytes,
- * 16-byte aligned.  Errors: EINVAL (as above; more than 2^31 places times
- * groups of 1,024 columns), EALIGN, EHIP. */
+ * 16-byte aligned.  A call of up to 2^29 places, counted in whole 128s, times
+ * groups of 128 columns (256 where dout has 16 bits) is never too large; a larger
+ * one may be.  Errors: EINVAL (as above; too large, before anything is written),
+ * EALIGN, EHIP. */
 int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld, const void *ids,
                           int32_t ids_bytes, int64_t tokens, int64_t vocab, int64_t width,
                           int64_t padding_id, float scale, void *grad, int32_t grad_dtype,

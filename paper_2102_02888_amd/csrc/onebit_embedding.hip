@@ -925,9 +925,15 @@ int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld,
     if (vocab == 0 || width == 0 || (tokens == 0 && accumulate)) return ONEBIT_OK;
     hipStream_t st = (hipStream_t)stream;
     const GradLayout l = grad_layout(tokens, width, elem_bytes(dout_dtype));
+    // Launches stay below 2^32 threads: where a short list's sums would not, because its
+    // rows are very wide, it goes the longer way, whose workgroups take many places.
+    const int across = (int)std::min<int64_t>(l.per_row, 128);
+    const int64_t groups = (l.per_row + across - 1) / across;
+    const bool small = tokens <= kSmallTokens &&
+                       tokens * groups + 4 * kFillBlocks < ((int64_t)1 << 32) / kSmallThreads;
     const int64_t blocks = (l.pieces * l.per_row + 255) / 256;
     const int64_t joins = (l.per_row + 256 / kJoin - 1) / (256 / kJoin);  // workgroups of a piece
-    if (blocks > (1 << 23) || l.pieces * joins > (1 << 23))
+    if (!small && (blocks > (1 << 23) || l.pieces * joins > (1 << 23)))
         return fail(ONEBIT_EINVAL, "%lld places of %lld columns are too many for one call",
                     (long long)tokens, (long long)width);
     char *ws = (char *)workspace;
@@ -939,7 +945,6 @@ int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld,
     int now = 0;
     // Half of the rows are zeroed beside the sort of a short list, all of them where
     // there are too many for its bits; the others beside the sums.
-    const bool small = tokens <= kSmallTokens;
     const int words = small && vocab <= kSmallRows ? (int)((vocab + 31) / 32) : 0;
     Fill rest = fill;
     if (small) {
@@ -984,15 +989,13 @@ int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld,
            vocab, (int)width, (int)l.per_row, l.piece, l.pieces, scale, accumulate, dout_ld,
            grad_ld, (float *)(ws + l.partial)};
     const int absent = accumulate ? 0 : (int)std::min<int64_t>(4 * kFillBlocks, (rest.end - rest.begin + 31) / 32);
-    const int across = (int)std::min<int64_t>(l.per_row, 128);
-    const int groups = (int)((l.per_row + across - 1) / across);
     auto sums = [&](auto columns, auto *d, auto *g) {
         using D = std::remove_pointer_t<decltype(d)>;
         using G = std::remove_pointer_t<decltype(g)>;
         constexpr int V = decltype(columns)::value;
         if (small) {
-            k_grad_rows<D, G, V><<<(int)tokens * groups + absent, kSmallThreads, 0, st>>>(
-                s, (const D *)dout, (G *)grad, across, groups, (const uint32_t *)(ws + l.begins),
+            k_grad_rows<D, G, V><<<(int)(tokens * groups) + absent, kSmallThreads, 0, st>>>(
+                s, (const D *)dout, (G *)grad, across, (int)groups, (const uint32_t *)(ws + l.begins),
                 (const uint32_t *)(ws + l.rows), (const uint32_t *)(ws + l.present), rest);
             return;
         }

@@ -312,3 +312,21 @@ def test_one_workspace_for_shorter_and_narrower_calls(dev, src):
         want.index_add_(0, torch.where(ids < 0, vocab, ids), dout.float())
         assert torch.equal(grad, want[:-1]), (tokens, width)
         assert bool((behind == 0xA5).all()), (tokens, width)
+
+
+@pytest.mark.parametrize("src,width", [("f32", 523776), ("f32", 524292), ("bf16", 1048584)])
+def test_gradient_of_short_lists_of_very_wide_rows(dev, src, width):
+    """Up to 4,096 places on both sides of where a workgroup for every row and group
+    of columns would be 2^32 threads and more."""
+    import paper_2102_02888_amd as ob
+    tokens, vocab = 4096, 3
+    dout = torch.randint(-4, 5, (tokens, width), device=dev, dtype=TYPES[src],
+                         generator=_gen(dev, 1))
+    ids = torch.randint(-1, vocab - 1, (tokens,), device=dev, generator=_gen(dev, 2))
+    grad = torch.full((vocab, width), 3.0, device=dev)
+    ob.onebit_embedding_grad(dout, ids, grad, ob.embedding_workspace(tokens, vocab, width, dev))
+    for v in range(vocab):  # small integers: exact in any order
+        want = torch.zeros(width, device=dev)
+        for part in torch.nonzero(ids == v)[:, 0].split(256):
+            want += dout[part].float().sum(0)
+        assert torch.equal(grad[v], want), v

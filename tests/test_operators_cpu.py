@@ -124,3 +124,12 @@ def test_matrices_kernels_refusals_and_empty_lists(lib):
     for bad in ((-1, 4), (4, (1 << 20) + 1), (1 << 16, 1 << 16)):
         with pytest.raises(_native.OnebitError):
             matrices_kernels([(4, 4), bad])
+
+
+def test_gradient_too_large_for_a_launch_is_refused_before_it(lib):
+    """(The pointers are not read: nothing is launched.)"""
+    for tokens, width, dtype in ((1 << 30, 257, 0), ((1 << 31) - 1, 1, 0), (1 << 29, 513, 1),
+                                 (1, (1 << 31) - 1, 0)):
+        assert lib.onebit_embedding_grad(4096, dtype, width, 4096, 4, tokens, 10, width, -1, 1.0,
+                                         4096, 0, width, 0, 4096, None) == -1, (tokens, width)
+        assert b"too many" in lib.onebit_last_error()
