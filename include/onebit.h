@@ -443,7 +443,9 @@ typedef struct onebit_matrices_s *onebit_matrices;
 #define ONEBIT_PRODUCTS_F32 0
 #define ONEBIT_PRODUCTS_F16 1
 
-/* How the step's update is scaled, by the matrix's shape. */
+/* How the step's update is scaled, by the matrix's shape.  SPECTRAL is meant for
+ * matrices whose rows are outputs and whose columns are inputs (y = W x); where they are
+ * stored the other way (y = x W), RMS does not depend on it. */
 #define ONEBIT_MUON_SCALE_NONE 0     /* 1                          */
 #define ONEBIT_MUON_SCALE_SPECTRAL 1 /* sqrt(max(1, rows / cols))  */
 #define ONEBIT_MUON_SCALE_RMS 2      /* 0.2 sqrt(max(rows, cols))  */

@@ -15,7 +15,7 @@ import torch
 import torch.nn.functional as F
 
 from .embedding import embedding_workspace, onebit_embedding_forward, onebit_embedding_grad
-from .muon import Matrices, Muon
+from .muon import MUON_SCALE_RMS, Matrices, Muon
 from .onebit import Plan
 from .optimizer import OnebitAdam
 
@@ -30,7 +30,8 @@ class Model:
         self.adam = OnebitAdam(self.plan, device, lr=3e-3, warmup_steps=40)
         self.mats = Matrices([s for _ in range(layers) for s in ((width, 4 * width),
                                                                  (4 * width, width))])
-        self.muon = Muon(self.mats, device, lr=0.02, n_workers=n_workers)
+        # (a matrix's rows are its inputs here, h @ a: not what the spectral scale is for)
+        self.muon = Muon(self.mats, device, lr=0.005, scale=MUON_SCALE_RMS, n_workers=n_workers)
         self.table = self._table(self.adam.x)
         self.table.normal_(0.0, 0.05, generator=gen)
         self.matrices = [self.mats.view(self.muon.x, k) for k in range(2 * layers)]

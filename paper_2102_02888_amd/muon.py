@@ -177,7 +177,10 @@ def onebit_muon_step(mats, x, m, grads, lr, momentum, workspace, nesterov=True, 
                      scale=MUON_SCALE_SPECTRAL, products=PRODUCTS_F32, steps=5, eps=1e-7,
                      coefficients=None, stream=None):
     """One Muon step of the matrices of x: the mean of grads' rows, momentum m,
-    orthogonalised update.  grads: one flat buffer, or [n, >= extent] rows."""
+    orthogonalised update.  grads: one flat buffer, or [n, >= extent] rows.
+    scale: MUON_SCALE_SPECTRAL, sqrt(max(1, rows / columns)), is for matrices
+    with a row per output (y = W x); MUON_SCALE_RMS, 0.2 sqrt(max(rows,
+    columns)), fits both ways of storing them."""
     xp, _ = _flat(x, mats, "x", torch.float32)
     mp, _ = _flat(m, mats, "m", torch.float32)
     if not isinstance(grads, torch.Tensor) or grads.dtype not in _GRAD_DTYPES:

@@ -57,3 +57,16 @@ def test_model_learns_its_tokens(dev):
     assert abs(first - math.log(1000)) < 1.0
     assert not model.adam.in_warmup
     assert float(last) < 3.5
+
+
+def test_updates_do_not_depend_on_which_side_the_rows_are(dev):
+    """The layers' matrices, width x 4 width and back, are used as h @ a, with inputs as
+    rows.  Orthogonalised updates of both have the same number of singular values
+    near 1; the scale must not make the one that leads back the larger."""
+    from paper_2102_02888_amd.lm_example import Model
+    model = Model(dev)
+    old = [m.clone() for m in model.matrices]
+    model.step()
+    for a, b in zip(range(0, len(old), 2), range(1, len(old), 2)):
+        one, two = (float((model.matrices[k] - old[k]).norm()) for k in (a, b))
+        assert 0.75 < one / two < 1.33, (one, two)
