@@ -436,8 +436,9 @@ int onebit_embedding_grad(const void *dout, int32_t dout_dtype, int64_t dout_ld,
  *   meant for 16-bit outputs.
  * Coefficients.  The three numbers a, b, c (host array, read during the call;
  *   NULL: 3.4445, -4.7750, 2.0315).  Refused when the singular values could
- *   leave the range that the fp16 operands hold (|X|, |A| and the polynomial's
- *   change up to 7.5). */
+ *   leave the range that the fp16 operands hold: |X|, |A| and the change of
+ *   a + b v + c v^2 over them up to 7.5; and |b| + 0.75 |c| up to 7.5, whatever the
+ *   matrices, which bounds the products while one of a norm far below eps grows. */
 typedef struct onebit_matrices_s *onebit_matrices;
 
 #define ONEBIT_PRODUCTS_F32 0

@@ -455,3 +455,21 @@ def test_muon_step_by_every_kernel(dev, name, products, tol, n, grad):
         far = float((mats.view(opt.x, k).double() - want_x).norm())
         assert far < tol * move + 2.0 ** -22 * float(want_x.norm()), (k, far, move)
     mats.close()
+
+
+@pytest.mark.parametrize("kind", ["noise", "tiny"])
+def test_coefficients_up_to_the_stated_bound(dev, kind):
+    """|b| + 0.75 |c| is 7.4 in one call and 7.6 in the other, which is refused; all
+    other bounds hold.  A singular value grows up to 4^5 = 1,024 times instead of
+    480: twice the tolerance of the default's."""
+    import paper_2102_02888_amd as ob
+    mats = ob.Matrices([(100, 160)])
+    grad, res = torch.zeros(mats.extent, device=dev), torch.zeros(mats.extent, device=dev)
+    _fill(mats, grad, [_values(dev, 100, 160, kind, 1)])
+    work = mats.workspace(dev)
+    abc = (4.0, -5.9, 2.0)
+    ob.onebit_orthogonalize(mats, grad, res, work, coefficients=abc)
+    assert _rel(mats.view(res, 0), _ortho64(mats.view(grad, 0), abc=abc)) < 2e-5
+    with pytest.raises(ob.OnebitError, match="leave the range"):
+        ob.onebit_orthogonalize(mats, grad, res, work, coefficients=(4.0, -6.1, 2.0))
+    mats.close()
