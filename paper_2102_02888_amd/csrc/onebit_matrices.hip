@@ -56,6 +56,7 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 constexpr float kScale = 8192.f;
 constexpr double kRange = 7.5;
 
+constexpr int kPartGroups = 4;  // groups of waves of the tiles whose Gram sums go in parts
 constexpr int kSlab = 64;    // fp16 numbers of an operand's row that are staged together
 constexpr int kPrep = 64;    // rows and columns of a workgroup of the first iterate
 
@@ -609,7 +610,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_product(
     const _Float16 *pa = (STEP == kGram ? x : STEP == kPoly ? d : b) + i0 * pitch;
     const _Float16 *pb = kDeep ? x + j0 * kind : (STEP == kGram ? x : d) + j0 * pitch;
     // Slabs: all of them, an even number but for tiles of 64, or this part's.
-    constexpr bool kInParts = STEP == kGram && KG > 1;
+    constexpr bool kInParts = STEP == kGram && KG == kPartGroups;
     const int all_slabs = (int)(pitch / kSlab);
     const int slab0 = kInParts ? (int)((int64_t)all_slabs * it.part / mt.parts) : 0;
     const int slabs = kInParts ? (int)((int64_t)all_slabs * (it.part + 1) / mt.parts) - slab0 : all_slabs;
@@ -1255,7 +1256,7 @@ int64_t tiles_of(const Sizes &z, const Shape &h, int pad, bool symmetric)
 int64_t part_slabs(const std::vector<Sizes> &all, const Shape &h, int pad, int kind)
 {
     constexpr int64_t kWhole = (int64_t)1 << 40;
-    if (h.groups < 4) return kWhole;
+    if (h.groups != kPartGroups) return kWhole;
     int64_t tiles = 0, longest = 0;
     for (const Sizes &z : all) {
         tiles += tiles_of(z, h, pad, true);
