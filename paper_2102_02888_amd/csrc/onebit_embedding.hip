@@ -102,7 +102,7 @@ __device__ __forceinline__ int64_t row_of(int64_t base, int per_row, int &in_row
 // few hundred places still fills the GPU's CUs.  Memory bounds it: 131,072 places
 // of 1,024 columns, fp32 table of 30,522 rows to bf16, move at least 394 MB and take
 // 76 us (5.2 TB/s; a copy of 8 GiB reaches 6.8); 10,007 places of 771, bf16 to fp32,
-// 46 MB and 8.8 us; 512 places of 1,024 are the launch alone, 7 us.
+// 46 MB and 8.8 us; 512 places of 1,024 take 2.8 us, the call around them 7.
 template <class T, class O>
 __global__ __launch_bounds__(256) void k_embedding(const T *__restrict__ table, int64_t table_ld,
                                                    int64_t vocab, int width, int per_row,
@@ -140,9 +140,11 @@ constexpr int kDigits = 256;
 // Places that one workgroup sorts, in LDS (whose size sets the limit): one launch for
 // the sort and one for the sums, where the longer way takes two for every 8 bits of
 // the id, one for the sums and one for the rows that cross pieces.  us this way and
-// that (vocabulary 30,522): 128 places of 1,024 bf16 columns 24.0 / 43.5, 1,024 of
-// them 27.4 / 46.9, 4,096 48.2 / 54.2, 4,096 of 256 29.5 / 36.8, 4,096 of 771 in fp32
-// on top of a gradient 36.3 / 37.7.
+// that (vocabulary 30,522, Zipf-distributed ids): 128 places of 1,024 bf16 columns
+// 24.3 / 42.8, 1,024 of them 26.1 / 46.9, 4,096 45.4 / 53.5, 4,096 of 256 29.1 / 36.6,
+// 4,096 of 771 in fp32 on top of a gradient 34.5 / 34.5.  The sums are one workgroup's
+// for each row and group of columns, so that a single id throughout costs more this
+// way: 128 places 31 / 43, 1,024 90 / 52, 4,096 303 / 75.
 constexpr int kSmallTokens = 4096;
 constexpr int kSmallThreads = 1024;
 constexpr int kSmallRows = 1 << 18;  // rows that the sorting workgroup has bits for
@@ -556,8 +558,9 @@ struct Raw {  // elements as they lie in memory
 
 // A thread's work is a chain: the list's entries, the rows they name, their sums.
 // (Memory bounds it where the list is long: 131,072 bf16 places of 1,024 columns,
-// fp32 gradient of 30,522 rows, move 394 MB in 81 to 91 us, 4.3 to 4.9 TB/s; 33,333 fp32
-// places of 771 columns added to 5,003 rows, 134 MB in 32 us.)
+// fp32 gradient of 30,522 rows, move 394 MB in 80 to 93 us, 4.2 to 4.9 TB/s, a third of
+// the rows zeroed in between; 33,333 fp32 places of 771 columns added to 5,003 rows, 134
+// MB in 31 us.)
 // Each part runs a batch ahead of the next: while a batch is added, the next one's
 // rows and the entries of the one after are under way.  The loads stand outside of
 // every branch (an entry that adds nothing reads row 0 instead): where their
@@ -757,10 +760,12 @@ struct GradLayout {
 size_t round_up(size_t a, size_t m) { return (a + m - 1) / m * m; }
 
 // Columns of a thread: 16 bytes of dout, or one where a row is shorter than that.
-// Places per piece: as many as still leave 2^18 threads, up to 128, which bounds
-// the partial sums and the join's chains.  us, pieces of 16 / 32 / 64 / 128:
-// 131,072 bf16 places of 1,024 columns 187 / 165 / 159 / 156, 33,333 fp32 ones of
-// 771 68 / 78 / 100 / 100 (97 threads a row).
+// Places per piece: as many as still leave 2^18 threads, from 8 to 128, which bounds
+// the partial sums and the join's chains.  us of the call, pieces of 8 / 16 / 32 / 64 /
+// 128: 131,072 bf16 places of 1,024 columns 179 / 147 / 128 / 126 / 123 (64 here), of a
+// single id 894 / 496 / 296 / 192 / 153; 33,333 fp32 ones of 771, added, 76 / 72 / 79 /
+// 95 / 140 (16; 193 threads a row); 20,000 bf16 ones of 1,024 81 / 76 / 75 / 76 / 98
+// (8).
 constexpr int kLeastPiece = 8, kMostPiece = 128;
 constexpr int64_t kPieceThreads = 1 << 18;
 

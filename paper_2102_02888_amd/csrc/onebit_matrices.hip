@@ -293,7 +293,7 @@ __device__ __forceinline__ int column(int k)
 // First iterate, X = u / (||u||_F + eps), padding zeroed: 64 x 64 of the matrix
 // for a workgroup, 8 of a row for a thread, turned in LDS where X is the transpose.
 // It is a launch of its own because the factor needs the whole norm.  Memory bounds
-// it: 302M fp32 elements to hi and lo 460 us (2.4 GB, 5.3 TB/s).
+// it: 302M fp32 elements to hi and lo 460 to 500 us (2.4 GB, 4.8 to 5.3 TB/s).
 template <bool PAIRS, class S>
 __global__ __launch_bounds__(256) void k_first(const Mat *__restrict__ mats,
                                                const Item *__restrict__ items, S src, double eps,
@@ -571,8 +571,8 @@ __device__ __forceinline__ int deep_place(int byte)
 // Measured on that list (96 of 1,024 x 1,024, 24 of 4,096 x 1,024, 24 of 1,024 x 4,096;
 // us, and the share of the time that the matrix cores are busy):
 //            gram       poly       next        last
-//   pairs    970 66%    607 55%    1,672 66%   1,952 56%
-//   halves   437 53%    268 44%      867 44%     836 45%
+//   pairs    963 67%    608 55%    1,683 67%   1,625 69%  (of a Muon step 1,913 56%)
+//   halves   434 54%    256 44%      861 43%     816 45%
 // There is no LDS bank conflict but in the last one's turned tiles.  What bounds
 // pairs is the matrix cores in the slabs and memory in the epilogue, which one tile's
 // products cannot hide where it has its CU to itself; for halves, with a third of the
