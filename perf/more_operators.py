@@ -225,8 +225,6 @@ def prepare(case, seed):
             teacher = other.topk(min(k, vocab), dim=1)
             s["t_ids"] = teacher.indices.contiguous()
             s["t_logits"] = teacher.values.to(s["logits"].dtype).contiguous()
-        if own:
-            s["work"] = s["ob"].logprobs_workspace(rows, vocab, dev)
     return s
 
 
@@ -256,21 +254,21 @@ def _run_own(s):
                                  causal=case["causal"])
         return {"out": s["out"], "dqkv": s["dqkv"]}
     if kind == "logp" and not case["grad"]:
-        ob.onebit_logprobs_forward(s["logits"], s["ids"], s["value"], s["work"],
-                                   scale=case["scale"], entropy=s["entropy"],
-                                   top_ids=s["top_ids"], top_logprobs=s["top_logprobs"])
+        ob.onebit_logprobs_forward(s["logits"], s["ids"], s["value"], scale=case["scale"],
+                                   entropy=s["entropy"], top_ids=s["top_ids"],
+                                   top_logprobs=s["top_logprobs"])
         return {"logprobs": s["value"], "entropy": s["entropy"], "top_ids": s["top_ids"],
                 "top_logprobs": s["top_logprobs"]}
     if kind == "logp":
-        ob.onebit_logprobs_grad(s["logits"], s["ids"], s["weight"], s["dlogits"], s["work"],
+        ob.onebit_logprobs_grad(s["logits"], s["ids"], s["weight"], s["dlogits"],
                                 scale=case["scale"], logprobs=s["value"])
         return {"logprobs": s["value"], "dlogits": s["dlogits"]}
     if not case["grad"]:
-        ob.onebit_distill_forward(s["logits"], s["t_ids"], s["t_logits"], s["value"], s["work"],
+        ob.onebit_distill_forward(s["logits"], s["t_ids"], s["t_logits"], s["value"],
                                   scale=case["scale"])
         return s["value"]
     ob.onebit_distill_grad(s["logits"], s["t_ids"], s["t_logits"], s["weight"], s["dlogits"],
-                           s["work"], scale=case["scale"], loss=s["value"])
+                           scale=case["scale"], loss=s["value"])
     return {"loss": s["value"], "dlogits": s["dlogits"]}
 
 
