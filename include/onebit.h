@@ -500,6 +500,108 @@ int onebit_muon_step(onebit_matrices mats, float *x, float *m, const void *grads
                      int32_t products, int32_t steps, const float *coefficients, float eps,
                      void *workspace, onebit_stream stream);
 
+/* ---------------------------------------------------------------------------
+ * Layer norm
+ * ---------------------------------------------------------------------------
+ * z = (x - mean(x)) / sqrt(var(x) + eps) of each row, var the mean of the squared
+ * differences; y = z * weight + bias.  weight and bias hold `width` elements of
+ * w_dtype, such as a tensor inside the flat parameters, or are NULL (1 and 0).
+ * Element types are ONEBIT_GRAD_*; pointers and leading dimensions need no
+ * alignment beyond the element's own.  Statistics and sums are fp32, the mean being
+ * taken twice, so that rows far off zero lose nothing; results are rounded once.
+ * A NaN or an infinity in a row makes that row NaN.  width is at most 16,384;
+ * rows = 0 and width = 0 are allowed. */
+
+/* Errors: EINVAL (null, rows below 0 or 2^31 and above, a width out of range, a
+ * leading dimension below width with more than one row, unknown type, eps below 0 or
+ * not finite), EALIGN, EHIP. */
+int onebit_layer_norm_forward(const void *x, int32_t x_dtype, int64_t x_ld, int64_t rows,
+                              int64_t width, const void *weight, const void *bias,
+                              int32_t w_dtype, float eps, void *y, int32_t y_dtype, int64_t y_ld,
+                              onebit_stream stream);
+
+/* Bytes of workspace that onebit_layer_norm_grad needs for at most this many rows and
+ * columns.  Errors: EINVAL (as above, bytes NULL). */
+int onebit_layer_norm_grad_workspace(int64_t rows, int64_t width, size_t *bytes);
+
+/* With g = dy * weight and r = 1 / sqrt(var + eps), of each row
+ *   dx = r (g - mean(g) - z mean(g z))
+ * and, over the rows, dweight = sum of dy z, dbias = sum of dy; with accumulate != 0
+ * the sums are added to dweight and dbias instead.  The statistics are formed from x
+ * again, in the same pass.  Sums over the rows are added in an order that depends on
+ * the sizes alone (no atomics); one rounding to the gradient's type, after the old
+ * value is added in fp32.  dx: x's type; it may be dy's own buffer (same type and ld).
+ * dx, dweight and dbias may be NULL, where they are not wanted.  workspace:
+ * onebit_layer_norm_grad_workspace() bytes, 16-byte aligned (NULL without dweight and
+ * dbias).  Errors: EINVAL, EALIGN, EHIP. */
+int onebit_layer_norm_grad(const void *dy, int32_t dy_dtype, int64_t dy_ld, const void *x,
+                           int32_t x_dtype, int64_t x_ld, int64_t rows, int64_t width,
+                           const void *weight, int32_t w_dtype, float eps, void *dx,
+                           int64_t dx_ld, void *dweight, void *dbias, int32_t dw_dtype,
+                           int32_t accumulate, void *workspace, onebit_stream stream);
+
+/* ---------------------------------------------------------------------------
+ * Losses over a vocabulary's logits
+ * ---------------------------------------------------------------------------
+ * logits: `rows` rows of `vocab` elements of an ONEBIT_GRAD_* type, ld apart;
+ * p = softmax(scale * logits), scale (one over the temperature) in (0, 1e30].
+ * Pointers and leading dimensions need no alignment beyond the element's own.
+ * Statistics are fp32.  A logit of -infinity has no probability, one of the type's
+ * lowest number next to none unless all are; a row without a logit above -infinity
+ * has no distribution: log-probabilities -infinity, entropy 0, gradient 0.  A NaN or
+ * a logit of +infinity makes its row NaN.  Each call is one launch (per 2^21 rows),
+ * needs no workspace, and reads every row once up to 65,536 logits.  vocab is at most
+ * 2^30; rows = 0 and vocab = 0 are allowed. */
+
+/* logprobs[r] = log p of token ids[r], 0 where the id lies outside [0, vocab) (a place
+ * that holds no token); entropy[r] = -sum of p log p; and the `top` (0 to 64) largest
+ * logits of each row, in order, the lowest index first among equal ones and NaN above
+ * all: their indices in top_ids (rows x top, integers of ids_bytes) and log p in
+ * top_logprobs (rows x top).  Where vocab < top, -1 and -infinity fill the rest.
+ * Outputs that are NULL are left out; ids may be NULL without logprobs.
+ * Errors: EINVAL (null, a size out of range, a leading dimension below vocab with more
+ * than one row, unknown type, scale or top out of range), EALIGN, EHIP. */
+int onebit_logprobs_forward(const void *logits, int32_t dtype, int64_t ld, int64_t rows,
+                            int64_t vocab, const void *ids, int32_t ids_bytes, float scale,
+                            float *logprobs, float *entropy, int32_t top, void *top_ids,
+                            float *top_logprobs, onebit_stream stream);
+
+/* The logits' gradient of  sum over r of grad_logprobs[r] logprobs[r] + grad_entropy[r]
+ * entropy[r]  (either may be NULL, for zeros):
+ *   dlogits[r][v] = scale (g ([v = ids[r]] - p_v) - h p_v (log p_v + entropy[r])),
+ * and zeros for a row whose id lies outside the vocabulary.  It needs nothing of the
+ * forward call, and gives logprobs and entropy itself where they are not NULL, so that
+ * a training step whose weights are known takes this call alone.  dlogits: logits'
+ * type, d_ld apart; it may be the logits' own buffer (same ld).
+ * Errors: as above. */
+int onebit_logprobs_grad(const void *logits, int32_t dtype, int64_t ld, int64_t rows,
+                         int64_t vocab, const void *ids, int32_t ids_bytes, float scale,
+                         const float *grad_logprobs, const float *grad_entropy, void *dlogits,
+                         int64_t d_ld, float *logprobs, float *entropy, onebit_stream stream);
+
+/* Distillation from a teacher's top logits.  teacher_ids (rows x top integers of
+ * ids_bytes) and teacher_logits (rows of `top` elements of teacher_dtype, teacher_ld
+ * apart; 1 to 256) name alternatives; q = softmax(scale * teacher_logits) over those of
+ * a row whose id lies in [0, vocab), and
+ *   loss[r] = sum over k of q_k (log q_k - log p of token teacher_ids[r][k]),
+ * terms with q_k = 0 left out; 0 for a row without an alternative whose logit is above
+ * -infinity.  A token may be named more than once.
+ * Errors: EINVAL (as above; top out of range), EALIGN, EHIP. */
+int onebit_distill_forward(const void *logits, int32_t dtype, int64_t ld, int64_t rows,
+                           int64_t vocab, const void *teacher_ids, int32_t ids_bytes,
+                           const void *teacher_logits, int32_t teacher_dtype, int64_t teacher_ld,
+                           int32_t top, float scale, float *loss, onebit_stream stream);
+
+/* The logits' gradient of the sum over r of grad_loss[r] loss[r]:
+ *   dlogits[r][v] = scale grad_loss[r] (p_v - sum of q_k over teacher_ids[r][k] = v),
+ * zeros for a row without an alternative; the teacher gets none.  Gives the loss too
+ * where it is not NULL.  dlogits as in onebit_logprobs_grad.  Errors: as above. */
+int onebit_distill_grad(const void *logits, int32_t dtype, int64_t ld, int64_t rows,
+                        int64_t vocab, const void *teacher_ids, int32_t ids_bytes,
+                        const void *teacher_logits, int32_t teacher_dtype, int64_t teacher_ld,
+                        int32_t top, float scale, const float *grad_loss, void *dlogits,
+                        int64_t d_ld, float *loss, onebit_stream stream);
+
 /* Name of a status code (static string). */
 const char *onebit_status_str(int32_t status);
 

@@ -13,9 +13,15 @@ from .embedding import (  # noqa: F401
     embedding_workspace, onebit_embedding_forward, onebit_embedding_grad,
 )
 from .freeze import VarianceFreezeDetector  # noqa: F401
+from .loss import (  # noqa: F401
+    onebit_distill_forward, onebit_distill_grad, onebit_logprobs_forward, onebit_logprobs_grad,
+)
 from .muon import (  # noqa: F401
     Matrices, Muon, MUON_SCALE_NONE, MUON_SCALE_RMS, MUON_SCALE_SPECTRAL, PRODUCTS_F16,
     PRODUCTS_F32, matrices_kernels, onebit_muon_step, onebit_orthogonalize, products_for,
+)
+from .norm import (  # noqa: F401
+    layer_norm_workspace, onebit_layer_norm_forward, onebit_layer_norm_grad,
 )
 from .optimizer import OnebitAdam  # noqa: F401
 from ._native import OnebitError, lib  # noqa: F401

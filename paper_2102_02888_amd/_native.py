@@ -65,6 +65,19 @@ SIGNATURES = {
     "onebit_orthogonalize": [_vp, _vp, _i32, _vp, _i32, _i32, _i32, _vp, _f32, _vp, _vp],
     "onebit_muon_step": [_vp, _vp, _vp, _vp, _i32, _i64, _i32, _f32, _f32, _i32, _f32, _i32, _i32,
                          _i32, _vp, _f32, _vp, _vp],
+    "onebit_layer_norm_forward": [_vp, _i32, _i64, _i64, _i64, _vp, _vp, _i32, _f32, _vp, _i32,
+                                  _i64, _vp],
+    "onebit_layer_norm_grad_workspace": [_i64, _i64, _vp],
+    "onebit_layer_norm_grad": [_vp, _i32, _i64, _vp, _i32, _i64, _i64, _i64, _vp, _i32, _f32, _vp,
+                               _i64, _vp, _vp, _i32, _i32, _vp, _vp],
+    "onebit_logprobs_forward": [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _f32, _vp, _vp, _i32, _vp,
+                                _vp, _vp],
+    "onebit_logprobs_grad": [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _f32, _vp, _vp, _vp, _i64,
+                             _vp, _vp, _vp],
+    "onebit_distill_forward": [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _i32, _i64, _i32,
+                               _f32, _vp, _vp],
+    "onebit_distill_grad": [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _i32, _i64, _i32, _f32,
+                            _vp, _vp, _i64, _vp, _vp],
     "onebit_status_str": [_i32],
     "onebit_last_error": [],
 }

@@ -59,6 +59,20 @@ def _ids(ids):
     return ids.data_ptr(), _ID_BYTES[ids.dtype], ids.numel()
 
 
+def _workspace(workspace, size, *sizes):
+    """Pointer of a workspace that holds what the call named `size` says."""
+    if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda \
+            or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous GPU tensor")
+    _one_device(workspace)
+    need = ctypes.c_size_t()
+    call(size, *sizes, ctypes.byref(need))
+    if workspace.numel() * workspace.element_size() < need.value:
+        raise ValueError("workspace has %d bytes; the call needs %d"
+                         % (workspace.numel() * workspace.element_size(), need.value))
+    return workspace.data_ptr()
+
+
 def _one_device(*tensors):
     """The calls run on the current device, where all tensors have to be."""
     here = torch.cuda.current_device()
@@ -95,15 +109,8 @@ def onebit_embedding_grad(grad_out, ids, grad_table, workspace, scale=1.0, paddi
     if grad_table.dim() != 2:
         raise ValueError("grad_table must be 2-D")
     dp, dcode, dld, _, _ = _matrix(grad_out, "grad_out", tokens, width)
-    if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda \
-            or not workspace.is_contiguous():
-        raise TypeError("workspace must be a contiguous GPU tensor")
-    _one_device(grad_out, ids, grad_table, workspace)
-    need = ctypes.c_size_t()
-    call("onebit_embedding_grad_workspace", tokens, vocab, width, ctypes.byref(need))
-    if workspace.numel() * workspace.element_size() < need.value:
-        raise ValueError("workspace has %d bytes; the call needs %d"
-                         % (workspace.numel() * workspace.element_size(), need.value))
+    _one_device(grad_out, ids, grad_table)
+    work = _workspace(workspace, "onebit_embedding_grad_workspace", tokens, vocab, width)
     call("onebit_embedding_grad", dp, dcode, dld, ip, ib, tokens, vocab, width,
          int(-1 if padding_idx is None else padding_idx), float(scale), gp, gcode, gld,
-         int(bool(accumulate)), workspace.data_ptr(), _stream(stream))
+         int(bool(accumulate)), work, _stream(stream))
