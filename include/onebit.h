@@ -602,6 +602,56 @@ int onebit_distill_grad(const void *logits, int32_t dtype, int64_t ld, int64_t r
                         int32_t top, float scale, const float *grad_loss, void *dlogits,
                         int64_t d_ld, float *loss, onebit_stream stream);
 
+/* ---------------------------------------------------------------------------
+ * Attention over packed sequences
+ * ---------------------------------------------------------------------------
+ * q, k, v, out: a row per token, ld elements apart, that holds its heads one after
+ * another, `dim` (1 to 128) elements each: `heads` of q and out, `kv_heads` of k and v,
+ * each of which serves heads / kv_heads heads in turn.  They may be parts of one
+ * projection's rows.  All are of one type, ONEBIT_GRAD_BF16 or ONEBIT_GRAD_F16 (the
+ * matrix cores' operands); pointers and leading dimensions need no alignment beyond
+ * the element's own.  Sequence s is the tokens starts[s] to starts[s + 1] - 1 (device
+ * array of sequences + 1 int32, not decreasing, in [0, tokens]; what lies outside that
+ * range is cut off); it may be empty.  A token sees its own sequence, up to itself
+ * with causal != 0:
+ *   out_i = sum over j of P_ij v_j,  P_i = softmax over j of scale q_i k_j.
+ * Scores, their exponentials and all sums are fp32, P and its gradient are rounded to
+ * the operands' type between two products.  Tokens in no sequence are neither read
+ * nor written.  A NaN or an infinity among a sequence's numbers may make any result of
+ * that sequence and head NaN; others are not touched by it. */
+
+/* lse (may be NULL): tokens x heads floats, the logarithm of the sum over j of
+ * exp(scale q_i k_j).  scale is in (0, 1e30].
+ * Errors: EINVAL (null, tokens or sequences below 0 or above 2^30, heads no multiple
+ * of kv_heads or above 2^14, dim out of range, another type, a leading dimension below
+ * a row's width with more than one token, more than 2^24 workgroups), EALIGN, EHIP. */
+int onebit_attention_forward(const void *q, int64_t q_ld, const void *k, int64_t k_ld,
+                             const void *v, int64_t v_ld, int32_t dtype, int64_t tokens,
+                             int32_t heads, int32_t kv_heads, int32_t dim, const int32_t *starts,
+                             int64_t sequences, int32_t causal, float scale, void *out,
+                             int64_t out_ld, float *lse, onebit_stream stream);
+
+/* Bytes of workspace that onebit_attention_grad needs for at most this many tokens and
+ * heads.  Errors: EINVAL (as above, bytes NULL). */
+int onebit_attention_grad_workspace(int64_t tokens, int32_t heads, size_t *bytes);
+
+/* The gradients of sum of dout out: with D_i = dout_i out_i and
+ * dS_ij = P_ij (dout_i v_j - D_i),
+ *   dv_j = sum over i of P_ij dout_i, dq_i = scale sum over j of dS_ij k_j,
+ *   dk_j = scale sum over i of dS_ij q_i,
+ * dk and dv over all heads that share them.  out and lse are the forward call's.  No
+ * atomics: results are the same bit for bit from call to call.  With ONEBIT_GRAD_F16
+ * dS is scaled by a power of two from the largest magnitude in dout before it is
+ * rounded.  dq, dk, dv: of the same type, written for the tokens of the sequences; they
+ * may be parts of one buffer's rows.  workspace: 16-byte aligned.  Errors: as above. */
+int onebit_attention_grad(const void *dout, int64_t dout_ld, const void *q, int64_t q_ld,
+                          const void *k, int64_t k_ld, const void *v, int64_t v_ld,
+                          const void *out, int64_t out_ld, const float *lse, int32_t dtype,
+                          int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim,
+                          const int32_t *starts, int64_t sequences, int32_t causal, float scale,
+                          void *dq, int64_t dq_ld, void *dk, int64_t dk_ld, void *dv,
+                          int64_t dv_ld, void *workspace, onebit_stream stream);
+
 /* Name of a status code (static string). */
 const char *onebit_status_str(int32_t status);
 

@@ -9,6 +9,9 @@ from .onebit import (  # noqa: F401
     onebit_server_reduce_compress, onebit_step, onebit_step_noalloc, onebit_warmup_adam_step,
     onebit_worker_compress, onebit_uncompressed_step, onebit_adam_message_step, onebit_l1_norm,
 )
+from .attention import (  # noqa: F401
+    attention_workspace, onebit_attention_forward, onebit_attention_grad,
+)
 from .embedding import (  # noqa: F401
     embedding_workspace, onebit_embedding_forward, onebit_embedding_grad,
 )

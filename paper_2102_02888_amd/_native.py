@@ -78,6 +78,12 @@ SIGNATURES = {
                                _f32, _vp, _vp],
     "onebit_distill_grad": [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _i32, _i64, _i32, _f32,
                             _vp, _vp, _i64, _vp, _vp],
+    "onebit_attention_forward": [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _i64, _i32, _i32, _i32,
+                                 _vp, _i64, _i32, _f32, _vp, _i64, _vp, _vp],
+    "onebit_attention_grad_workspace": [_i64, _i32, _vp],
+    "onebit_attention_grad": [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32,
+                              _i64, _i32, _i32, _i32, _vp, _i64, _i32, _f32, _vp, _i64, _vp, _i64,
+                              _vp, _i64, _vp, _vp],
     "onebit_status_str": [_i32],
     "onebit_last_error": [],
 }

@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("onebit_kernels.hip", "onebit_abi.hip",
                                                    "onebit_embedding.hip", "onebit_matrices.hip",
-                                                   "onebit_norm.hip", "onebit_loss.hip")]
+                                                   "onebit_norm.hip", "onebit_loss.hip",
+                                                   "onebit_attention.hip")]
 LIB = os.path.join(HERE, "lib", "libonebit.so")
 ARGS_SOURCE = os.path.join(HERE, "csrc", "binding_args.cpp")
 PROBE_SOURCE = os.path.join(HERE, "csrc", "hbm_probe.hip")
