@@ -108,47 +108,128 @@ __device__ __forceinline__ vec8<T> load8(const T *row, int at, int dim, bool the
     return v;
 }
 
-// A tile of kTile rows of DP numbers in LDS, 16 bytes between rows so that 16 lanes
-// with a row each reach all banks.
+typedef __attribute__((address_space(3))) void lds_void;
+
+// 16 bytes per lane, from `at` bytes behind `base` (the same in all lanes) to consecutive
+// places from `lds` on; zeros from `bytes` on.  (The host compiler, which only needs the
+// kernels' names, does not take the builtin at this size.)
+__device__ __forceinline__ void load_to_lds(const void *base, uint32_t bytes, char *lds, int at)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const uint64_t a = (uint64_t)base;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+        (void *)(((uint64_t)hi << 32) | lo), (short)0, __builtin_amdgcn_readfirstlane(bytes),
+        0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)lds, 16, at, 0, 0, 0);
+#endif
+}
+
+// A tile of kTile rows of DP numbers in LDS, in pieces of 16 bytes.  A row's pieces are
+// permuted so that neither 16 rows' same piece nor 4 rows' 64 bytes share a bank:
+// piece p of row r is at place p ^ turned(r).
+template <int DP>
+__device__ __forceinline__ int turned(int r)
+{
+    if constexpr (DP == 128) return (r & 3) << 2 | (r >> 2 & 3);
+    if constexpr (DP == 64) return (r >> 1 & 1) << 2 | (r >> 2 & 3);
+    return r >> 2 & 3;  // rows of 64 or 192 bytes lie in different banks by fours
+}
+
 template <class T, int DP>
 struct Tile {
-    static constexpr int kPitch = DP * 2 + 16, kBytes = kTile * kPitch;
-    static constexpr int kEach = kTile * (DP / 8) / kThreads;  // pieces of a thread
-    vec8<T> held[kEach];
-    // rows `at` and on of `rows`, into registers
-    __device__ __forceinline__ void load(const T *base, int64_t ld, int at, int rows, int dim)
+    static constexpr int kPitch = DP * 2, kBytes = kTile * kPitch, kPieces = DP / 8;
+    // A lane's places in a fragment: rows() of 32 rows, columns() of 16.
+    int row_at, low_at, high_at;
+    __device__ __forceinline__ Tile()
     {
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            const int piece = threadIdx.x + k * kThreads, row = at + piece / (DP / 8);
-            held[k] = load8(base + (int64_t)row * ld, piece % (DP / 8) * 8, dim, row < rows);
-        }
+        const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
+        row_at = column() * kPitch + (upper() ^ turned<DP>(column())) * 16;
+        const int r = 4 * (g >> 1) + (j >> 2), p = (g & 1) * 2 + (j >> 1 & 1), in = (j & 1) * 8;
+        low_at = r * kPitch + (p ^ turned<DP>(r)) * 16 + in;
+        high_at = (r + 8) * kPitch + (p ^ turned<DP>(r + 8)) * 16 + in;
     }
-    __device__ __forceinline__ void store(char *lds) const
+    // ... `pieces` further on in the row (the places of rows of 192 bytes are permuted
+    // by fours of pieces alone)
+    static __device__ __forceinline__ int further(int at, int pieces)
     {
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            const int piece = threadIdx.x + k * kThreads;
-            *(vec8<T> *)(lds + piece / (DP / 8) * kPitch + piece % (DP / 8) * 16) = held[k];
-        }
+        if constexpr (DP == 96) return (at ^ (pieces & 3) * 16) + (pieces >> 2) * 64;
+        return at ^ pieces * 16;
     }
     // First operand, rows of the tile: 32 from `row` on, numbers 16 k and on.
-    static __device__ __forceinline__ vec8<T> rows(const char *lds, int row, int k)
+    __device__ __forceinline__ vec8<T> rows(const char *lds, int row, int k) const
     {
-        return *(const vec8<T> *)(lds + (row + column()) * kPitch + (k * 16 + upper() * 8) * 2);
+        return *(const vec8<T> *)(lds + row * kPitch + further(row_at, 2 * k));
     }
     // First operand, the tile's columns: 32 from 32 c on, over 16 rows from `row` on, in
     // the order of the scores (above).  A transposing read takes 4 rows x 16 columns
     // per 16 lanes.
-    static __device__ __forceinline__ vec8<T> columns(const char *lds, int row, int c)
+    __device__ __forceinline__ vec8<T> columns(const char *lds, int row, int c) const
     {
-        const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
-        const char *at = lds + (row + 4 * (g >> 1) + (j >> 2)) * kPitch +
-                         (c * 32 + (g & 1) * 16 + (j & 3) * 4) * 2;
-        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)at);
+        const char *at = lds + row * kPitch;
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) v4s *)(at + further(low_at, 4 * c)));
         const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) v4s *)(at + 8 * kPitch));
+            (__attribute__((address_space(3))) v4s *)(at + further(high_at, 4 * c)));
         return __builtin_bit_cast(vec8<T>, (v8s)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+// Brings tiles of a side's rows to LDS, by WAVES waves of which this is the `wave`-th.
+// DIRECT: rows of whole pieces on 4-byte borders, straight from memory to LDS, every wave
+// 1 KB at a time; what is not there is read as zero by the buffer's bound.  Otherwise
+// through registers, number by number at a row's end.  start() begins a tile's loads,
+// finish() ends them (a barrier has to follow).
+template <class T, int DP, int WAVES, bool DIRECT>
+struct Loader {
+    static constexpr int kEach = kTile * (DP / 8) / (WAVES * 64);  // pieces of a thread
+    int wave, at[DIRECT ? kEach : 1];
+    vec8<T> held[DIRECT ? 1 : kEach];
+    __device__ __forceinline__ int piece(int k) const
+    {
+        return (k * WAVES + wave) * 64 + (threadIdx.x & 63);
+    }
+    __device__ __forceinline__ Loader(int w, int64_t ld, int dim) : wave(w)
+    {
+        if constexpr (DIRECT) {
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                const int row = piece(k) / (DP / 8);
+                const int from = (piece(k) % (DP / 8) ^ turned<DP>(row)) * 8;
+                at[k] = from < dim ? (row * (int)ld + from) * 2 : (int)0x80000000;
+            }
+        }
+    }
+    // rows `first` and on of the `rows` at base
+    __device__ __forceinline__ void start(const T *base, int64_t ld, int dim, int first, int rows,
+                                          char *lds)
+    {
+        if constexpr (DIRECT) {
+            const int64_t bytes = ((rows - 1 - first) * ld + dim) * 2;
+            const uint32_t bound = (uint32_t)(bytes < 0x7fffffff ? bytes : 0x7fffffff);
+#pragma unroll
+            for (int k = 0; k < kEach; ++k)
+                load_to_lds(base + first * ld, bound, lds + (k * WAVES + wave) * 1024, at[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                const int row = first + piece(k) / (DP / 8);
+                held[k] = load8(base + (int64_t)row * ld, piece(k) % (DP / 8) * 8, dim, row < rows);
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(char *lds) const
+    {
+        if constexpr (DIRECT) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        } else {
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                const int row = piece(k) / (DP / 8);
+                *(vec8<T> *)(lds + row * DP * 2 + (piece(k) % (DP / 8) ^ turned<DP>(row)) * 16) = held[k];
+            }
+        }
     }
 };
 
@@ -156,10 +237,13 @@ struct Tile {
 template <class T>
 __device__ __forceinline__ vec8<T> narrow(const f32x16 &s, int half)
 {
-    vec8<T> v;
+    typedef float pair __attribute__((ext_vector_type(2)));
+    typedef T narrow_pair __attribute__((ext_vector_type(2)));
+    narrow_pair v[4];  // (two at a time, an instruction each)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = (T)s[half * 8 + k];
-    return v;
+    for (int k = 0; k < 4; ++k)
+        v[k] = __builtin_convertvector((pair{s[half * 8 + 2 * k], s[half * 8 + 2 * k + 1]}), narrow_pair);
+    return __builtin_bit_cast(vec8<T>, v);
 }
 
 // Both halves' values of a column.
@@ -194,130 +278,157 @@ __device__ __forceinline__ void store_column(T *to, const f32x16 (&acc)[DP / 32]
         }
 }
 
-// out = softmax(scale q k') v for QB * 32 queries of a wave, one pass over the keys
-// with a running maximum m and sum l per query (both halves of a wave have a query; m
-// is the same in both, l adds up at the end).
-template <class T, int DP, int QB>
-__global__ __launch_bounds__(kThreads) void k_attention(const T *__restrict__ q,
-                                                        const T *__restrict__ k,
-                                                        const T *__restrict__ v, Sides s,
-                                                        T *__restrict__ out,
-                                                        float *__restrict__ lse, int tiles)
+// How a workgroup's four waves share its work: WR of them have 32 rows each (queries, or
+// keys for dk and dv), and WS streams of waves take every WS-th tile of the other side,
+// whose sums are joined at the end.  Each stream has its tiles in LDS, NB deep.
+template <int DP, int WR, int NB>
+struct Share {
+    static constexpr int kStreams = kWaves / WR, kRows = 32 * WR;
+    static constexpr int kTileBytes = kTile * DP * 2, kLds = kStreams * NB * 2 * kTileBytes;
+    static_assert(kStreams * WR == kWaves && (kWaves - WR) * DP * 32 * 4 <= kLds, "sums are joined in LDS");
+};
+
+// Brings what the streams' waves have of the same rows to the first stream's wave: take(i)
+// gets the number of a lane of each other stream's wave where give has put it.  COUNT
+// numbers per lane, in LDS (which no wave reads for anything else any more).
+template <int WR, int COUNT, class Give, class Take>
+__device__ __forceinline__ void join_streams(char *lds, int stream, int row_wave, Give give, Take take)
 {
-    using Kv = Tile<T, DP>;
-    constexpr int kRows = kWaves * 32 * QB;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][Kv::kBytes];
+    constexpr int kStreams = kWaves / WR;
+    float *at = (float *)lds + (threadIdx.x & 63);
+    if (stream > 0) {
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k) at[(((stream - 1) * WR + row_wave) * COUNT + k) * 64] = give(k);
+    }
+    __syncthreads();
+    if (stream == 0)
+        for (int other = 1; other < kStreams; ++other) {
+            const float *from = at + ((other - 1) * WR + row_wave) * COUNT * 64;
+            take([&](int k) { return from[k * 64]; });
+        }
+}
+
+// out = softmax(scale q k') v for 32 queries of a wave, one pass over the keys with a
+// running maximum m and sum l per query (both halves of a wave have a query; m is the
+// same in both, l adds up at the end).
+template <class T, int DP, int WR, int NB, bool DIRECT>
+__global__ __launch_bounds__(kThreads, 2) void k_attention(const T *__restrict__ q,
+                                                           const T *__restrict__ k,
+                                                           const T *__restrict__ v, Sides s,
+                                                           T *__restrict__ out,
+                                                           float *__restrict__ lse, int tiles)
+{
+    using W = Share<DP, WR, NB>;
+    const Tile<T, DP> tile_at;
+    __shared__ __attribute__((aligned(1024))) char lds[W::kLds];
     const int head = blockIdx.x % s.heads, tile = tiles - 1 - blockIdx.x / s.heads;
-    const Range in = find_sequence(s, tile, kRows);
+    const Range in = find_sequence(s, tile, W::kRows);
     if (in.at < 0 || in.at >= in.length) return;
-    const int wave = wave_number(), row0 = in.at + wave * 32 * QB;
+    const int wave = wave_number(), stream = wave / WR, row0 = in.at + wave % WR * 32;
     const int kv = head / (s.heads / s.kv_heads);
     const T *kp = k + in.first * s.k_ld + kv * s.dim, *vp = v + in.first * s.v_ld + kv * s.dim;
-    vec8<T> qf[QB][DP / 16];
+    const int keys = s.causal ? min(in.length, in.at + W::kRows) : in.length;
+    char *const own = lds + stream * NB * 2 * W::kTileBytes;
+    const auto buffer = [&](int turn, int side) { return own + (turn * 2 + side) * W::kTileBytes; };
+    Loader<T, DP, WR, DIRECT> kt(wave % WR, s.k_ld, s.dim), vt(wave % WR, s.v_ld, s.dim);
+    const auto start = [&](int at, int turn) {
+        if (at >= keys) return;
+        kt.start(kp, s.k_ld, s.dim, at, in.length, buffer(turn, 0));
+        vt.start(vp, s.v_ld, s.dim, at, in.length, buffer(turn, 1));
+    };
+    const auto finish = [&](int at, int turn) {
+        if (at >= keys) return;
+        kt.finish(buffer(turn, 0));
+        vt.finish(buffer(turn, 1));
+    };
+    start(stream * kTile, 0);
+    const int row = row0 + column();
+    const int64_t token = in.first + row;
+    vec8<T> qf[DP / 16];
 #pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        const int row = row0 + b * 32 + column();
-        const T *qp = q + (int64_t)(in.first + row) * s.q_ld + head * s.dim;
-#pragma unroll
-        for (int c = 0; c < DP / 16; ++c)
-            qf[b][c] = load8(qp, c * 16 + upper() * 8, s.dim, row < in.length);
-    }
-    const int keys = s.causal ? min(in.length, in.at + kRows) : in.length;
+    for (int d = 0; d < DP / 16; ++d)
+        qf[d] = load8(q + token * s.q_ld + head * s.dim, d * 16 + upper() * 8, s.dim, row < in.length);
     const float c = s.scale * kLog2e;
-    f32x16 o[QB][DP / 32] = {};
-    float m[QB], l[QB];
-#pragma unroll
-    for (int b = 0; b < QB; ++b) m[b] = -INFINITY, l[b] = 0.f;
-    Kv kt, vt;
-    kt.load(kp, s.k_ld, 0, in.length, s.dim);
-    vt.load(vp, s.v_ld, 0, in.length, s.dim);
-    kt.store(lds[0][0]);
-    vt.store(lds[0][1]);
+    f32x16 o[DP / 32] = {};
+    float m = -INFINITY, l = 0.f;
+    finish(stream * kTile, 0);
     __syncthreads();
-    for (int at = 0, turn = 0; at < keys; at += kTile, turn ^= 1) {
-        const bool more = at + kTile < keys;
-        if (more) {
-            kt.load(kp, s.k_ld, at + kTile, in.length, s.dim);
-            vt.load(vp, s.v_ld, at + kTile, in.length, s.dim);
-        }
+    constexpr int kStep = W::kStreams * kTile;
+    for (int first = 0, turn = 0; first < keys; first += kStep) {
+        const int at = first + stream * kTile;
+        if (NB > 1) start(at + kStep, turn ^ 1);
         // (with the mask, a tile that a wave does not skip leaves each of its rows a key)
-        if (!(s.causal && at > row0 + 32 * QB - 1)) {
-            f32x16 p[QB][2] = {};
+        if (at < keys && !(s.causal && at > row0 + 31)) {
+            f32x16 p[2] = {};
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int d = 0; d < DP / 16; ++d) {
-                    const vec8<T> f = Kv::rows(lds[turn][0], h * 32, d);
-#pragma unroll
-                    for (int b = 0; b < QB; ++b) p[b][h] = mma(f, qf[b][d], p[b][h]);
-                }
+                for (int d = 0; d < DP / 16; ++d)
+                    p[h] = mma(tile_at.rows(buffer(turn, 0), h * 32, d), qf[d], p[h]);
             if (at + kTile > in.length || (s.causal && at + kTile - 1 > row0)) {
+                const int end = s.causal ? min(in.length, row + 1) : in.length;
 #pragma unroll
-                for (int b = 0; b < QB; ++b) {
-                    const int row = row0 + b * 32 + column();
-                    const int end = s.causal ? min(in.length, row + 1) : in.length;
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                    for (int i = 0; i < 16; ++i)
+                        if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) >= end) p[h][i] = -INFINITY;
+            }
+            float most = p[0][0];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) >= end)
-                                p[b][h][i] = -INFINITY;
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, p[h][i]);
+            most = fmaxf(m, both_halves(most, [](float x, float y) { return fmaxf(x, y); }));
+            const float alpha = __builtin_amdgcn_exp2f((m - most) * c), mc = most * c;
+            m = most;
+            float sum = 0.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    p[h][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[h][i], c, -mc));
+                    sum += p[h][i];
                 }
-            }
+            l = __builtin_fmaf(l, alpha, sum);
+            if (__ballot(alpha != 1.f))
 #pragma unroll
-            for (int b = 0; b < QB; ++b) {
-                const auto larger = [](float x, float y) { return fmaxf(x, y); };
-                float most = p[b][0][0];
+                for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) most = fmaxf(most, p[b][h][i]);
-                most = fmaxf(m[b], both_halves(most, larger));
-                const float alpha = __builtin_amdgcn_exp2f((m[b] - most) * c), mc = most * c;
-                m[b] = most;
-                float sum = 0.f;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        p[b][h][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[b][h][i], c, -mc));
-                        sum += p[b][h][i];
-                    }
-                l[b] = __builtin_fmaf(l[b], alpha, sum);
-                if (__ballot(alpha != 1.f))
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[b][d][i] *= alpha;
-            }
+                    for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-                vec8<T> pf[QB];
+                const vec8<T> pf = narrow<T>(p[h / 2], h % 2);
 #pragma unroll
-                for (int b = 0; b < QB; ++b) pf[b] = narrow<T>(p[b][h / 2], h % 2);
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) {
-                    const vec8<T> f = Kv::columns(lds[turn][1], h * 16, d);
-#pragma unroll
-                    for (int b = 0; b < QB; ++b) o[b][d] = mma(f, pf[b], o[b][d]);
-                }
+                for (int d = 0; d < DP / 32; ++d)
+                    o[d] = mma(tile_at.columns(buffer(turn, 1), h * 16, d), pf, o[d]);
             }
         }
-        if (more) {
-            kt.store(lds[turn ^ 1][0]);
-            vt.store(lds[turn ^ 1][1]);
+        if (NB == 1) {
+            __syncthreads();
+            start(at + kStep, 0);
+        } else {
+            turn ^= 1;
         }
+        finish(at + kStep, turn);
         __syncthreads();
     }
+    l = both_halves(l, [](float x, float y) { return x + y; });
+    if constexpr (W::kStreams > 1)
+        join_streams<WR, DP / 2 + 2>(lds, stream, wave % WR,
+            [&](int k) { return k < DP / 2 ? o[k / 16][k % 16] : k == DP / 2 ? m : l; },
+            [&](auto number) {
+                const float m2 = number(DP / 2), l2 = number(DP / 2 + 1), most = fmaxf(m, m2);
+                const float a = __builtin_amdgcn_exp2f((m - most) * c);
+                const float b = __builtin_amdgcn_exp2f((m2 - most) * c);
+                m = most;
+                l = __builtin_fmaf(l, a, l2 * b);
 #pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        const int row = row0 + b * 32 + column();
-        const float sum = both_halves(l[b], [](float x, float y) { return x + y; });
-        if (row >= in.length) continue;
-        const int64_t token = in.first + row;
-        store_column<T, DP>(out + token * s.o_ld + head * s.dim, o[b], 1.f / sum, s.dim);
-        if (lse && upper() == 0) lse[token * s.heads + head] = m[b] * s.scale + logf(sum);
-    }
+                for (int k = 0; k < DP / 2; ++k)
+                    o[k / 16][k % 16] = __builtin_fmaf(o[k / 16][k % 16], a, number(k) * b);
+            });
+    if (stream > 0 || row >= in.length) return;
+    store_column<T, DP>(out + token * s.o_ld + head * s.dim, o, 1.f / l, s.dim);
+    if (lse && upper() == 0) lse[token * s.heads + head] = m * s.scale + logf(l);
 }
 
 // ---------------------------------------------------------------------------
@@ -391,224 +502,225 @@ struct Grads {
     int parts;
 };
 
-template <class T, int DP, int QB>
-__global__ __launch_bounds__(kThreads) void k_attention_dq(
+template <class T, int DP, int WR, int NB, bool DIRECT>
+__global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
     const T *__restrict__ dout, const T *__restrict__ q, const T *__restrict__ k,
     const T *__restrict__ v, Sides s, Grads g, const float *__restrict__ lse,
     const float *__restrict__ delta, const float *__restrict__ parts, T *__restrict__ dq,
     int tiles)
 {
-    using Kv = Tile<T, DP>;
-    constexpr int kRows = kWaves * 32 * QB;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][Kv::kBytes];
+    using W = Share<DP, WR, NB>;
+    const Tile<T, DP> tile_at;
+    __shared__ __attribute__((aligned(1024))) char lds[W::kLds];
     const int head = blockIdx.x % s.heads, tile = tiles - 1 - blockIdx.x / s.heads;
-    const Range in = find_sequence(s, tile, kRows);
+    const Range in = find_sequence(s, tile, W::kRows);
     if (in.at < 0 || in.at >= in.length) return;
-    const int wave = wave_number(), row0 = in.at + wave * 32 * QB;
+    const int wave = wave_number(), stream = wave / WR, row0 = in.at + wave % WR * 32;
     const int kv = head / (s.heads / s.kv_heads);
     const T *kp = k + in.first * s.k_ld + kv * s.dim, *vp = v + in.first * s.v_ld + kv * s.dim;
+    const int keys = s.causal ? min(in.length, in.at + W::kRows) : in.length;
+    char *const own = lds + stream * NB * 2 * W::kTileBytes;
+    const auto buffer = [&](int turn, int side) { return own + (turn * 2 + side) * W::kTileBytes; };
+    Loader<T, DP, WR, DIRECT> kt(wave % WR, s.k_ld, s.dim), vt(wave % WR, s.v_ld, s.dim);
+    const auto start = [&](int at, int turn) {
+        if (at >= keys) return;
+        kt.start(kp, s.k_ld, s.dim, at, in.length, buffer(turn, 0));
+        vt.start(vp, s.v_ld, s.dim, at, in.length, buffer(turn, 1));
+    };
+    const auto finish = [&](int at, int turn) {
+        if (at >= keys) return;
+        kt.finish(buffer(turn, 0));
+        vt.finish(buffer(turn, 1));
+    };
+    start(stream * kTile, 0);
     const float grow = gradient_scale<T>(parts, g.parts);
-    vec8<T> qf[QB][DP / 16], df[QB][DP / 16];
-    float l2[QB], dl[QB];
+    const int row = row0 + column();
+    const int64_t token = in.first + row;
+    const bool there = row < in.length;
+    vec8<T> qf[DP / 16], df[DP / 16];
 #pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        const int row = row0 + b * 32 + column();
-        const int64_t token = in.first + row;
-        const bool there = row < in.length;
-#pragma unroll
-        for (int c = 0; c < DP / 16; ++c) {
-            qf[b][c] = load8(q + token * s.q_ld + head * s.dim, c * 16 + upper() * 8, s.dim, there);
-            df[b][c] = load8(dout + token * g.d_ld + head * s.dim, c * 16 + upper() * 8, s.dim, there);
-        }
-        l2[b] = there ? lse[token * s.heads + head] * kLog2e : 0.f;
-        dl[b] = there ? delta[token * s.heads + head] : 0.f;
+    for (int d = 0; d < DP / 16; ++d) {
+        qf[d] = load8(q + token * s.q_ld + head * s.dim, d * 16 + upper() * 8, s.dim, there);
+        df[d] = load8(dout + token * g.d_ld + head * s.dim, d * 16 + upper() * 8, s.dim, there);
     }
-    const int keys = s.causal ? min(in.length, in.at + kRows) : in.length;
+    const float l2 = there ? lse[token * s.heads + head] * kLog2e : 0.f;
+    const float dl = there ? delta[token * s.heads + head] : 0.f;
     const float c = s.scale * kLog2e;
-    f32x16 acc[QB][DP / 32] = {};
-    Kv kt, vt;
-    kt.load(kp, s.k_ld, 0, in.length, s.dim);
-    vt.load(vp, s.v_ld, 0, in.length, s.dim);
-    kt.store(lds[0][0]);
-    vt.store(lds[0][1]);
+    f32x16 acc[DP / 32] = {};
+    finish(stream * kTile, 0);
     __syncthreads();
-    for (int at = 0, turn = 0; at < keys; at += kTile, turn ^= 1) {
-        const bool more = at + kTile < keys;
-        if (more) {
-            kt.load(kp, s.k_ld, at + kTile, in.length, s.dim);
-            vt.load(vp, s.v_ld, at + kTile, in.length, s.dim);
-        }
-        if (!(s.causal && at > row0 + 32 * QB - 1)) {
+    constexpr int kStep = W::kStreams * kTile;
+    for (int first = 0, turn = 0; first < keys; first += kStep) {
+        const int at = first + stream * kTile;
+        if (NB > 1) start(at + kStep, turn ^ 1);
+        if (at < keys && !(s.causal && at > row0 + 31)) {
             const bool mask = at + kTile > in.length || (s.causal && at + kTile - 1 > row0);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                f32x16 p[QB] = {}, dp[QB] = {};
+                f32x16 p = {}, dp = {};
 #pragma unroll
                 for (int d = 0; d < DP / 16; ++d) {
-                    const vec8<T> f = Kv::rows(lds[turn][0], h * 32, d);
-                    const vec8<T> w = Kv::rows(lds[turn][1], h * 32, d);
-#pragma unroll
-                    for (int b = 0; b < QB; ++b) {
-                        p[b] = mma(f, qf[b][d], p[b]);
-                        dp[b] = mma(w, df[b][d], dp[b]);
-                    }
+                    p = mma(tile_at.rows(buffer(turn, 0), h * 32, d), qf[d], p);
+                    dp = mma(tile_at.rows(buffer(turn, 1), h * 32, d), df[d], dp);
                 }
 #pragma unroll
-                for (int b = 0; b < QB; ++b) {
-                    const int row = row0 + b * 32 + column();
+                for (int i = 0; i < 16; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -l2));
+                    p[i] = e * ((dp[i] - dl) * grow);
+                }
+                if (mask) {
                     const int end = s.causal ? min(in.length, row + 1) : in.length;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(p[b][i], c, -l2[b]));
-                        p[b][i] = e * ((dp[b][i] - dl[b]) * grow);
-                        if (mask && at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) >= end)
-                            p[b][i] = 0.f;
-                    }
+                    for (int i = 0; i < 16; ++i)
+                        if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) >= end) p[i] = 0.f;
                 }
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    vec8<T> pf[QB];
+                    const vec8<T> pf = narrow<T>(p, half);
 #pragma unroll
-                    for (int b = 0; b < QB; ++b) pf[b] = narrow<T>(p[b], half);
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) {
-                        const vec8<T> f = Kv::columns(lds[turn][0], h * 32 + half * 16, d);
-#pragma unroll
-                        for (int b = 0; b < QB; ++b) acc[b][d] = mma(f, pf[b], acc[b][d]);
-                    }
+                    for (int d = 0; d < DP / 32; ++d)
+                        acc[d] = mma(tile_at.columns(buffer(turn, 0), h * 32 + half * 16, d), pf, acc[d]);
                 }
             }
         }
-        if (more) {
-            kt.store(lds[turn ^ 1][0]);
-            vt.store(lds[turn ^ 1][1]);
+        if (NB == 1) {
+            __syncthreads();
+            start(at + kStep, 0);
+        } else {
+            turn ^= 1;
         }
+        finish(at + kStep, turn);
         __syncthreads();
     }
+    if constexpr (W::kStreams > 1)
+        join_streams<WR, DP / 2>(lds, stream, wave % WR, [&](int k) { return acc[k / 16][k % 16]; },
+            [&](auto number) {
 #pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        const int row = row0 + b * 32 + column();
-        if (row < in.length)
-            store_column<T, DP>(dq + (int64_t)(in.first + row) * g.dq_ld + head * s.dim, acc[b],
-                                s.scale / grow, s.dim);
-    }
+                for (int k = 0; k < DP / 2; ++k) acc[k / 16][k % 16] += number(k);
+            });
+    if (stream == 0 && there)
+        store_column<T, DP>(dq + token * g.dq_ld + head * s.dim, acc, s.scale / grow, s.dim);
 }
 
-template <class T, int DP, int KB>
-__global__ __launch_bounds__(kThreads) void k_attention_dkv(
+template <class T, int DP, int WR, int NB, bool DIRECT>
+__global__ __launch_bounds__(kThreads, 2) void k_attention_dkv(
     const T *__restrict__ dout, const T *__restrict__ q, const T *__restrict__ k,
     const T *__restrict__ v, Sides s, Grads g, const float *__restrict__ lse,
     const float *__restrict__ delta, const float *__restrict__ parts, T *__restrict__ dk,
     T *__restrict__ dv, int tiles)
 {
-    using Q = Tile<T, DP>;
-    constexpr int kRows = kWaves * 32 * KB;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][Q::kBytes];
-    __shared__ float s_row[2][2][kTile];  // lse in base 2 and D of the tile's queries
+    using W = Share<DP, WR, NB>;
+    const Tile<T, DP> tile_at;
+    __shared__ __attribute__((aligned(1024))) char lds[W::kLds];
+    // lse in base 2 and D of the tiles' queries
+    __shared__ float s_row[W::kStreams][NB][2][kTile];
     const int kv = blockIdx.x % s.kv_heads, tile = blockIdx.x / s.kv_heads;
-    const Range in = find_sequence(s, tile, kRows);
+    const Range in = find_sequence(s, tile, W::kRows);
     if (in.at < 0 || in.at >= in.length) return;
-    const int wave = wave_number(), row0 = in.at + wave * 32 * KB;
+    const int wave = wave_number(), stream = wave / WR, row0 = in.at + wave % WR * 32;
     const int group = s.heads / s.kv_heads;
-    const float grow = gradient_scale<T>(parts, g.parts);
-    vec8<T> kf[KB][DP / 16], vf[KB][DP / 16];
-#pragma unroll
-    for (int b = 0; b < KB; ++b) {
-        const int row = row0 + b * 32 + column();
-        const int64_t token = in.first + row;
-#pragma unroll
-        for (int c = 0; c < DP / 16; ++c) {
-            kf[b][c] = load8(k + token * s.k_ld + kv * s.dim, c * 16 + upper() * 8, s.dim, row < in.length);
-            vf[b][c] = load8(v + token * s.v_ld + kv * s.dim, c * 16 + upper() * 8, s.dim, row < in.length);
-        }
-    }
-    const float c = s.scale * kLog2e;
-    f32x16 dka[KB][DP / 32] = {}, dva[KB][DP / 32] = {};
-    Q qt, dt;
-    float row_value = 0.f;
-    // the queries that see the tile's keys, a head of the group after the other
+    char *const own = lds + stream * NB * 2 * W::kTileBytes;
+    const auto buffer = [&](int turn, int side) { return own + (turn * 2 + side) * W::kTileBytes; };
+    // the queries that see the workgroup's keys, a head of the group after the other
     const int from = s.causal ? in.at / kTile * kTile : 0;
     const int per_head = (in.length - from + kTile - 1) / kTile, steps = per_head * group;
-    auto load = [&](int step) {
+    Loader<T, DP, WR, DIRECT> qt(wave % WR, s.q_ld, s.dim), dt(wave % WR, g.d_ld, s.dim);
+    float row_value[2];
+    const auto start = [&](int step, int turn) {
+        if (step >= steps) return;
         const int head = kv * group + step / per_head, at = from + step % per_head * kTile;
-        qt.load(q + in.first * s.q_ld + head * s.dim, s.q_ld, at, in.length, s.dim);
-        dt.load(dout + in.first * g.d_ld + head * s.dim, g.d_ld, at, in.length, s.dim);
-        if (threadIdx.x < 2 * kTile) {
-            const int row = at + threadIdx.x % kTile;
+        qt.start(q + in.first * s.q_ld + head * s.dim, s.q_ld, s.dim, at, in.length, buffer(turn, 0));
+        dt.start(dout + in.first * g.d_ld + head * s.dim, g.d_ld, s.dim, at, in.length, buffer(turn, 1));
+        if (wave % WR == 0) {
+            const int row = at + (threadIdx.x & 63);
             const int64_t to = (int64_t)(in.first + row) * s.heads + head;
             // (behind the end: a score of 0 less infinity has no weight)
-            row_value = threadIdx.x < kTile ? (row < in.length ? lse[to] * kLog2e : INFINITY)
-                                            : (row < in.length ? delta[to] : 0.f);
+            row_value[0] = row < in.length ? lse[to] * kLog2e : INFINITY;
+            row_value[1] = row < in.length ? delta[to] : 0.f;
         }
     };
-    auto store = [&](int turn) {
-        qt.store(lds[turn][0]);
-        dt.store(lds[turn][1]);
-        if (threadIdx.x < 2 * kTile) s_row[turn][threadIdx.x / kTile][threadIdx.x % kTile] = row_value;
+    const auto finish = [&](int step, int turn) {
+        if (step >= steps) return;
+        qt.finish(buffer(turn, 0));
+        dt.finish(buffer(turn, 1));
+        if (wave % WR == 0) {
+            s_row[stream][turn][0][threadIdx.x & 63] = row_value[0];
+            s_row[stream][turn][1][threadIdx.x & 63] = row_value[1];
+        }
     };
-    load(0);
-    store(0);
+    start(stream, 0);
+    const float grow = gradient_scale<T>(parts, g.parts);
+    const int row = row0 + column();
+    const int64_t token = in.first + row;
+    vec8<T> kf[DP / 16], vf[DP / 16];
+#pragma unroll
+    for (int d = 0; d < DP / 16; ++d) {
+        kf[d] = load8(k + token * s.k_ld + kv * s.dim, d * 16 + upper() * 8, s.dim, row < in.length);
+        vf[d] = load8(v + token * s.v_ld + kv * s.dim, d * 16 + upper() * 8, s.dim, row < in.length);
+    }
+    const float c = s.scale * kLog2e;
+    f32x16 dka[DP / 32] = {}, dva[DP / 32] = {};
+    finish(stream, 0);
     __syncthreads();
-    for (int step = 0, turn = 0; step < steps; ++step, turn ^= 1) {
-        if (step + 1 < steps) load(step + 1);
+    for (int first = 0, turn = 0; first < steps; first += W::kStreams) {
+        const int step = first + stream;
+        if (NB > 1) start(step + W::kStreams, turn ^ 1);
         const int at = from + step % per_head * kTile;
-        if (!(s.causal && at + kTile - 1 < row0)) {
-            const bool mask = s.causal && at < row0 + 32 * KB - 1;
+        if (step < steps && !(s.causal && at + kTile - 1 < row0)) {
+            const bool mask = s.causal && at < row0 + 31;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                f32x16 p[KB] = {}, dp[KB] = {};
+                f32x16 p = {}, dp = {};
 #pragma unroll
                 for (int d = 0; d < DP / 16; ++d) {
-                    const vec8<T> f = Q::rows(lds[turn][0], h * 32, d);
-                    const vec8<T> w = Q::rows(lds[turn][1], h * 32, d);
-#pragma unroll
-                    for (int b = 0; b < KB; ++b) {
-                        p[b] = mma(f, kf[b][d], p[b]);
-                        dp[b] = mma(w, vf[b][d], dp[b]);
-                    }
+                    p = mma(tile_at.rows(buffer(turn, 0), h * 32, d), kf[d], p);
+                    dp = mma(tile_at.rows(buffer(turn, 1), h * 32, d), vf[d], dp);
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int r = h * 32 + upper() * 4 + i % 4 + 8 * (i / 4);
-                    const float l2 = s_row[turn][0][r], dl = s_row[turn][1][r];
-#pragma unroll
-                    for (int b = 0; b < KB; ++b) {
-                        float e = __builtin_amdgcn_exp2f(__builtin_fmaf(p[b][i], c, -l2));
-                        float ds = e * ((dp[b][i] - dl) * grow);
-                        if (mask && at + r < row0 + b * 32 + column()) e = 0.f, ds = 0.f;
-                        p[b][i] = e;
-                        dp[b][i] = ds;
-                    }
+                    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -s_row[stream][turn][0][r]));
+                    dp[i] = p[i] * ((dp[i] - s_row[stream][turn][1][r]) * grow);
                 }
+                if (mask)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) < row) p[i] = 0.f, dp[i] = 0.f;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    vec8<T> pf[KB], sf[KB];
-#pragma unroll
-                    for (int b = 0; b < KB; ++b) pf[b] = narrow<T>(p[b], half), sf[b] = narrow<T>(dp[b], half);
+                    const vec8<T> pf = narrow<T>(p, half), sf = narrow<T>(dp, half);
 #pragma unroll
                     for (int d = 0; d < DP / 32; ++d) {
-                        const vec8<T> f = Q::columns(lds[turn][1], h * 32 + half * 16, d);
-                        const vec8<T> w = Q::columns(lds[turn][0], h * 32 + half * 16, d);
-#pragma unroll
-                        for (int b = 0; b < KB; ++b) {
-                            dva[b][d] = mma(f, pf[b], dva[b][d]);
-                            dka[b][d] = mma(w, sf[b], dka[b][d]);
-                        }
+                        dva[d] = mma(tile_at.columns(buffer(turn, 1), h * 32 + half * 16, d), pf, dva[d]);
+                        dka[d] = mma(tile_at.columns(buffer(turn, 0), h * 32 + half * 16, d), sf, dka[d]);
                     }
                 }
             }
         }
-        if (step + 1 < steps) store(turn ^ 1);
+        if (NB == 1) {
+            __syncthreads();
+            start(step + W::kStreams, 0);
+        } else {
+            turn ^= 1;
+        }
+        finish(step + W::kStreams, turn);
         __syncthreads();
     }
+    if constexpr (W::kStreams > 1) {
+        const auto join = [&](f32x16(&acc)[DP / 32]) {
+            join_streams<WR, DP / 2>(lds, stream, wave % WR, [&](int k) { return acc[k / 16][k % 16]; },
+                [&](auto number) {
 #pragma unroll
-    for (int b = 0; b < KB; ++b) {
-        const int row = row0 + b * 32 + column();
-        if (row >= in.length) continue;
-        const int64_t token = in.first + row;
-        store_column<T, DP>(dk + token * g.dk_ld + kv * s.dim, dka[b], s.scale / grow, s.dim);
-        store_column<T, DP>(dv + token * g.dv_ld + kv * s.dim, dva[b], 1.f, s.dim);
+                    for (int k = 0; k < DP / 2; ++k) acc[k / 16][k % 16] += number(k);
+                });
+        };
+        join(dka);
+        __syncthreads();
+        join(dva);
     }
+    if (stream > 0 || row >= in.length) return;
+    store_column<T, DP>(dk + token * g.dk_ld + kv * s.dim, dka, s.scale / grow, s.dim);
+    store_column<T, DP>(dv + token * g.dv_ld + kv * s.dim, dva, 1.f, s.dim);
 }
 
 template <class F>
@@ -618,14 +730,31 @@ void with_half(int32_t dtype, F &&f)
     else f((_Float16 *)nullptr);
 }
 
+// Calls f(padded dim, rows of waves, depth, direct).
 template <class F>
-void with_dim(int dim, F &&f)
+void with_shape(int dim, bool few, bool direct, F &&f)
 {
     using std::integral_constant;
-    if (dim <= 32) f(integral_constant<int, 32>{});
-    else if (dim <= 64) f(integral_constant<int, 64>{});
-    else if (dim <= 96) f(integral_constant<int, 96>{});
-    else f(integral_constant<int, 128>{});
+    auto go = [&](auto padded, auto waves, auto depth) {
+        if (direct) f(padded, waves, depth, std::true_type{});
+        else f(padded, waves, depth, std::false_type{});
+    };
+    auto by_waves = [&](auto padded) {
+        constexpr int kFew = decltype(padded)::value <= 64 ? 1 : 2;
+        if (few) go(padded, integral_constant<int, kFew>{}, integral_constant<int, 1>{});
+        else go(padded, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+    };
+    if (dim <= 32) by_waves(integral_constant<int, 32>{});
+    else if (dim <= 64) by_waves(integral_constant<int, 64>{});
+    else if (dim <= 96) by_waves(integral_constant<int, 96>{});
+    else by_waves(integral_constant<int, 128>{});
+}
+
+// Whether a side's tiles can be read straight into LDS: pieces of 16 bytes on 4-byte
+// borders, a tile's rows within the buffer's 2 GiB.
+bool direct_side(const void *p, int64_t ld, int dim)
+{
+    return dim % 8 == 0 && (uintptr_t)p % 4 == 0 && ld % 2 == 0 && ld < (1 << 23);
 }
 
 int check_side(const void *p, int64_t ld, int64_t tokens, int64_t width, const char *name)
@@ -653,16 +782,21 @@ int check_attention(int32_t dtype, int64_t tokens, int32_t heads, int32_t kv_hea
     return ONEBIT_OK;
 }
 
-// Tiles of `rows` tokens that cover every sequence (find_sequence), and whether a
-// launch of one workgroup for each and each head is possible.
-int tile_count(int64_t tokens, int64_t sequences, int heads, int rows, int *tiles)
+// Tiles of `rows` tokens that cover every sequence (find_sequence): a launch has a
+// workgroup for each and each head.
+int check_tiles(int64_t tokens, int64_t sequences, int heads)
 {
-    const int64_t n = tokens / rows + sequences;
-    if (n * heads >= ((int64_t)1 << 32) / kThreads)
+    if ((tokens / 128 + sequences) * heads >= ((int64_t)1 << 32) / kThreads)
         return fail(ONEBIT_EINVAL, "%lld tokens in %lld sequences with %d heads are too many for one call",
                     (long long)tokens, (long long)sequences, heads);
-    *tiles = (int)n;
     return ONEBIT_OK;
+}
+
+int tile_count(int64_t tokens, int64_t sequences, int rows) { return (int)(tokens / rows + sequences); }
+
+bool few_tiles(int64_t tokens, int64_t sequences, int heads)
+{
+    return (tokens / 128 + sequences) * heads <= 512;
 }
 
 int delta_blocks(int64_t tokens, int heads)
@@ -690,16 +824,17 @@ int onebit_attention_forward(const void *q, int64_t q_ld, const void *k, int64_t
     TRY(check_side(v, v_ld, tokens, kv_width, "v"));
     TRY(check_side(out, out_ld, tokens, width, "out"));
     if ((uintptr_t)lse % 4) return fail(ONEBIT_EALIGN, "lse is not 4-byte aligned");
-    constexpr int kBlocks = 1, kRows = kWaves * 32 * kBlocks;
-    int tiles;
-    TRY(tile_count(tokens, sequences, heads, kRows, &tiles));
+    TRY(check_tiles(tokens, sequences, heads));
     if (tokens == 0 || sequences == 0) return ONEBIT_OK;
     const Sides s{q_ld, k_ld, v_ld, out_ld, starts, (int)tokens, (int)sequences,
                   heads, kv_heads, dim, scale, causal};
     with_half(dtype, [&](auto *t) {
-        with_dim(dim, [&](auto padded) {
+        with_shape(dim, few_tiles(tokens, sequences, heads),
+                   direct_side(k, k_ld, dim) && direct_side(v, v_ld, dim),
+                   [&](auto padded, auto waves, auto depth, auto direct) {
             using T = std::remove_pointer_t<decltype(t)>;
-            k_attention<T, decltype(padded)::value, kBlocks>
+            const int tiles = tile_count(tokens, sequences, 32 * waves);
+            k_attention<T, padded(), waves(), depth(), direct()>
                 <<<tiles * heads, kThreads, 0, (hipStream_t)stream>>>(
                     (const T *)q, (const T *)k, (const T *)v, s, (T *)out, lse, tiles);
         });
@@ -738,9 +873,7 @@ int onebit_attention_grad(const void *dout, int64_t dout_ld, const void *q, int6
     if ((uintptr_t)lse % 4) return fail(ONEBIT_EALIGN, "lse is not 4-byte aligned");
     if (!workspace) return fail(ONEBIT_EINVAL, "workspace is NULL");
     if ((uintptr_t)workspace % 16) return fail(ONEBIT_EALIGN, "workspace is not 16-byte aligned");
-    constexpr int kBlocks = 1, kRows = kWaves * 32 * kBlocks;
-    int tiles;
-    TRY(tile_count(tokens, sequences, heads, kRows, &tiles));
+    TRY(check_tiles(tokens, sequences, heads));
     if (tokens == 0 || sequences == 0) return ONEBIT_OK;
     const Sides s{q_ld, k_ld, v_ld, out_ld, starts, (int)tokens, (int)sequences,
                   heads, kv_heads, dim, scale, causal};
@@ -751,14 +884,23 @@ int onebit_attention_grad(const void *dout, int64_t dout_ld, const void *q, int6
         using T = std::remove_pointer_t<decltype(t)>;
         k_attention_delta<T><<<g.parts, kThreads, 0, st>>>((const T *)dout, dout_ld,
                                                            (const T *)out, s, delta, parts);
-        with_dim(dim, [&](auto padded) {
-            constexpr int DP = decltype(padded)::value;
-            k_attention_dkv<T, DP, kBlocks><<<tiles * kv_heads, kThreads, 0, st>>>(
-                (const T *)dout, (const T *)q, (const T *)k, (const T *)v, s, g, lse, delta, parts,
-                (T *)dk, (T *)dv, tiles);
-            k_attention_dq<T, DP, kBlocks><<<tiles * heads, kThreads, 0, st>>>(
-                (const T *)dout, (const T *)q, (const T *)k, (const T *)v, s, g, lse, delta, parts,
-                (T *)dq, tiles);
+        with_shape(dim, few_tiles(tokens, sequences, kv_heads),
+                   direct_side(q, q_ld, dim) && direct_side(dout, dout_ld, dim),
+                   [&](auto padded, auto waves, auto depth, auto direct) {
+            const int tiles = tile_count(tokens, sequences, 32 * waves);
+            k_attention_dkv<T, padded(), waves(), depth(), direct()>
+                <<<tiles * kv_heads, kThreads, 0, st>>>(
+                    (const T *)dout, (const T *)q, (const T *)k, (const T *)v, s, g, lse, delta,
+                    parts, (T *)dk, (T *)dv, tiles);
+        });
+        with_shape(dim, few_tiles(tokens, sequences, heads),
+                   direct_side(k, k_ld, dim) && direct_side(v, v_ld, dim),
+                   [&](auto padded, auto waves, auto depth, auto direct) {
+            const int tiles = tile_count(tokens, sequences, 32 * waves);
+            k_attention_dq<T, padded(), waves(), depth(), direct()>
+                <<<tiles * heads, kThreads, 0, st>>>(
+                    (const T *)dout, (const T *)q, (const T *)k, (const T *)v, s, g, lse, delta,
+                    parts, (T *)dq, tiles);
         });
     });
     return launched("attention gradient launch");

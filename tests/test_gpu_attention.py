@@ -26,10 +26,10 @@ def _gen(dev, seed):
     return torch.Generator(device=dev).manual_seed(seed)
 
 
-def _side(tokens, heads, dim, dtype, dev, extra, seed, std=1.0):
-    """[tokens, heads, dim], `extra` elements between tokens, from an odd element on."""
-    flat = torch.randn(tokens * (heads * dim + extra) + 1, device=dev, generator=_gen(dev, seed)) * std
-    return flat.to(dtype)[1:].view(tokens, heads * dim + extra)[:, :heads * dim].unflatten(1, (heads, dim))
+def _side(tokens, heads, dim, dtype, dev, extra, seed, std=1.0, shift=0):
+    """[tokens, heads, dim], `extra` elements between tokens, from element `shift` on."""
+    flat = torch.randn(tokens * (heads * dim + extra) + shift, device=dev, generator=_gen(dev, seed)) * std
+    return flat.to(dtype)[shift:].view(tokens, heads * dim + extra)[:, :heads * dim].unflatten(1, (heads, dim))
 
 
 def _reference(q, k, v, at, causal, scale, dout=None, kind="bf16"):
@@ -83,7 +83,7 @@ def _reference(q, k, v, at, causal, scale, dout=None, kind="bf16"):
 
 
 def _check(dev, lengths, heads, kv, dim, kind, causal, extra=0, scale=None, before=0, after=0,
-           std=1.0, dstd=1.0):
+           std=1.0, dstd=1.0, shift=0):
     """Forward and backward over sequences of these lengths, with tokens in front of and
     behind them that belong to none and hold NaN."""
     import paper_2102_02888_amd as ob
@@ -92,7 +92,7 @@ def _check(dev, lengths, heads, kv, dim, kind, causal, extra=0, scale=None, befo
         at.append(at[-1] + n)
     tokens = at[-1] + after
     starts = torch.tensor(at, dtype=torch.int32, device=dev)
-    q, k, v, dout = (_side(tokens, h, dim, dtype, dev, extra, 1 + s, std if s < 2 else 1.0)
+    q, k, v, dout = (_side(tokens, h, dim, dtype, dev, extra, 1 + s, std if s < 2 else 1.0, shift)
                      for s, h in enumerate((heads, kv, kv, heads)))
     dout *= dstd
     none = torch.ones(tokens, dtype=torch.bool, device=dev)
@@ -144,11 +144,20 @@ def test_attention(dev, lengths, heads, kv, dim, kind, causal):
     _check(dev, lengths, heads, kv, dim, kind, causal, extra=dim % 2 * 3)
 
 
+@pytest.mark.parametrize("dim", [8, 32, 40, 64, 72, 80, 96, 104, 128])
+@pytest.mark.parametrize("extra,shift", [(1, 0), (0, 1), (2, 2), (16, 8)])
+def test_alignments(dev, dim, extra, shift):
+    """Rows on 16-byte, 4-byte and odd borders: whole pieces go straight to LDS, others
+    through registers."""
+    _check(dev, [150, 33], 2, 1, dim, "bf16", True, extra=extra, shift=shift)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
 @pytest.mark.parametrize("causal", [True, False])
 def test_tokens_outside_the_sequences(dev, kind, causal):
     """Neither read, NaN as they are, nor written."""
-    _check(dev, [70, 1, 200], 4, 2, 64, kind, causal, extra=5, before=3, after=130)
+    _check(dev, [70, 1, 200], 4, 2, 64, kind, causal, extra=5, before=3, after=130, shift=1)
+    _check(dev, [70, 1, 200], 4, 2, 64, kind, causal, extra=8, before=3, after=130)
     _check(dev, [40], 2, 2, 128, kind, causal, before=129, after=1)
 
 
@@ -286,16 +295,15 @@ def test_rows_past_32_bits(dev):
     results = sides[1][:, :4 * heads * dim].unflatten(1, (4 * heads, dim)).split(heads, 1)
     lse = torch.zeros(tokens, heads, device=dev)
     ob.onebit_attention_forward(*parts, starts, results[0], lse)
-    small = [t[-n:].contiguous() for t in parts]
-    s2 = torch.tensor([0, n], dtype=torch.int32, device=dev)
-    out, l2 = torch.empty_like(small[0]), torch.empty(n, heads, device=dev)
-    ob.onebit_attention_forward(*small, s2, out, l2)
-    assert torch.equal(results[0][-n:], out) and torch.equal(lse[-n:], l2)
-    grads = [torch.empty_like(t) for t in small]
-    ob.onebit_attention_grad(parts[0], *parts, results[0], lse, starts, *results[1:],
-                             ob.attention_workspace(tokens, heads, dev))
-    ob.onebit_attention_grad(small[0], *small, out, l2, s2, *grads, ob.attention_workspace(n, heads, dev))
-    assert all(torch.equal(a[-n:], b) for a, b in zip(results[1:], grads))
+    # the same tokens side by side (which kernels run goes by the number of tokens, too)
+    small = [t.contiguous() for t in parts]
+    out, l2 = torch.empty_like(small[0]), torch.empty(tokens, heads, device=dev)
+    ob.onebit_attention_forward(*small, starts, out, l2)
+    assert torch.equal(results[0][-n:], out[-n:]) and torch.equal(lse[-n:], l2[-n:])
+    grads, work = [torch.empty_like(t) for t in small], ob.attention_workspace(tokens, heads, dev)
+    ob.onebit_attention_grad(parts[0], *parts, results[0], lse, starts, *results[1:], work)
+    ob.onebit_attention_grad(small[0], *small, out, l2, starts, *grads, work)
+    assert all(torch.equal(a[-n:], b[-n:]) for a, b in zip(results[1:], grads))
     assert not bool(sides[1][:-n].any())
 
 
