@@ -284,8 +284,10 @@ __device__ __forceinline__ void store_column(T *to, const f32x16 (&acc)[DP / 32]
 template <int DP, int WR, int NB>
 struct Share {
     static constexpr int kStreams = kWaves / WR, kRows = 32 * WR;
-    static constexpr int kTileBytes = kTile * DP * 2, kLds = kStreams * NB * 2 * kTileBytes;
-    static_assert(kStreams * WR == kWaves && (kWaves - WR) * DP * 32 * 4 <= kLds, "sums are joined in LDS");
+    static constexpr int kTileBytes = kTile * DP * 2, kLds = kStreams * 2 * kTileBytes;
+    static_assert(kStreams * WR == kWaves, "four waves");
+    static constexpr int kSums = (kWaves - WR) * 64 * (DP / 2 + 2) * 4;  // where streams are joined
+    static constexpr int kFirst = kLds > kSums ? kLds : kSums;
 };
 
 // Brings what the streams' waves have of the same rows to the first stream's wave: take(i)
@@ -320,7 +322,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention(const T *__restrict__
 {
     using W = Share<DP, WR, NB>;
     const Tile<T, DP> tile_at;
-    __shared__ __attribute__((aligned(1024))) char lds[W::kLds];
+    // (two arrays, so that a tile's loads are not waited for before the other is read)
+    __shared__ __attribute__((aligned(1024))) char lds[W::kFirst], lds2[NB > 1 ? W::kLds : 1024];
     const int head = blockIdx.x % s.heads, tile = tiles - 1 - blockIdx.x / s.heads;
     const Range in = find_sequence(s, tile, W::kRows);
     if (in.at < 0 || in.at >= in.length) return;
@@ -328,20 +331,19 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention(const T *__restrict__
     const int kv = head / (s.heads / s.kv_heads);
     const T *kp = k + in.first * s.k_ld + kv * s.dim, *vp = v + in.first * s.v_ld + kv * s.dim;
     const int keys = s.causal ? min(in.length, in.at + W::kRows) : in.length;
-    char *const own = lds + stream * NB * 2 * W::kTileBytes;
-    const auto buffer = [&](int turn, int side) { return own + (turn * 2 + side) * W::kTileBytes; };
+    const int own = stream * 2 * W::kTileBytes, other = own + W::kTileBytes;
     Loader<T, DP, WR, DIRECT> kt(wave % WR, s.k_ld, s.dim), vt(wave % WR, s.v_ld, s.dim);
-    const auto start = [&](int at, int turn) {
+    const auto start = [&](int at, char *to) {
         if (at >= keys) return;
-        kt.start(kp, s.k_ld, s.dim, at, in.length, buffer(turn, 0));
-        vt.start(vp, s.v_ld, s.dim, at, in.length, buffer(turn, 1));
+        kt.start(kp, s.k_ld, s.dim, at, in.length, to + own);
+        vt.start(vp, s.v_ld, s.dim, at, in.length, to + other);
     };
-    const auto finish = [&](int at, int turn) {
+    const auto finish = [&](int at, char *to) {
         if (at >= keys) return;
-        kt.finish(buffer(turn, 0));
-        vt.finish(buffer(turn, 1));
+        kt.finish(to + own);
+        vt.finish(to + other);
     };
-    start(stream * kTile, 0);
+    start(stream * kTile, lds);
     const int row = row0 + column();
     const int64_t token = in.first + row;
     vec8<T> qf[DP / 16];
@@ -351,12 +353,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention(const T *__restrict__
     const float c = s.scale * kLog2e;
     f32x16 o[DP / 32] = {};
     float m = -INFINITY, l = 0.f;
-    finish(stream * kTile, 0);
+    finish(stream * kTile, lds);
     __syncthreads();
     constexpr int kStep = W::kStreams * kTile;
-    for (int first = 0, turn = 0; first < keys; first += kStep) {
-        const int at = first + stream * kTile;
-        if (NB > 1) start(at + kStep, turn ^ 1);
+    const auto step = [&](int at, const char *from, char *next) {
+        if (NB > 1) start(at + kStep, next);
         // (with the mask, a tile that a wave does not skip leaves each of its rows a key)
         if (at < keys && !(s.causal && at > row0 + 31)) {
             f32x16 p[2] = {};
@@ -364,7 +365,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention(const T *__restrict__
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int d = 0; d < DP / 16; ++d)
-                    p[h] = mma(tile_at.rows(buffer(turn, 0), h * 32, d), qf[d], p[h]);
+                    p[h] = mma(tile_at.rows(from + own, h * 32, d), qf[d], p[h]);
             if (at + kTile > in.length || (s.causal && at + kTile - 1 > row0)) {
                 const int end = s.causal ? min(in.length, row + 1) : in.length;
 #pragma unroll
@@ -378,39 +379,47 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention(const T *__restrict__
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) most = fmaxf(most, p[h][i]);
-            most = fmaxf(m, both_halves(most, [](float x, float y) { return fmaxf(x, y); }));
-            const float alpha = __builtin_amdgcn_exp2f((m - most) * c), mc = most * c;
-            m = most;
-            float sum = 0.f;
+            most = both_halves(most, [](float x, float y) { return fmaxf(x, y); });
+            // What is summed so far is brought to the new maximum only where that is
+            // 2^8 above the one in use: until then numbers grow to 2^8, and lose nothing.
+            if (__ballot((most - m) * c > 8.f)) {
+                most = fmaxf(m, most);
+                const float alpha = __builtin_amdgcn_exp2f((m - most) * c);
+                m = most;
+                l *= alpha;
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+            }
+            const float mc = m * c;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     p[h][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[h][i], c, -mc));
-                    sum += p[h][i];
+                    l += p[h][i];
                 }
-            l = __builtin_fmaf(l, alpha, sum);
-            if (__ballot(alpha != 1.f))
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
                 const vec8<T> pf = narrow<T>(p[h / 2], h % 2);
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d)
-                    o[d] = mma(tile_at.columns(buffer(turn, 1), h * 16, d), pf, o[d]);
+                    o[d] = mma(tile_at.columns(from + other, h * 16, d), pf, o[d]);
             }
         }
         if (NB == 1) {
             __syncthreads();
-            start(at + kStep, 0);
-        } else {
-            turn ^= 1;
+            start(at + kStep, next);
         }
-        finish(at + kStep, turn);
+        finish(at + kStep, next);
         __syncthreads();
+    };
+    for (int at = stream * kTile, end = keys + stream * kTile; at < end; at += kStep) {
+        step(at, lds, NB > 1 ? lds2 : lds);
+        if (NB == 1) continue;
+        if ((at += kStep) >= end) break;
+        step(at, lds2, lds);
     }
     l = both_halves(l, [](float x, float y) { return x + y; });
     if constexpr (W::kStreams > 1)
@@ -511,7 +520,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
 {
     using W = Share<DP, WR, NB>;
     const Tile<T, DP> tile_at;
-    __shared__ __attribute__((aligned(1024))) char lds[W::kLds];
+    // (two arrays, so that a tile's loads are not waited for before the other is read)
+    __shared__ __attribute__((aligned(1024))) char lds[W::kFirst], lds2[NB > 1 ? W::kLds : 1024];
     const int head = blockIdx.x % s.heads, tile = tiles - 1 - blockIdx.x / s.heads;
     const Range in = find_sequence(s, tile, W::kRows);
     if (in.at < 0 || in.at >= in.length) return;
@@ -519,20 +529,19 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
     const int kv = head / (s.heads / s.kv_heads);
     const T *kp = k + in.first * s.k_ld + kv * s.dim, *vp = v + in.first * s.v_ld + kv * s.dim;
     const int keys = s.causal ? min(in.length, in.at + W::kRows) : in.length;
-    char *const own = lds + stream * NB * 2 * W::kTileBytes;
-    const auto buffer = [&](int turn, int side) { return own + (turn * 2 + side) * W::kTileBytes; };
+    const int own = stream * 2 * W::kTileBytes, other = own + W::kTileBytes;
     Loader<T, DP, WR, DIRECT> kt(wave % WR, s.k_ld, s.dim), vt(wave % WR, s.v_ld, s.dim);
-    const auto start = [&](int at, int turn) {
+    const auto start = [&](int at, char *to) {
         if (at >= keys) return;
-        kt.start(kp, s.k_ld, s.dim, at, in.length, buffer(turn, 0));
-        vt.start(vp, s.v_ld, s.dim, at, in.length, buffer(turn, 1));
+        kt.start(kp, s.k_ld, s.dim, at, in.length, to + own);
+        vt.start(vp, s.v_ld, s.dim, at, in.length, to + other);
     };
-    const auto finish = [&](int at, int turn) {
+    const auto finish = [&](int at, char *to) {
         if (at >= keys) return;
-        kt.finish(buffer(turn, 0));
-        vt.finish(buffer(turn, 1));
+        kt.finish(to + own);
+        vt.finish(to + other);
     };
-    start(stream * kTile, 0);
+    start(stream * kTile, lds);
     const float grow = gradient_scale<T>(parts, g.parts);
     const int row = row0 + column();
     const int64_t token = in.first + row;
@@ -547,12 +556,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
     const float dl = there ? delta[token * s.heads + head] : 0.f;
     const float c = s.scale * kLog2e;
     f32x16 acc[DP / 32] = {};
-    finish(stream * kTile, 0);
+    finish(stream * kTile, lds);
     __syncthreads();
     constexpr int kStep = W::kStreams * kTile;
-    for (int first = 0, turn = 0; first < keys; first += kStep) {
-        const int at = first + stream * kTile;
-        if (NB > 1) start(at + kStep, turn ^ 1);
+    const auto step = [&](int at, const char *from, char *next) {
+        if (NB > 1) start(at + kStep, next);
         if (at < keys && !(s.causal && at > row0 + 31)) {
             const bool mask = at + kTile > in.length || (s.causal && at + kTile - 1 > row0);
 #pragma unroll
@@ -560,8 +568,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
                 f32x16 p = {}, dp = {};
 #pragma unroll
                 for (int d = 0; d < DP / 16; ++d) {
-                    p = mma(tile_at.rows(buffer(turn, 0), h * 32, d), qf[d], p);
-                    dp = mma(tile_at.rows(buffer(turn, 1), h * 32, d), df[d], dp);
+                    p = mma(tile_at.rows(from + own, h * 32, d), qf[d], p);
+                    dp = mma(tile_at.rows(from + other, h * 32, d), df[d], dp);
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -569,6 +577,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
                     p[i] = e * ((dp[i] - dl) * grow);
                 }
                 if (mask) {
+                    asm volatile("");  // (a branch, not a selection per score)
                     const int end = s.causal ? min(in.length, row + 1) : in.length;
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
@@ -579,18 +588,22 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
                     const vec8<T> pf = narrow<T>(p, half);
 #pragma unroll
                     for (int d = 0; d < DP / 32; ++d)
-                        acc[d] = mma(tile_at.columns(buffer(turn, 0), h * 32 + half * 16, d), pf, acc[d]);
+                        acc[d] = mma(tile_at.columns(from + own, h * 32 + half * 16, d), pf, acc[d]);
                 }
             }
         }
         if (NB == 1) {
             __syncthreads();
-            start(at + kStep, 0);
-        } else {
-            turn ^= 1;
+            start(at + kStep, next);
         }
-        finish(at + kStep, turn);
+        finish(at + kStep, next);
         __syncthreads();
+    };
+    for (int at = stream * kTile, end = keys + stream * kTile; at < end; at += kStep) {
+        step(at, lds, NB > 1 ? lds2 : lds);
+        if (NB == 1) continue;
+        if ((at += kStep) >= end) break;
+        step(at, lds2, lds);
     }
     if constexpr (W::kStreams > 1)
         join_streams<WR, DP / 2>(lds, stream, wave % WR, [&](int k) { return acc[k / 16][k % 16]; },
@@ -611,7 +624,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dkv(
 {
     using W = Share<DP, WR, NB>;
     const Tile<T, DP> tile_at;
-    __shared__ __attribute__((aligned(1024))) char lds[W::kLds];
+    // (two arrays, so that a tile's loads are not waited for before the other is read)
+    __shared__ __attribute__((aligned(1024))) char lds[W::kFirst], lds2[NB > 1 ? W::kLds : 1024];
     // lse in base 2 and D of the tiles' queries
     __shared__ float s_row[W::kStreams][NB][2][kTile];
     const int kv = blockIdx.x % s.kv_heads, tile = blockIdx.x / s.kv_heads;
@@ -619,36 +633,35 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dkv(
     if (in.at < 0 || in.at >= in.length) return;
     const int wave = wave_number(), stream = wave / WR, row0 = in.at + wave % WR * 32;
     const int group = s.heads / s.kv_heads;
-    char *const own = lds + stream * NB * 2 * W::kTileBytes;
-    const auto buffer = [&](int turn, int side) { return own + (turn * 2 + side) * W::kTileBytes; };
+    const int own = stream * 2 * W::kTileBytes, other = own + W::kTileBytes;
     // the queries that see the workgroup's keys, a head of the group after the other
-    const int from = s.causal ? in.at / kTile * kTile : 0;
-    const int per_head = (in.length - from + kTile - 1) / kTile, steps = per_head * group;
+    const int begin = s.causal ? in.at / kTile * kTile : 0;
+    const int per_head = (in.length - begin + kTile - 1) / kTile, steps = per_head * group;
     Loader<T, DP, WR, DIRECT> qt(wave % WR, s.q_ld, s.dim), dt(wave % WR, g.d_ld, s.dim);
     float row_value[2];
-    const auto start = [&](int step, int turn) {
+    const auto start = [&](int step, char *to, int turn) {
         if (step >= steps) return;
-        const int head = kv * group + step / per_head, at = from + step % per_head * kTile;
-        qt.start(q + in.first * s.q_ld + head * s.dim, s.q_ld, s.dim, at, in.length, buffer(turn, 0));
-        dt.start(dout + in.first * g.d_ld + head * s.dim, g.d_ld, s.dim, at, in.length, buffer(turn, 1));
+        const int head = kv * group + step / per_head, at = begin + step % per_head * kTile;
+        qt.start(q + in.first * s.q_ld + head * s.dim, s.q_ld, s.dim, at, in.length, to + own);
+        dt.start(dout + in.first * g.d_ld + head * s.dim, g.d_ld, s.dim, at, in.length, to + other);
         if (wave % WR == 0) {
             const int row = at + (threadIdx.x & 63);
-            const int64_t to = (int64_t)(in.first + row) * s.heads + head;
+            const int64_t at_row = (int64_t)(in.first + row) * s.heads + head;
             // (behind the end: a score of 0 less infinity has no weight)
-            row_value[0] = row < in.length ? lse[to] * kLog2e : INFINITY;
-            row_value[1] = row < in.length ? delta[to] : 0.f;
+            row_value[0] = row < in.length ? lse[at_row] * kLog2e : INFINITY;
+            row_value[1] = row < in.length ? delta[at_row] : 0.f;
         }
     };
-    const auto finish = [&](int step, int turn) {
+    const auto finish = [&](int step, char *to, int turn) {
         if (step >= steps) return;
-        qt.finish(buffer(turn, 0));
-        dt.finish(buffer(turn, 1));
+        qt.finish(to + own);
+        dt.finish(to + other);
         if (wave % WR == 0) {
             s_row[stream][turn][0][threadIdx.x & 63] = row_value[0];
             s_row[stream][turn][1][threadIdx.x & 63] = row_value[1];
         }
     };
-    start(stream, 0);
+    start(stream, lds, 0);
     const float grow = gradient_scale<T>(parts, g.parts);
     const int row = row0 + column();
     const int64_t token = in.first + row;
@@ -660,12 +673,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dkv(
     }
     const float c = s.scale * kLog2e;
     f32x16 dka[DP / 32] = {}, dva[DP / 32] = {};
-    finish(stream, 0);
+    finish(stream, lds, 0);
     __syncthreads();
-    for (int first = 0, turn = 0; first < steps; first += W::kStreams) {
-        const int step = first + stream;
-        if (NB > 1) start(step + W::kStreams, turn ^ 1);
-        const int at = from + step % per_head * kTile;
+    const auto go = [&](int step, const char *from, char *next, int turn) {
+        const int then = NB > 1 ? turn ^ 1 : 0;
+        if (NB > 1) start(step + W::kStreams, next, then);
+        const int at = begin + step % per_head * kTile;
         if (step < steps && !(s.causal && at + kTile - 1 < row0)) {
             const bool mask = s.causal && at < row0 + 31;
 #pragma unroll
@@ -673,8 +686,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dkv(
                 f32x16 p = {}, dp = {};
 #pragma unroll
                 for (int d = 0; d < DP / 16; ++d) {
-                    p = mma(tile_at.rows(buffer(turn, 0), h * 32, d), kf[d], p);
-                    dp = mma(tile_at.rows(buffer(turn, 1), h * 32, d), vf[d], dp);
+                    p = mma(tile_at.rows(from + own, h * 32, d), kf[d], p);
+                    dp = mma(tile_at.rows(from + other, h * 32, d), vf[d], dp);
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -682,29 +695,35 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dkv(
                     p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -s_row[stream][turn][0][r]));
                     dp[i] = p[i] * ((dp[i] - s_row[stream][turn][1][r]) * grow);
                 }
-                if (mask)
+                if (mask) {
+                    asm volatile("");  // (a branch, not a selection per score)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) < row) p[i] = 0.f, dp[i] = 0.f;
+                }
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     const vec8<T> pf = narrow<T>(p, half), sf = narrow<T>(dp, half);
 #pragma unroll
                     for (int d = 0; d < DP / 32; ++d) {
-                        dva[d] = mma(tile_at.columns(buffer(turn, 1), h * 32 + half * 16, d), pf, dva[d]);
-                        dka[d] = mma(tile_at.columns(buffer(turn, 0), h * 32 + half * 16, d), sf, dka[d]);
+                        dva[d] = mma(tile_at.columns(from + other, h * 32 + half * 16, d), pf, dva[d]);
+                        dka[d] = mma(tile_at.columns(from + own, h * 32 + half * 16, d), sf, dka[d]);
                     }
                 }
             }
         }
         if (NB == 1) {
             __syncthreads();
-            start(step + W::kStreams, 0);
-        } else {
-            turn ^= 1;
+            start(step + W::kStreams, next, then);
         }
-        finish(step + W::kStreams, turn);
+        finish(step + W::kStreams, next, then);
         __syncthreads();
+    };
+    for (int step = stream, end = steps + stream; step < end; step += W::kStreams) {
+        go(step, lds, NB > 1 ? lds2 : lds, 0);
+        if (NB == 1) continue;
+        if ((step += W::kStreams) >= end) break;
+        go(step, lds2, lds, 1);
     }
     if constexpr (W::kStreams > 1) {
         const auto join = [&](f32x16(&acc)[DP / 32]) {
