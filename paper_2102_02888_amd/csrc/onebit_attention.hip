@@ -90,11 +90,14 @@ __device__ __forceinline__ Range find_sequence(const Sides &s, int tile, int row
 }
 
 // 8 numbers of a row of `dim` from `at` on; zeros behind its end and without a row.
-template <class T>
+// WHOLE: dim is a multiple of 8.
+template <bool WHOLE, class T>
 __device__ __forceinline__ vec8<T> load8(const T *row, int at, int dim, bool there)
 {
     T t[8] = {};
-    if (there) {
+    if (WHOLE) {
+        if (there && at < dim) __builtin_memcpy(t, row + at, sizeof t);
+    } else if (there) {
         if (at + 8 <= dim) {
             __builtin_memcpy(t, row + at, sizeof t);
         } else {
@@ -181,9 +184,9 @@ struct Tile {
 // 1 KB at a time; what is not there is read as zero by the buffer's bound.  Otherwise
 // through registers, number by number at a row's end.  start() begins a tile's loads,
 // finish() ends them (a barrier has to follow).
-template <class T, int DP, int WAVES, bool DIRECT>
+template <class T, int DP, int ROWS, int WAVES, bool DIRECT>
 struct Loader {
-    static constexpr int kEach = kTile * (DP / 8) / (WAVES * 64);  // pieces of a thread
+    static constexpr int kEach = ROWS * (DP / 8) / (WAVES * 64);  // pieces of a thread
     int wave, at[DIRECT ? kEach : 1];
     vec8<T> held[DIRECT ? 1 : kEach];
     __device__ __forceinline__ int piece(int k) const
@@ -215,7 +218,7 @@ struct Loader {
 #pragma unroll
             for (int k = 0; k < kEach; ++k) {
                 const int row = first + piece(k) / (DP / 8);
-                held[k] = load8(base + (int64_t)row * ld, piece(k) % (DP / 8) * 8, dim, row < rows);
+                held[k] = load8<false>(base + (int64_t)row * ld, piece(k) % (DP / 8) * 8, dim, row < rows);
             }
         }
     }
@@ -256,7 +259,8 @@ __device__ __forceinline__ float both_halves(float v, F f)
 }
 
 // Stores a lane's column of a [DP, 32] result: row `to` of a tensor, times `factor`.
-template <class T, int DP>
+// WHOLE: dim is a multiple of 8.
+template <bool WHOLE, class T, int DP>
 __device__ __forceinline__ void store_column(T *to, const f32x16 (&acc)[DP / 32], float factor,
                                              int dim)
 {
@@ -268,9 +272,9 @@ __device__ __forceinline__ void store_column(T *to, const f32x16 (&acc)[DP / 32]
             T t[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) t[k] = (T)(acc[c][i + k] * factor);
-            if (at + 4 <= dim) {
+            if (WHOLE ? at < dim : at + 4 <= dim) {
                 __builtin_memcpy(to + at, t, sizeof t);
-            } else {
+            } else if (!WHOLE) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     if (at + k < dim) to[at + k] = t[k];
@@ -280,11 +284,14 @@ __device__ __forceinline__ void store_column(T *to, const f32x16 (&acc)[DP / 32]
 
 // How a workgroup's four waves share its work: WR of them have 32 rows each (queries, or
 // keys for dk and dv), and WS streams of waves take every WS-th tile of the other side,
-// whose sums are joined at the end.  Each stream has its tiles in LDS, NB deep.
-template <int DP, int WR, int NB>
+// whose sums are joined at the end.  Each stream has STAGE rows of both of the other
+// sides in LDS, NB deep.
+template <int DP, int WR, int NB, int STAGE>
 struct Share {
     static constexpr int kStreams = kWaves / WR, kRows = 32 * WR;
-    static constexpr int kTileBytes = kTile * DP * 2, kLds = kStreams * 2 * kTileBytes;
+    static constexpr int kStage = STAGE;
+    static constexpr int kTileBytes = kStage * DP * 2, kRowsAt = kStreams * 2 * kTileBytes;
+    static constexpr int kLds = kRowsAt + kStreams * 2 * kStage * 4;  // two numbers of each row
     static_assert(kStreams * WR == kWaves, "four waves");
     static constexpr int kSums = (kWaves - WR) * 64 * (DP / 2 + 2) * 4;  // where streams are joined
     static constexpr int kFirst = kLds > kSums ? kLds : kSums;
@@ -320,7 +327,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention(const T *__restrict__
                                                            T *__restrict__ out,
                                                            float *__restrict__ lse, int tiles)
 {
-    using W = Share<DP, WR, NB>;
+    using W = Share<DP, WR, NB, kTile>;
     const Tile<T, DP> tile_at;
     // (two arrays, so that a tile's loads are not waited for before the other is read)
     __shared__ __attribute__((aligned(1024))) char lds[W::kFirst], lds2[NB > 1 ? W::kLds : 1024];
@@ -332,7 +339,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention(const T *__restrict__
     const T *kp = k + in.first * s.k_ld + kv * s.dim, *vp = v + in.first * s.v_ld + kv * s.dim;
     const int keys = s.causal ? min(in.length, in.at + W::kRows) : in.length;
     const int own = stream * 2 * W::kTileBytes, other = own + W::kTileBytes;
-    Loader<T, DP, WR, DIRECT> kt(wave % WR, s.k_ld, s.dim), vt(wave % WR, s.v_ld, s.dim);
+    Loader<T, DP, W::kStage, WR, DIRECT> kt(wave % WR, s.k_ld, s.dim), vt(wave % WR, s.v_ld, s.dim);
     const auto start = [&](int at, char *to) {
         if (at >= keys) return;
         kt.start(kp, s.k_ld, s.dim, at, in.length, to + own);
@@ -349,65 +356,68 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention(const T *__restrict__
     vec8<T> qf[DP / 16];
 #pragma unroll
     for (int d = 0; d < DP / 16; ++d)
-        qf[d] = load8(q + token * s.q_ld + head * s.dim, d * 16 + upper() * 8, s.dim, row < in.length);
+        qf[d] = load8<DIRECT>(q + token * s.q_ld + head * s.dim, d * 16 + upper() * 8, s.dim, row < in.length);
     const float c = s.scale * kLog2e;
     f32x16 o[DP / 32] = {};
     float m = -INFINITY, l = 0.f;
     finish(stream * kTile, lds);
     __syncthreads();
     constexpr int kStep = W::kStreams * kTile;
+    // A tile of keys; masked: some of them are not seen by a query of the wave.  (With
+    // the mask, a tile that a wave does not skip leaves each of its rows a key.)
+    const auto tile_sums = [&](int at, const char *from, bool masked) {
+        f32x16 p[2] = {};
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) p[h] = mma(tile_at.rows(from + own, h * 32, d), qf[d], p[h]);
+        if (masked) {
+            asm volatile("");  // (a branch, not a selection per score)
+            const int end = s.causal ? min(in.length, row + 1) : in.length;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) >= end) p[h][i] = -INFINITY;
+        }
+        float most = p[0][0];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, p[h][i]);
+        most = both_halves(most, [](float x, float y) { return fmaxf(x, y); });
+        // What is summed so far is brought to the new maximum only where that is
+        // 2^8 above the one in use: until then numbers grow to 2^8, and lose nothing.
+        if (__ballot((most - m) * c > 8.f)) {
+            most = fmaxf(m, most);
+            const float alpha = __builtin_amdgcn_exp2f((m - most) * c);
+            m = most;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+        }
+        const float mc = m * c;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                p[h][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[h][i], c, -mc));
+                l += p[h][i];
+            }
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const vec8<T> pf = narrow<T>(p[h / 2], h % 2);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+                o[d] = mma(tile_at.columns(from + other, h * 16, d), pf, o[d]);
+        }
+    };
     const auto step = [&](int at, const char *from, char *next) {
         if (NB > 1) start(at + kStep, next);
-        // (with the mask, a tile that a wave does not skip leaves each of its rows a key)
-        if (at < keys && !(s.causal && at > row0 + 31)) {
-            f32x16 p[2] = {};
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int d = 0; d < DP / 16; ++d)
-                    p[h] = mma(tile_at.rows(from + own, h * 32, d), qf[d], p[h]);
-            if (at + kTile > in.length || (s.causal && at + kTile - 1 > row0)) {
-                const int end = s.causal ? min(in.length, row + 1) : in.length;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) >= end) p[h][i] = -INFINITY;
-            }
-            float most = p[0][0];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) most = fmaxf(most, p[h][i]);
-            most = both_halves(most, [](float x, float y) { return fmaxf(x, y); });
-            // What is summed so far is brought to the new maximum only where that is
-            // 2^8 above the one in use: until then numbers grow to 2^8, and lose nothing.
-            if (__ballot((most - m) * c > 8.f)) {
-                most = fmaxf(m, most);
-                const float alpha = __builtin_amdgcn_exp2f((m - most) * c);
-                m = most;
-                l *= alpha;
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
-            }
-            const float mc = m * c;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    p[h][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[h][i], c, -mc));
-                    l += p[h][i];
-                }
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                const vec8<T> pf = narrow<T>(p[h / 2], h % 2);
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
-                    o[d] = mma(tile_at.columns(from + other, h * 16, d), pf, o[d]);
-            }
-        }
+        if (at < keys && !(s.causal && at > row0 + 31))
+            tile_sums(at, from, at + kTile > in.length || (s.causal && at + kTile - 1 > row0));
         if (NB == 1) {
             __syncthreads();
             start(at + kStep, next);
@@ -415,7 +425,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention(const T *__restrict__
         finish(at + kStep, next);
         __syncthreads();
     };
-    for (int at = stream * kTile, end = keys + stream * kTile; at < end; at += kStep) {
+    for (int at = stream * kTile, end = keys + at; at < end; at += kStep) {
         step(at, lds, NB > 1 ? lds2 : lds);
         if (NB == 1) continue;
         if ((at += kStep) >= end) break;
@@ -436,7 +446,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention(const T *__restrict__
                     o[k / 16][k % 16] = __builtin_fmaf(o[k / 16][k % 16], a, number(k) * b);
             });
     if (stream > 0 || row >= in.length) return;
-    store_column<T, DP>(out + token * s.o_ld + head * s.dim, o, 1.f / l, s.dim);
+    store_column<DIRECT, T, DP>(out + token * s.o_ld + head * s.dim, o, 1.f / l, s.dim);
     if (lse && upper() == 0) lse[token * s.heads + head] = m * s.scale + logf(l);
 }
 
@@ -470,7 +480,7 @@ __global__ __launch_bounds__(kThreads) void k_attention_delta(const T *__restric
         const T *a = dout + token * d_ld + head * s.dim, *b = out + token * s.o_ld + head * s.dim;
         float sum = 0.f;
         for (int at = lane * 8; at < s.dim; at += 64) {
-            const vec8<T> x = load8(a, at, s.dim, true), y = load8(b, at, s.dim, true);
+            const vec8<T> x = load8<false>(a, at, s.dim, true), y = load8<false>(b, at, s.dim, true);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 sum = __builtin_fmaf((float)x[k], (float)y[k], sum);
@@ -518,7 +528,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
     const float *__restrict__ delta, const float *__restrict__ parts, T *__restrict__ dq,
     int tiles)
 {
-    using W = Share<DP, WR, NB>;
+    using W = Share<DP, WR, NB, kTile>;
     const Tile<T, DP> tile_at;
     // (two arrays, so that a tile's loads are not waited for before the other is read)
     __shared__ __attribute__((aligned(1024))) char lds[W::kFirst], lds2[NB > 1 ? W::kLds : 1024];
@@ -530,7 +540,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
     const T *kp = k + in.first * s.k_ld + kv * s.dim, *vp = v + in.first * s.v_ld + kv * s.dim;
     const int keys = s.causal ? min(in.length, in.at + W::kRows) : in.length;
     const int own = stream * 2 * W::kTileBytes, other = own + W::kTileBytes;
-    Loader<T, DP, WR, DIRECT> kt(wave % WR, s.k_ld, s.dim), vt(wave % WR, s.v_ld, s.dim);
+    Loader<T, DP, W::kStage, WR, DIRECT> kt(wave % WR, s.k_ld, s.dim), vt(wave % WR, s.v_ld, s.dim);
     const auto start = [&](int at, char *to) {
         if (at >= keys) return;
         kt.start(kp, s.k_ld, s.dim, at, in.length, to + own);
@@ -549,49 +559,52 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
     vec8<T> qf[DP / 16], df[DP / 16];
 #pragma unroll
     for (int d = 0; d < DP / 16; ++d) {
-        qf[d] = load8(q + token * s.q_ld + head * s.dim, d * 16 + upper() * 8, s.dim, there);
-        df[d] = load8(dout + token * g.d_ld + head * s.dim, d * 16 + upper() * 8, s.dim, there);
+        qf[d] = load8<DIRECT>(q + token * s.q_ld + head * s.dim, d * 16 + upper() * 8, s.dim, there);
+        df[d] = load8<DIRECT>(dout + token * g.d_ld + head * s.dim, d * 16 + upper() * 8, s.dim, there);
     }
     const float l2 = there ? lse[token * s.heads + head] * kLog2e : 0.f;
-    const float dl = there ? delta[token * s.heads + head] : 0.f;
+    // (a product starts from -D instead of 0)
+    const float dl = there ? -delta[token * s.heads + head] : 0.f;
+    const f32x16 less_d = {dl, dl, dl, dl, dl, dl, dl, dl, dl, dl, dl, dl, dl, dl, dl, dl};
     const float c = s.scale * kLog2e;
     f32x16 acc[DP / 32] = {};
     finish(stream * kTile, lds);
     __syncthreads();
     constexpr int kStep = W::kStreams * kTile;
-    const auto step = [&](int at, const char *from, char *next) {
-        if (NB > 1) start(at + kStep, next);
-        if (at < keys && !(s.causal && at > row0 + 31)) {
-            const bool mask = at + kTile > in.length || (s.causal && at + kTile - 1 > row0);
+    // A tile of keys; masked: some of them are not seen by a query of the wave.
+    const auto tile_sums = [&](int at, const char *from, bool masked) {
+        const int end = s.causal ? min(in.length, row + 1) : in.length;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                f32x16 p = {}, dp = {};
+        for (int h = 0; h < 2; ++h) {
+            f32x16 p = {}, dp = less_d;
 #pragma unroll
-                for (int d = 0; d < DP / 16; ++d) {
-                    p = mma(tile_at.rows(from + own, h * 32, d), qf[d], p);
-                    dp = mma(tile_at.rows(from + other, h * 32, d), df[d], dp);
-                }
+            for (int d = 0; d < DP / 16; ++d) {
+                p = mma(tile_at.rows(from + own, h * 32, d), qf[d], p);
+                dp = mma(tile_at.rows(from + other, h * 32, d), df[d], dp);
+            }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -l2));
-                    p[i] = e * ((dp[i] - dl) * grow);
-                }
-                if (mask) {
-                    asm volatile("");  // (a branch, not a selection per score)
-                    const int end = s.causal ? min(in.length, row + 1) : in.length;
+            for (int i = 0; i < 16; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -l2)) * (dp[i] * grow);
+            }
+            if (masked) {
+                asm volatile("");
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) >= end) p[i] = 0.f;
-                }
+                for (int i = 0; i < 16; ++i)
+                    if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) >= end) p[i] = 0.f;
+            }
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const vec8<T> pf = narrow<T>(p, half);
+            for (int half = 0; half < 2; ++half) {
+                const vec8<T> pf = narrow<T>(p, half);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d)
-                        acc[d] = mma(tile_at.columns(from + own, h * 32 + half * 16, d), pf, acc[d]);
-                }
+                for (int d = 0; d < DP / 32; ++d)
+                    acc[d] = mma(tile_at.columns(from + own, h * 32 + half * 16, d), pf, acc[d]);
             }
         }
+    };
+    const auto step = [&](int at, const char *from, char *next) {
+        if (NB > 1) start(at + kStep, next);
+        if (at < keys && !(s.causal && at > row0 + 31))
+            tile_sums(at, from, at + kTile > in.length || (s.causal && at + kTile - 1 > row0));
         if (NB == 1) {
             __syncthreads();
             start(at + kStep, next);
@@ -599,7 +612,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
         finish(at + kStep, next);
         __syncthreads();
     };
-    for (int at = stream * kTile, end = keys + stream * kTile; at < end; at += kStep) {
+    for (int at = stream * kTile, end = keys + at; at < end; at += kStep) {
         step(at, lds, NB > 1 ? lds2 : lds);
         if (NB == 1) continue;
         if ((at += kStep) >= end) break;
@@ -612,7 +625,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
                 for (int k = 0; k < DP / 2; ++k) acc[k / 16][k % 16] += number(k);
             });
     if (stream == 0 && there)
-        store_column<T, DP>(dq + token * g.dq_ld + head * s.dim, acc, s.scale / grow, s.dim);
+        store_column<DIRECT, T, DP>(dq + token * g.dq_ld + head * s.dim, acc, s.scale / grow, s.dim);
 }
 
 template <class T, int DP, int WR, int NB, bool DIRECT>
@@ -622,12 +635,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dkv(
     const float *__restrict__ delta, const float *__restrict__ parts, T *__restrict__ dk,
     T *__restrict__ dv, int tiles)
 {
-    using W = Share<DP, WR, NB>;
+    using W = Share<DP, WR, NB, WR == 4 && DP <= 64 ? 2 * kTile : kTile>;
     const Tile<T, DP> tile_at;
     // (two arrays, so that a tile's loads are not waited for before the other is read)
     __shared__ __attribute__((aligned(1024))) char lds[W::kFirst], lds2[NB > 1 ? W::kLds : 1024];
-    // lse in base 2 and D of the tiles' queries
-    __shared__ float s_row[W::kStreams][NB][2][kTile];
     const int kv = blockIdx.x % s.kv_heads, tile = blockIdx.x / s.kv_heads;
     const Range in = find_sequence(s, tile, W::kRows);
     if (in.at < 0 || in.at >= in.length) return;
@@ -635,95 +646,109 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dkv(
     const int group = s.heads / s.kv_heads;
     const int own = stream * 2 * W::kTileBytes, other = own + W::kTileBytes;
     // the queries that see the workgroup's keys, a head of the group after the other
-    const int begin = s.causal ? in.at / kTile * kTile : 0;
-    const int per_head = (in.length - begin + kTile - 1) / kTile, steps = per_head * group;
-    Loader<T, DP, WR, DIRECT> qt(wave % WR, s.q_ld, s.dim), dt(wave % WR, g.d_ld, s.dim);
+    const int begin = s.causal ? in.at / W::kStage * W::kStage : 0;
+    const int per_head = (in.length - begin + W::kStage - 1) / W::kStage, steps = per_head * group;
+    Loader<T, DP, W::kStage, WR, DIRECT> qt(wave % WR, s.q_ld, s.dim), dt(wave % WR, g.d_ld, s.dim);
+    // lse in base 2 and -D of a tile's queries lie behind the tiles
+    const auto rows_of = [&](auto *buffer) {
+        using F = std::conditional_t<std::is_const_v<std::remove_pointer_t<decltype(buffer)>>, const float, float>;
+        return (F *)(buffer + W::kRowsAt) + stream * 2 * W::kStage;
+    };
+    // (waves 0 .. kStage / 64 - 1 of a stream bring 64 rows' each)
     float row_value[2];
-    const auto start = [&](int step, char *to, int turn) {
+    const auto start = [&](int step, char *to) {
         if (step >= steps) return;
-        const int head = kv * group + step / per_head, at = begin + step % per_head * kTile;
+        const int head = kv * group + step / per_head, at = begin + step % per_head * W::kStage;
         qt.start(q + in.first * s.q_ld + head * s.dim, s.q_ld, s.dim, at, in.length, to + own);
         dt.start(dout + in.first * g.d_ld + head * s.dim, g.d_ld, s.dim, at, in.length, to + other);
-        if (wave % WR == 0) {
-            const int row = at + (threadIdx.x & 63);
+        if (wave % WR < W::kStage / 64) {
+            const int row = at + wave % WR * 64 + (threadIdx.x & 63);
             const int64_t at_row = (int64_t)(in.first + row) * s.heads + head;
             // (behind the end: a score of 0 less infinity has no weight)
             row_value[0] = row < in.length ? lse[at_row] * kLog2e : INFINITY;
-            row_value[1] = row < in.length ? delta[at_row] : 0.f;
+            row_value[1] = row < in.length ? -delta[at_row] : 0.f;
         }
     };
-    const auto finish = [&](int step, char *to, int turn) {
+    const auto finish = [&](int step, char *to) {
         if (step >= steps) return;
         qt.finish(to + own);
         dt.finish(to + other);
-        if (wave % WR == 0) {
-            s_row[stream][turn][0][threadIdx.x & 63] = row_value[0];
-            s_row[stream][turn][1][threadIdx.x & 63] = row_value[1];
+        if (wave % WR < W::kStage / 64) {
+            const int r = wave % WR * 64 + (threadIdx.x & 63);
+            rows_of(to)[r] = row_value[0];
+            rows_of(to)[W::kStage + r] = row_value[1];
         }
     };
-    start(stream, lds, 0);
+    start(stream, lds);
     const float grow = gradient_scale<T>(parts, g.parts);
     const int row = row0 + column();
     const int64_t token = in.first + row;
     vec8<T> kf[DP / 16], vf[DP / 16];
 #pragma unroll
     for (int d = 0; d < DP / 16; ++d) {
-        kf[d] = load8(k + token * s.k_ld + kv * s.dim, d * 16 + upper() * 8, s.dim, row < in.length);
-        vf[d] = load8(v + token * s.v_ld + kv * s.dim, d * 16 + upper() * 8, s.dim, row < in.length);
+        kf[d] = load8<DIRECT>(k + token * s.k_ld + kv * s.dim, d * 16 + upper() * 8, s.dim, row < in.length);
+        vf[d] = load8<DIRECT>(v + token * s.v_ld + kv * s.dim, d * 16 + upper() * 8, s.dim, row < in.length);
     }
     const float c = s.scale * kLog2e;
     f32x16 dka[DP / 32] = {}, dva[DP / 32] = {};
-    finish(stream, lds, 0);
+    finish(stream, lds);
     __syncthreads();
-    const auto go = [&](int step, const char *from, char *next, int turn) {
-        const int then = NB > 1 ? turn ^ 1 : 0;
-        if (NB > 1) start(step + W::kStreams, next, then);
-        const int at = begin + step % per_head * kTile;
-        if (step < steps && !(s.causal && at + kTile - 1 < row0)) {
-            const bool mask = s.causal && at < row0 + 31;
+    // A tile of queries; masked: some of them are in front of a key of the wave.
+    const auto tile_sums = [&](int at, const char *from, const float *of_rows, bool masked) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                f32x16 p = {}, dp = {};
+        for (int h = 0; h < 2; ++h) {
+            f32x16 p = {}, dp;
 #pragma unroll
-                for (int d = 0; d < DP / 16; ++d) {
-                    p = mma(tile_at.rows(from + own, h * 32, d), kf[d], p);
-                    dp = mma(tile_at.rows(from + other, h * 32, d), vf[d], dp);
-                }
+            for (int i = 0; i < 16; ++i)
+                dp[i] = of_rows[W::kStage + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4)];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int r = h * 32 + upper() * 4 + i % 4 + 8 * (i / 4);
-                    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -s_row[stream][turn][0][r]));
-                    dp[i] = p[i] * ((dp[i] - s_row[stream][turn][1][r]) * grow);
-                }
-                if (mask) {
-                    asm volatile("");  // (a branch, not a selection per score)
+            for (int d = 0; d < DP / 16; ++d) {
+                p = mma(tile_at.rows(from + own, h * 32, d), kf[d], p);
+                dp = mma(tile_at.rows(from + other, h * 32, d), vf[d], dp);
+            }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) < row) p[i] = 0.f, dp[i] = 0.f;
-                }
+            for (int i = 0; i < 16; ++i) {
+                const int r = h * 32 + upper() * 4 + i % 4 + 8 * (i / 4);
+                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -of_rows[r]));
+                dp[i] = p[i] * (dp[i] * grow);
+            }
+            if (masked) {
+                asm volatile("");
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const vec8<T> pf = narrow<T>(p, half), sf = narrow<T>(dp, half);
+                for (int i = 0; i < 16; ++i)
+                    if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) < row) p[i] = 0.f, dp[i] = 0.f;
+            }
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) {
-                        dva[d] = mma(tile_at.columns(from + other, h * 32 + half * 16, d), pf, dva[d]);
-                        dka[d] = mma(tile_at.columns(from + own, h * 32 + half * 16, d), sf, dka[d]);
-                    }
+            for (int half = 0; half < 2; ++half) {
+                const vec8<T> pf = narrow<T>(p, half), sf = narrow<T>(dp, half);
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) {
+                    dva[d] = mma(tile_at.columns(from + other, h * 32 + half * 16, d), pf, dva[d]);
+                    dka[d] = mma(tile_at.columns(from + own, h * 32 + half * 16, d), sf, dka[d]);
                 }
             }
         }
+    };
+    const auto go = [&](int step, const char *from, char *next) {
+        if (NB > 1) start(step + W::kStreams, next);
+        const int at = begin + step % per_head * W::kStage;
+        if (step < steps)
+#pragma unroll 1
+            for (int t = at; t < min(at + W::kStage, in.length); t += kTile)
+                if (!(s.causal && t + kTile - 1 < row0))
+                    tile_sums(t, from + (t - at) * DP * 2, rows_of(from) + (t - at), s.causal && t < row0 + 31);
         if (NB == 1) {
             __syncthreads();
-            start(step + W::kStreams, next, then);
+            start(step + W::kStreams, next);
         }
-        finish(step + W::kStreams, next, then);
+        finish(step + W::kStreams, next);
         __syncthreads();
     };
     for (int step = stream, end = steps + stream; step < end; step += W::kStreams) {
-        go(step, lds, NB > 1 ? lds2 : lds, 0);
+        go(step, lds, NB > 1 ? lds2 : lds);
         if (NB == 1) continue;
         if ((step += W::kStreams) >= end) break;
-        go(step, lds2, lds, 1);
+        go(step, lds2, lds);
     }
     if constexpr (W::kStreams > 1) {
         const auto join = [&](f32x16(&acc)[DP / 32]) {
@@ -738,8 +763,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dkv(
         join(dva);
     }
     if (stream > 0 || row >= in.length) return;
-    store_column<T, DP>(dk + token * g.dk_ld + kv * s.dim, dka, s.scale / grow, s.dim);
-    store_column<T, DP>(dv + token * g.dv_ld + kv * s.dim, dva, 1.f, s.dim);
+    store_column<DIRECT, T, DP>(dk + token * g.dk_ld + kv * s.dim, dka, s.scale / grow, s.dim);
+    store_column<DIRECT, T, DP>(dv + token * g.dv_ld + kv * s.dim, dva, 1.f, s.dim);
 }
 
 template <class F>
