@@ -550,8 +550,9 @@ int onebit_layer_norm_grad(const void *dy, int32_t dy_dtype, int64_t dy_ld, cons
  * lowest number next to none unless all are; a row without a logit above -infinity
  * has no distribution: log-probabilities -infinity, entropy 0, gradient 0.  A NaN or
  * a logit of +infinity makes its row NaN.  Each call is one launch (per 2^21 rows),
- * needs no workspace, and reads every row once up to 65,536 logits.  vocab is at most
- * 2^30; rows = 0 and vocab = 0 are allowed. */
+ * needs no workspace, and reads every row once up to 16,384 logits (of 16 bits:
+ * 32,768), longer ones twice.  vocab is at most 2^30; rows = 0 and vocab = 0 are
+ * allowed. */
 
 /* logprobs[r] = log p of token ids[r], 0 where the id lies outside [0, vocab) (a place
  * that holds no token); entropy[r] = -sum of p log p; and the `top` (0 to 64) largest

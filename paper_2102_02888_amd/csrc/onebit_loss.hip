@@ -48,6 +48,7 @@ __device__ __forceinline__ void load_logits(const T *row, int at, int vocab, T (
 // thread is kCols logits from (c TH + thread) kCols on; -infinity behind the end.
 template <class T, int TH, int C>
 struct Held {
+    static constexpr bool kHeld = true;
     static constexpr int kWords = kCols * sizeof(T) / 4;
     uint32_t v[C][kWords];
     __device__ __forceinline__ Held(const T *row, int vocab)
@@ -87,6 +88,7 @@ struct Held {
 // ... one that does not fit: read again by every pass over it.
 template <class T, int TH>
 struct Held<T, TH, 0> {
+    static constexpr bool kHeld = false;
     const T *row;
     int vocab;
     __device__ __forceinline__ Held(const T *r, int n) : row(r), vocab(n) {}
@@ -103,6 +105,12 @@ struct Held<T, TH, 0> {
         }
     }
 };
+
+// Waves that a SIMD has to hold: two of the largest workgroups on a CU, so that one
+// computes while the other's loads and stores run (8,192 rows of 30,522 bf16 logits, the
+// distillation's gradient: 316 us with one, 214 with two).
+template <int TH>
+constexpr int kWavesFor = TH == 1024 ? 8 : 4;
 
 // LDS of a workgroup of TH threads.
 template <int TH>
@@ -125,29 +133,54 @@ __device__ __forceinline__ float most_of(float m, Shared<TH> &s)
 }
 
 // The row's largest logit, and of all of it the sum of e and, with ENT, of e d.
-// mine: the largest of this thread's.
-template <int TH, bool ENT, class Row>
+// mine: the largest of this thread's.  before: called before the barrier behind which
+// the sums are known.
+template <int TH, bool ENT, class Row, class Before>
 __device__ __forceinline__ void statistics(Row &row, float c, Shared<TH> &s, float &most,
-                                           float &mine, bool &mine_nan, float &sum, float &moment)
+                                           float &mine, bool &mine_nan, float &sum, float &moment,
+                                           Before before)
 {
     mine = kLowest;
-    row.each([&](float(&x)[kCols], int) {
-#pragma unroll
-        for (int k = 0; k < kCols; ++k) mine = fmaxf(mine, x[k]);
-    });
-    most = most_of<TH>(mine, s);
     float two[ENT ? 2 : 1] = {};
-    row.each([&](float(&x)[kCols], int) {
+    const auto add = [&](const float(&x)[kCols], float m) {
 #pragma unroll
         for (int k = 0; k < kCols; ++k) {
-            const float d = x[k] - most;
+            const float d = x[k] - m;
             const float e = __builtin_amdgcn_exp2f(d * c);
             two[0] += e;
             // (0 times -infinity is not wanted)
             if constexpr (ENT) two[1] = __builtin_fmaf(e, fmaxf(d, kLowest), two[1]);
         }
-    });
+    };
+    // brings the sums from this thread's maximum to another
+    const auto rebase = [&](float m) {
+        const float d = mine - m, f = __builtin_amdgcn_exp2f(d * c);
+        if constexpr (ENT) two[1] = f == 0.f ? 0.f : f * __builtin_fmaf(two[0], d, two[1]);
+        two[0] *= f;
+    };
+    if constexpr (Row::kHeld) {
+        row.each([&](float(&x)[kCols], int) {
+#pragma unroll
+            for (int k = 0; k < kCols; ++k) mine = fmaxf(mine, x[k]);
+        });
+        most = most_of<TH>(mine, s);
+        row.each([&](float(&x)[kCols], int) { add(x, most); });
+    } else {  // in one pass over the memory, each thread with a maximum of its own
+        row.each([&](float(&x)[kCols], int) {
+            float m = mine;
+#pragma unroll
+            for (int k = 0; k < kCols; ++k) m = fmaxf(m, x[k]);
+            if (m > mine) {
+                rebase(m);
+                mine = m;
+            }
+            add(x, m);
+        });
+        most = most_of<TH>(mine, s);
+        rebase(most);
+    }
     mine_nan = two[0] != two[0];
+    before();
     add_lanes<TH>(two, s.sums);
     sum = two[0];
     moment = ENT ? two[ENT ? 1 : 0] : 0.f;
@@ -179,38 +212,48 @@ struct SharedTop {
     float bound;
     int count;
     uint64_t best[TH / 64];
-    uint64_t key[kCandidates];
+    uint64_t key[kCandidates + 8];
 };
+
+// What top_of() needs before the barrier that it begins behind.
+template <int TH>
+__device__ __forceinline__ void prepare_top(float mine, SharedTop<TH> &s)
+{
+    constexpr int kPer = TH / SharedTop<TH>::kGroups;
+    const int tid = threadIdx.x;
+    float m = mine;
+    const auto larger = [](float a, float b) { return fmaxf(a, b); };
+    if constexpr (kPer == 8) m = over_lanes<8>(m, larger);
+    if constexpr (kPer == 4) m = larger(m, lanes<0xB1>(m)), m = larger(m, lanes<0x4E>(m));
+    if constexpr (kPer == 2) m = larger(m, lanes<0xB1>(m));
+    if (tid % kPer == 0) s.group[tid / kPer] = m;
+    if (tid == 0) s.count = 0;
+    for (int i = tid; i < kCandidates + 8; i += TH) s.key[i] = 0;  // below every key
+}
 
 // put(rank, column, logit) for the k largest of the row, by one thread each.
 template <int TH, class T, class Row, class Put>
 __device__ __forceinline__ void top_of(Row &row, const T *logits, int vocab, int k, float mine,
                                        bool mine_nan, SharedTop<TH> &s, Put put)
 {
-    constexpr int kGroups = SharedTop<TH>::kGroups, kPer = TH / kGroups;
+    constexpr int kGroups = SharedTop<TH>::kGroups;
     const int tid = threadIdx.x;
-    float m = mine;
-    const auto larger = [](float a, float b) { return fmaxf(a, b); };
-    if constexpr (kPer == 8) m = over_lanes<8>(m, larger);
-    if constexpr (kPer == 2) m = larger(m, lanes<0xB1>(m));
-    if (tid % kPer == 0) s.group[tid / kPer] = m;
-    if (tid == 0) s.count = 0;
-    __syncthreads();
-    if (tid < 64) {
-        // 20 bits of the order are enough for a bound
-        const uint32_t a = order_of(s.group[tid]);
-        const uint32_t b = kGroups > 64 ? order_of(s.group[kGroups - 64 + tid]) : 0;
-        uint32_t bound = 0;
-        for (int bit = 31; bit >= 12; --bit) {
-            const uint32_t at = bound | 1u << bit;
-            const int n = __popcll(__ballot(a >= at)) + __popcll(__ballot(b >= at));
-            if (n >= k) bound = at;
+    {
+        // Every wave looks at some of the groups' values: the one that fewer than k are
+        // above, and k or more are not below, is the k-th.
+        constexpr int kEach = kGroups / (TH / 64);
+        const int lane = tid & 63, first = __builtin_amdgcn_readfirstlane(tid >> 6) * kEach;
+        const float a = s.group[lane], b = kGroups > 64 ? s.group[kGroups - 64 + lane] : -INFINITY;
+        const float mine_of = s.group[first + lane % kEach];
+#pragma unroll 8
+        for (int i = 0; i < kEach; ++i) {
+            const float x = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine_of), i));
+            const int above = __popcll(__ballot(a > x)) + __popcll(__ballot(b > x));
+            const int reach = __popcll(__ballot(a >= x)) + __popcll(__ballot(b >= x));
+            // fewer than k groups with a logit above the lowest number (the largest of the
+            // others starts there): all logits
+            if (above < k && reach >= k && lane == 0) s.bound = x > kLowest ? x : -INFINITY;
         }
-        // fewer than k groups with a logit above the lowest number (the largest of the
-        // others starts there): all logits
-        const float x = bound <= 0x00800000u ? -INFINITY
-                      : __builtin_bit_cast(float, bound & 0x80000000u ? bound & 0x7fffffffu : ~bound);
-        if (tid == 0) s.bound = x;
     }
     __syncthreads();
     const float bound = s.bound;
@@ -238,7 +281,9 @@ __device__ __forceinline__ void top_of(Row &row, const T *logits, int vocab, int
         for (int i = tid; i < count; i += TH) {
             const uint64_t key = s.key[i];
             int rank = 0;
-            for (int j = 0; j < count; ++j) rank += s.key[j] > key;
+            for (int j = 0; j < count; j += 8)  // (zeros behind the last)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) rank += s.key[j + k] > key;
             if (rank < k) give(rank, key);
         }
     } else {  // many equal logits: one after another, each by a pass over the row in memory
@@ -285,7 +330,7 @@ struct Values {
 };
 
 template <class T, int TH, int C, bool ENT, bool TOP>
-__global__ __launch_bounds__(TH) void k_logprobs(const T *__restrict__ logits, Logits in,
+__global__ __launch_bounds__(TH, (kWavesFor<TH>)) void k_logprobs(const T *__restrict__ logits, Logits in,
                                                  const void *__restrict__ ids, int ids_bytes,
                                                  Values out)
 {
@@ -302,7 +347,11 @@ __global__ __launch_bounds__(TH) void k_logprobs(const T *__restrict__ logits, L
     }
     float most, mine, sum, moment;
     bool mine_nan;
-    statistics<TH, ENT>(row, in.scale * kLog2e, s, most, mine, mine_nan, sum, moment);
+    __shared__ SharedTop<TOP ? TH : 64> top;
+    statistics<TH, ENT>(row, in.scale * kLog2e, s, most, mine, mine_nan, sum, moment, [&] {
+        if constexpr (TOP) prepare_top(mine, top);
+    });
+    if constexpr (TOP && TH == 64) __syncthreads();
     const float ln = logf(sum);  // -infinity without a distribution
     const auto logprob = [&](float x) {
         return sum == 0.f ? -INFINITY : (x - most) * in.scale - ln;
@@ -312,7 +361,6 @@ __global__ __launch_bounds__(TH) void k_logprobs(const T *__restrict__ logits, L
         if (ENT) out.entropy[r] = sum == 0.f ? 0.f : ln - in.scale * (moment / sum);
     }
     if constexpr (TOP) {
-        __shared__ SharedTop<TH> top;
         top_of<TH>(row, at, in.vocab, out.top, mine, mine_nan, top,
                    [&](int rank, int column, float x) {
             const int64_t to = r * out.top + rank;
@@ -328,7 +376,7 @@ __global__ __launch_bounds__(TH) void k_logprobs(const T *__restrict__ logits, L
 // dx_v = scale (g ([v = t] - p_v) - h p_v (log p_v + entropy)); a row without a token
 // or without a distribution gets zeros.
 template <class T, int TH, int C, bool ENT>
-__global__ __launch_bounds__(TH) void k_logprobs_grad(const T *logits, Logits in,
+__global__ __launch_bounds__(TH, (kWavesFor<TH>)) void k_logprobs_grad(const T *logits, Logits in,
                                                       const void *__restrict__ ids, int ids_bytes,
                                                       const float *__restrict__ grad_logprob,
                                                       const float *__restrict__ grad_entropy,
@@ -356,7 +404,7 @@ __global__ __launch_bounds__(TH) void k_logprobs_grad(const T *logits, Logits in
     float most, mine, sum, moment;
     bool mine_nan;
     const float c = in.scale * kLog2e;
-    statistics<TH, ENT>(row, c, s, most, mine, mine_nan, sum, moment);
+    statistics<TH, ENT>(row, c, s, most, mine, mine_nan, sum, moment, [] {});
     const float ln = logf(sum);
     const float entropy = ENT ? ln - in.scale * (moment / sum) : 0.f;
     if (threadIdx.x == 0) {
@@ -409,85 +457,73 @@ __device__ __forceinline__ float load_teacher(const Teacher &t, int64_t at)
 
 // loss = sum of q_k (log q_k - log p of its token), q = softmax(scale teacher's logits)
 // over the alternatives whose token is one of the vocabulary;
-// dx_v = g scale ((sum of q) p_v - sum of q_k over id_k = v).  The first wave reads the
-// alternatives and, once the row is written, sets the columns that they name.
+// dx_v = g scale ((sum of q) p_v - sum of q_k over id_k = v).  A thread brings an
+// alternative to LDS and, once the row is written, sets the column that it names; the
+// first wave makes the teacher's softmax and the loss of them.
 template <class T, int TH, int C, bool GRAD>
-__global__ __launch_bounds__(TH) void k_distill(const T *logits, Logits in, Teacher t,
+__global__ __launch_bounds__(TH, (kWavesFor<TH>)) void k_distill(const T *logits, Logits in, Teacher t,
                                                 const float *__restrict__ grad_loss, T *dlogits,
                                                 int64_t d_ld, float *__restrict__ loss)
 {
-    constexpr int kPer = kMostTeacher / 64;
     __shared__ Shared<TH> s;
-    __shared__ int32_t s_id[GRAD ? kMostTeacher : 1];
-    __shared__ float s_q[GRAD ? kMostTeacher : 1];
-    const int lane = threadIdx.x;
+    // an alternative's token (-1: none), teacher's and student's logit, and q
+    __shared__ __attribute__((aligned(16))) int32_t s_id[kMostTeacher];
+    __shared__ float s_z[kMostTeacher], s_x[kMostTeacher];
+    __shared__ __attribute__((aligned(16))) float s_q[kMostTeacher];
+    const int tid = threadIdx.x, top = (t.top + 3) & ~3;
     const int64_t r = in.first + blockIdx.x;
     const T *at = logits + r * in.ld;
-    Held<T, TH, C> row(at, in.vocab);
-    int32_t id[kPer];
-    float x[kPer], q[kPer], logq[kPer];
-    float total = 0.f;
-    if (lane < 64) {
-        float z[kPer], m = kLowest;
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            const int j = k * 64 + lane;
-            id[k] = -1, z[k] = -INFINITY, x[k] = 0.f;
-            if (j >= t.top) continue;
+#pragma unroll 1
+    for (int j = tid; j < top; j += TH) {
+        int id = -1;
+        float z = -INFINITY;
+        if (j < t.top) {
             const int64_t v = load_id(t.ids, t.ids_bytes, r * t.top + j);
-            if (v < 0 || v >= in.vocab) continue;
-            id[k] = (int32_t)v;
-            z[k] = load_teacher(t, r * t.ld + j);
-            x[k] = (float)at[v];
-            m = fmaxf(m, z[k]);
+            if (v >= 0 && v < in.vocab) id = (int)v, z = load_teacher(t, r * t.ld + j);
         }
-        m = over_lanes<64>(m, [](float a, float b) { return fmaxf(a, b); });
-        float sum[1] = {0.f};
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            logq[k] = (z[k] - m) * in.scale;
-            q[k] = __builtin_amdgcn_exp2f((z[k] - m) * (in.scale * kLog2e));
-            sum[0] += q[k];
-        }
-        add_lanes<64>(sum, nullptr);
-        const float ln = logf(sum[0]), inverse = sum[0] == 0.f ? 0.f : 1.f / sum[0];
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            q[k] *= inverse;
-            logq[k] -= ln;
-            if (GRAD) s_id[k * 64 + lane] = id[k], s_q[k * 64 + lane] = q[k];
-        }
-        // 1, 0 without a teacher, NaN
-        total = sum[0] == 0.f ? 0.f : sum[0] * inverse == sum[0] * inverse ? 1.f : NAN;
-        // (the logits that were looked up are waited for here, before the barriers
-        // behind which the row may be written in place)
-        float seen = 0.f;
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) seen += x[k];
-        if (lane == 0) s.taken[0] = seen, s.taken[1] = total;
+        s_id[j] = id, s_z[j] = z, s_q[j] = 0.f;
     }
+    Held<T, TH, C> row(at, in.vocab);
     float most, mine, sum, moment;
     bool mine_nan;
     const float c = in.scale * kLog2e;
-    statistics<TH, false>(row, c, s, most, mine, mine_nan, sum, moment);
+    statistics<TH, false>(row, c, s, most, mine, mine_nan, sum, moment, [&] {
+        // (the logits that are looked up are waited for here, before the barrier behind
+        // which the row may be written in place)
+#pragma unroll 1
+        for (int j = tid; j < t.top; j += TH) s_x[j] = s_id[j] >= 0 ? (float)at[s_id[j]] : 0.f;
+        if (tid >= 64) return;
+        float m = kLowest, all[1] = {0.f};
+#pragma unroll 1
+        for (int j = tid; j < t.top; j += 64) m = fmaxf(m, s_z[j]);
+        m = over_lanes<64>(m, [](float a, float b) { return fmaxf(a, b); });
+#pragma unroll 1
+        for (int j = tid; j < t.top; j += 64) all[0] += __builtin_amdgcn_exp2f((s_z[j] - m) * c);
+        add_lanes<64>(all, nullptr);
+        if (tid == 0) s.taken[0] = m, s.taken[1] = all[0];
+    });
     if constexpr (TH == 64) __syncthreads();
-    const float ln = logf(sum);
-    if (lane < 64 && loss) {
+    const float teacher_most = s.taken[0], teacher_sum = s.taken[1];
+    if (tid < 64) {
+        const float ln = logf(sum), teacher_ln = logf(teacher_sum);
+        const float inverse = teacher_sum == 0.f ? 0.f : 1.f / teacher_sum;
         float part[1] = {0.f};
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            const float logp = sum == 0.f ? -INFINITY : (x[k] - most) * in.scale - ln;
-            if (id[k] >= 0 && q[k] != 0.f) part[0] += q[k] * (logq[k] - logp);
+#pragma unroll 1
+        for (int j = tid; j < t.top; j += 64) {
+            const float q = __builtin_amdgcn_exp2f((s_z[j] - teacher_most) * c) * inverse;
+            const float logq = (s_z[j] - teacher_most) * in.scale - teacher_ln;
+            const float logp = sum == 0.f ? -INFINITY : (s_x[j] - most) * in.scale - ln;
+            if (s_id[j] >= 0 && q != 0.f) part[0] += q * (logq - logp);
+            s_q[j] = q;
         }
         add_lanes<64>(part, nullptr);
-        if (lane == 0) loss[r] = part[0];
+        if (tid == 0 && loss) loss[r] = part[0];
     }
     if constexpr (GRAD) {
         T *to = dlogits + r * d_ld;
-        total = s.taken[1];
         const float g = grad_loss[r] * in.scale;
-        const bool zero = sum == 0.f || total == 0.f;
-        const float a = zero ? 0.f : g * total / sum;
+        const bool zero = sum == 0.f || teacher_sum == 0.f;
+        const float a = zero ? 0.f : g * (teacher_sum / teacher_sum) / sum;  // (NaN stays)
         row.each([&](float(&v)[kCols], int col) {
             if (col >= in.vocab) return;
 #pragma unroll
@@ -498,28 +534,42 @@ __global__ __launch_bounds__(TH) void k_distill(const T *logits, Logits in, Teac
         // Two stores to one place: the first has arrived before the second is sent.
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (lane < 64 && !zero) {
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) {
-                if (id[k] < 0) continue;
-                float all = 0.f;  // a token that is named twice: each lane writes the same
-                for (int j = 0; j < t.top; ++j) all += s_id[j] == id[k] ? s_q[j] : 0.f;
-                to[id[k]] = (T)(a * __builtin_amdgcn_exp2f((x[k] - most) * c) - g * all);
+        if (!zero)
+#pragma unroll 1
+            for (int j = tid; j < t.top; j += TH) {
+                const int id = s_id[j];
+                if (id < 0) continue;
+                float all = 0.f;  // a token that is named twice: each thread writes the same
+                for (int k = 0; k < top; k += 4) {
+                    const int4 others = *(const int4 *)(s_id + k);
+                    const float4 theirs = *(const float4 *)(s_q + k);
+                    all += others.x == id ? theirs.x : 0.f;
+                    all += others.y == id ? theirs.y : 0.f;
+                    all += others.z == id ? theirs.z : 0.f;
+                    all += others.w == id ? theirs.w : 0.f;
+                }
+                to[id] = (T)(a * __builtin_amdgcn_exp2f((s_x[j] - most) * c) - g * all);
             }
-        }
     }
 }
 
-// Calls f(threads, pieces) for rows of this many logits.
-template <class F>
+// Calls f(threads, pieces) for rows of this many logits.  A row in registers is read
+// once; a longer one twice, the second time from the caches for the most part.  us with
+// 1,024 threads, from registers and from memory (a floor of 74 for reading, 147 with the
+// gradient): 8,192 rows of 30,522 bf16 logits 109 and 128, gradient 186 and 295,
+// distillation 215 and 319; 4,096 rows of 30,522 fp32 ones 80 and 80, 236 and 233, 341
+// and 247 (half the row's registers are left, and two workgroups no longer fit a CU).
+// 8,192 rows of 9,000 bf16 ones 76 with 1,024 threads.
+template <class T, class F>
 void with_shape(int64_t vocab, F &&f)
 {
     using std::integral_constant;
     if (vocab <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
     else if (vocab <= 2048) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
     else if (vocab <= 8192) f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    else if (vocab <= 16384) f(integral_constant<int, 512>{}, integral_constant<int, 4>{});
+    else if constexpr (sizeof(T) == 4) f(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
     else if (vocab <= 32768) f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
-    else if (vocab <= 65536) f(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
     else f(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
 }
 
@@ -591,7 +641,7 @@ int onebit_logprobs_forward(const void *logits, int32_t dtype, int64_t ld, int64
     if (rows == 0 || !(logprobs || entropy || top)) return ONEBIT_OK;
     const Values out{logprobs, entropy, top_ids, top_logprobs, top, ids_bytes};
     with_type(dtype, [&](auto *t) {
-        with_shape(vocab, [&](auto threads, auto pieces) {
+        with_shape<std::remove_pointer_t<decltype(t)>>(vocab, [&](auto threads, auto pieces) {
             with_flag(entropy, [&](auto ent) {
                 with_flag(top > 0, [&](auto tops) {
                     using T = std::remove_pointer_t<decltype(t)>;
@@ -624,7 +674,7 @@ int onebit_logprobs_grad(const void *logits, int32_t dtype, int64_t ld, int64_t 
     if (rows == 0) return ONEBIT_OK;
     const Values out{logprobs, entropy, nullptr, nullptr, 0, 4};
     with_type(dtype, [&](auto *t) {
-        with_shape(vocab, [&](auto threads, auto pieces) {
+        with_shape<std::remove_pointer_t<decltype(t)>>(vocab, [&](auto threads, auto pieces) {
             with_flag(grad_entropy || entropy, [&](auto ent) {
                 using T = std::remove_pointer_t<decltype(t)>;
                 constexpr int TH = decltype(threads)::value, C = decltype(pieces)::value;
@@ -653,7 +703,7 @@ int onebit_distill_forward(const void *logits, int32_t dtype, int64_t ld, int64_
     if (!loss && rows > 0) return fail(ONEBIT_EINVAL, "loss is NULL");
     if (rows == 0) return ONEBIT_OK;
     with_type(dtype, [&](auto *t) {
-        with_shape(vocab, [&](auto threads, auto pieces) {
+        with_shape<std::remove_pointer_t<decltype(t)>>(vocab, [&](auto threads, auto pieces) {
             using T = std::remove_pointer_t<decltype(t)>;
             constexpr int TH = decltype(threads)::value, C = decltype(pieces)::value;
             with_rows(rows, [&](int64_t first, int blocks) {
@@ -682,7 +732,7 @@ int onebit_distill_grad(const void *logits, int32_t dtype, int64_t ld, int64_t r
     if (!grad_loss && rows > 0) return fail(ONEBIT_EINVAL, "grad_loss is NULL");
     if (rows == 0) return ONEBIT_OK;
     with_type(dtype, [&](auto *t) {
-        with_shape(vocab, [&](auto threads, auto pieces) {
+        with_shape<std::remove_pointer_t<decltype(t)>>(vocab, [&](auto threads, auto pieces) {
             using T = std::remove_pointer_t<decltype(t)>;
             constexpr int TH = decltype(threads)::value, C = decltype(pieces)::value;
             with_rows(rows, [&](int64_t first, int blocks) {

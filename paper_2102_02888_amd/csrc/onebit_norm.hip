@@ -204,38 +204,47 @@ __global__ __launch_bounds__(kThreads<L>) void k_norm_grad(
     }
 }
 
-// Adds the workgroups' sums: 16 columns a workgroup, whose 16 groups of threads take
-// every sixteenth sum.
-constexpr int kJoinCols = 16, kJoinParts = 16;
+// Adds the workgroups' sums: 16 columns a workgroup, whose 64 groups of threads take
+// every 64th sum, up to kJoinAhead of them loaded before the first is added.
+constexpr int kJoinCols = 16, kJoinParts = 64, kJoinAhead = 8;
 
-__global__ __launch_bounds__(256) void k_norm_join(const float *__restrict__ partial, int parts,
-                                                   int width, void *__restrict__ dweight,
-                                                   void *__restrict__ dbias, int dtype,
-                                                   int accumulate)
+template <class G>
+__device__ __forceinline__ void put_sum(void *to, int k, float s, int accumulate)
+{
+    G *q = (G *)to + k;
+    *q = (G)(accumulate ? (float)*q + s : s);
+}
+
+__global__ __launch_bounds__(kJoinCols *kJoinParts) void k_norm_join(
+    const float *__restrict__ partial, int parts, int width, void *__restrict__ dweight,
+    void *__restrict__ dbias, int dtype, int accumulate)
 {
     __shared__ float sums[kJoinParts][kJoinCols];
     const int col = threadIdx.x % kJoinCols, part = threadIdx.x / kJoinCols;
     const int at = blockIdx.x * kJoinCols + col;
     float s = 0.f;
     if (at < 2 * width)
-        for (int p = part; p < parts; p += kJoinParts) s += partial[(int64_t)p * 2 * width + at];
+        for (int first = part; first < parts; first += kJoinParts * kJoinAhead) {
+            float v[kJoinAhead];
+#pragma unroll
+            for (int k = 0; k < kJoinAhead; ++k) {
+                const int p = first + k * kJoinParts;
+                v[k] = p < parts ? partial[(int64_t)p * 2 * width + at] : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < kJoinAhead; ++k) s += v[k];
+        }
     sums[part][col] = s;
     __syncthreads();
     if (part > 0 || at >= 2 * width) return;
+#pragma unroll
     for (int p = 1; p < kJoinParts; ++p) s += sums[p][col];
     void *to = at < width ? dweight : dbias;
     const int k = at < width ? at : at - width;
     if (!to) return;
-    if (dtype == ONEBIT_GRAD_F32) {
-        float *q = (float *)to + k;
-        *q = accumulate ? *q + s : s;
-    } else if (dtype == ONEBIT_GRAD_BF16) {
-        __bf16 *q = (__bf16 *)to + k;
-        *q = (__bf16)(accumulate ? (float)*q + s : s);
-    } else {
-        _Float16 *q = (_Float16 *)to + k;
-        *q = (_Float16)(accumulate ? (float)*q + s : s);
-    }
+    if (dtype == ONEBIT_GRAD_F32) put_sum<float>(to, k, s, accumulate);
+    else if (dtype == ONEBIT_GRAD_BF16) put_sum<__bf16>(to, k, s, accumulate);
+    else put_sum<_Float16>(to, k, s, accumulate);
 }
 
 // Calls f(L, C) for rows of this width.
@@ -369,7 +378,7 @@ int onebit_layer_norm_grad(const void *dy, int32_t dy_dtype, int64_t dy_ld, cons
         });
     TRY(launched("layer norm gradient launch"));
     if (!sums) return ONEBIT_OK;
-    k_norm_join<<<(int)((2 * width + kJoinCols - 1) / kJoinCols), 256, 0, st>>>(
+    k_norm_join<<<(int)((2 * width + kJoinCols - 1) / kJoinCols), kJoinCols * kJoinParts, 0, st>>>(
         partial, parts, (int)width, dweight, dbias, dw_dtype, accumulate);
     return launched("layer norm join launch");
 }
