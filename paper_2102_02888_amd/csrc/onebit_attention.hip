@@ -321,7 +321,7 @@ __device__ __forceinline__ void join_streams(char *lds, int stream, int row_wave
 // running maximum m and sum l per query (both halves of a wave have a query; m is the
 // same in both, l adds up at the end).
 template <class T, int DP, int WR, int NB, bool DIRECT>
-__global__ __launch_bounds__(kThreads, 2) void k_attention(const T *__restrict__ q,
+__global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_attention(const T *__restrict__ q,
                                                            const T *__restrict__ k,
                                                            const T *__restrict__ v, Sides s,
                                                            T *__restrict__ out,
@@ -522,7 +522,7 @@ struct Grads {
 };
 
 template <class T, int DP, int WR, int NB, bool DIRECT>
-__global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
+__global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_attention_dq(
     const T *__restrict__ dout, const T *__restrict__ q, const T *__restrict__ k,
     const T *__restrict__ v, Sides s, Grads g, const float *__restrict__ lse,
     const float *__restrict__ delta, const float *__restrict__ parts, T *__restrict__ dq,
@@ -629,7 +629,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attention_dq(
 }
 
 template <class T, int DP, int WR, int NB, bool DIRECT>
-__global__ __launch_bounds__(kThreads, 2) void k_attention_dkv(
+__global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_attention_dkv(
     const T *__restrict__ dout, const T *__restrict__ q, const T *__restrict__ k,
     const T *__restrict__ v, Sides s, Grads g, const float *__restrict__ lse,
     const float *__restrict__ delta, const float *__restrict__ parts, T *__restrict__ dk,
@@ -784,8 +784,7 @@ void with_shape(int dim, bool few, bool direct, F &&f)
         else f(padded, waves, depth, std::false_type{});
     };
     auto by_waves = [&](auto padded) {
-        constexpr int kFew = decltype(padded)::value <= 64 ? 1 : 2;
-        if (few) go(padded, integral_constant<int, kFew>{}, integral_constant<int, 1>{});
+        if (few) go(padded, integral_constant<int, 1>{}, integral_constant<int, 1>{});
         else go(padded, integral_constant<int, 4>{}, integral_constant<int, 2>{});
     };
     if (dim <= 32) by_waves(integral_constant<int, 32>{});
@@ -838,10 +837,19 @@ int check_tiles(int64_t tokens, int64_t sequences, int heads)
 
 int tile_count(int64_t tokens, int64_t sequences, int rows) { return (int)(tokens / rows + sequences); }
 
-bool few_tiles(int64_t tokens, int64_t sequences, int heads)
+// Whether a call has so few tiles of 128 rows that its waves share the other side of 32
+// rows instead.  us with whole tiles and so: attention of one prompt of 512 with 16 heads
+// of 64 (80 tiles) 12.7 and 7.8, of 8,192 with 2 heads (130) 104 and 48, of 2,048 with 16
+// (272) 32 and 27 causal, 33 and 40 not, of four of 1,024 (576) 27 and 39; with heads of
+// 128, one of 4,096 with 4 (132) 77 and 50, of 1,000 with 32 (256) 26 and 45.  Gradients,
+// whose tiles of keys go through the queries of all heads on them: 2,048 with 16 heads on
+// 4 of 128 (68 tiles of keys) 629 and 177, eleven documents with 12 on 4 of 80 (228) 278
+// and 160, four of 1,024 with 8 of 128 (288) 137 and 126, of 64 (576) 77 and 98.
+bool few_tiles(int64_t tokens, int64_t sequences, int heads, int most)
 {
-    return (tokens / 128 + sequences) * heads <= 512;
+    return (tokens / 128 + sequences) * heads <= most;
 }
+constexpr int kFewQueryTiles = 255, kFewKeyTiles = 320;
 
 int delta_blocks(int64_t tokens, int heads)
 {
@@ -873,7 +881,7 @@ int onebit_attention_forward(const void *q, int64_t q_ld, const void *k, int64_t
     const Sides s{q_ld, k_ld, v_ld, out_ld, starts, (int)tokens, (int)sequences,
                   heads, kv_heads, dim, scale, causal};
     with_half(dtype, [&](auto *t) {
-        with_shape(dim, few_tiles(tokens, sequences, heads),
+        with_shape(dim, few_tiles(tokens, sequences, heads, kFewQueryTiles),
                    direct_side(k, k_ld, dim) && direct_side(v, v_ld, dim),
                    [&](auto padded, auto waves, auto depth, auto direct) {
             using T = std::remove_pointer_t<decltype(t)>;
@@ -928,7 +936,7 @@ int onebit_attention_grad(const void *dout, int64_t dout_ld, const void *q, int6
         using T = std::remove_pointer_t<decltype(t)>;
         k_attention_delta<T><<<g.parts, kThreads, 0, st>>>((const T *)dout, dout_ld,
                                                            (const T *)out, s, delta, parts);
-        with_shape(dim, few_tiles(tokens, sequences, kv_heads),
+        with_shape(dim, few_tiles(tokens, sequences, kv_heads, kFewKeyTiles),
                    direct_side(q, q_ld, dim) && direct_side(dout, dout_ld, dim),
                    [&](auto padded, auto waves, auto depth, auto direct) {
             const int tiles = tile_count(tokens, sequences, 32 * waves);
@@ -937,7 +945,7 @@ int onebit_attention_grad(const void *dout, int64_t dout_ld, const void *q, int6
                     (const T *)dout, (const T *)q, (const T *)k, (const T *)v, s, g, lse, delta,
                     parts, (T *)dk, (T *)dv, tiles);
         });
-        with_shape(dim, few_tiles(tokens, sequences, heads),
+        with_shape(dim, few_tiles(tokens, sequences, heads, kFewQueryTiles),
                    direct_side(k, k_ld, dim) && direct_side(v, v_ld, dim),
                    [&](auto padded, auto waves, auto depth, auto direct) {
             const int tiles = tile_count(tokens, sequences, 32 * waves);
