@@ -144,6 +144,15 @@ def test_attention(dev, lengths, heads, kv, dim, kind, causal):
     _check(dev, lengths, heads, kv, dim, kind, causal, extra=dim % 2 * 3)
 
 
+@pytest.mark.parametrize("heads,kv", [(64, 64), (120, 60)])
+@pytest.mark.parametrize("dim,shift", [(16, 0), (33, 0), (64, 0), (64, 1), (80, 0), (128, 0), (128, 1)])
+@pytest.mark.parametrize("kind,causal", [("bf16", True), ("f16", False)])
+def test_calls_of_many_tiles(dev, heads, kv, dim, shift, kind, causal):
+    """More than 320 tiles of 128 tokens and a head: whole tiles go through the keys (the
+    other tests' calls are small, and their waves share them)."""
+    _check(dev, [130, 64, 257], heads, kv, dim, kind, causal, extra=2, shift=shift)
+
+
 @pytest.mark.parametrize("dim", [8, 32, 40, 64, 72, 80, 96, 104, 128])
 @pytest.mark.parametrize("extra,shift", [(1, 0), (0, 1), (2, 2), (16, 8)])
 def test_alignments(dev, dim, extra, shift):
