@@ -102,8 +102,12 @@ __device__ __forceinline__ float centre(float (&x)[C][kCols], int lane, int widt
 template <int L>
 constexpr int kThreads = L < 256 ? 256 : L;
 
+// y = (x - mean) r w + b, a row per L threads, weight and bias in registers over all rows
+// of a workgroup.  Memory bounds it: 131,072 bf16 rows of 1,024 (537 MB) take 90 us (5.9
+// TB/s; a copy of 8 GiB reaches 6.8), 10,007 fp32 rows of 771 to bf16 11 us (4.2 TB/s), 16
+// rows 3.7.
 template <class T, class O, int L, int C>
-__global__ __launch_bounds__(kThreads<L>) void k_norm(const T *__restrict__ x, int64_t x_ld,
+__global__ __launch_bounds__(kThreads<L>) void k_layer_norm(const T *__restrict__ x, int64_t x_ld,
                                                       int64_t rows, int width,
                                                       const void *__restrict__ weight,
                                                       const void *__restrict__ bias, int w_dtype,
@@ -133,9 +137,11 @@ __global__ __launch_bounds__(kThreads<L>) void k_norm(const T *__restrict__ x, i
 
 // dx = r (g - mean(g) - z mean(g z)) with z = (x - mean) r and g = dy w, and the sums
 // of dy z and dy over the workgroup's rows, in registers until the last one.  Sums of
-// a column are added in an order that depends on the rows and the width alone.
+// a column are added in an order that depends on the rows and the width alone.  Memory
+// bounds it: 131,072 bf16 rows of 1,024 (805 MB) take 152 us (5.3 TB/s), 10,007 fp32 rows
+// of 771 19.  Loading a row ahead costs a workgroup per CU in registers: 190 us.
 template <class D, class T, int L, int C>
-__global__ __launch_bounds__(kThreads<L>) void k_norm_grad(
+__global__ __launch_bounds__(kThreads<L>) void k_layer_norm_grad(
     const D *dy, int64_t dy_ld, const T *__restrict__ x, int64_t x_ld, int64_t rows,
     int width, const void *__restrict__ weight, int w_dtype, float eps, T *dx,
     int64_t dx_ld, float *__restrict__ partial)
@@ -205,7 +211,8 @@ __global__ __launch_bounds__(kThreads<L>) void k_norm_grad(
 }
 
 // Adds the workgroups' sums: 16 columns a workgroup, whose 64 groups of threads take
-// every 64th sum, up to kJoinAhead of them loaded before the first is added.
+// every 64th sum, up to kJoinAhead of them loaded before the first is added (1,024 sums
+// of 2,048 columns: 6 us; 16 groups of 16 threads, one load behind the other, 29).
 constexpr int kJoinCols = 16, kJoinParts = 64, kJoinAhead = 8;
 
 template <class G>
@@ -215,7 +222,7 @@ __device__ __forceinline__ void put_sum(void *to, int k, float s, int accumulate
     *q = (G)(accumulate ? (float)*q + s : s);
 }
 
-__global__ __launch_bounds__(kJoinCols *kJoinParts) void k_norm_join(
+__global__ __launch_bounds__(kJoinCols *kJoinParts) void k_layer_norm_join(
     const float *__restrict__ partial, int parts, int width, void *__restrict__ dweight,
     void *__restrict__ dbias, int dtype, int accumulate)
 {
@@ -323,7 +330,7 @@ int onebit_layer_norm_forward(const void *x, int32_t x_dtype, int64_t x_ld, int6
                 using T = std::remove_pointer_t<decltype(t)>;
                 using O = std::remove_pointer_t<decltype(o)>;
                 constexpr int L = decltype(lanes)::value, C = decltype(pieces)::value;
-                k_norm<T, O, L, C><<<blocks_for(rows, L, kMostBlocks), kThreads<L>, 0,
+                k_layer_norm<T, O, L, C><<<blocks_for(rows, L, kMostBlocks), kThreads<L>, 0,
                                      (hipStream_t)stream>>>((const T *)x, x_ld, rows, (int)width,
                                                             weight, bias, w_dtype, eps, (O *)y,
                                                             y_ld);
@@ -370,7 +377,7 @@ int onebit_layer_norm_grad(const void *dy, int32_t dy_dtype, int64_t dy_ld, cons
                     using T = std::remove_pointer_t<decltype(t)>;
                     constexpr int L = decltype(lanes)::value, C = decltype(pieces)::value;
                     parts = blocks_for(rows, L, kMostParts);
-                    k_norm_grad<D, T, L, C><<<parts, kThreads<L>, 0, st>>>(
+                    k_layer_norm_grad<D, T, L, C><<<parts, kThreads<L>, 0, st>>>(
                         (const D *)dy, dy_ld, (const T *)x, x_ld, rows, (int)width, weight,
                         w_dtype, eps, (T *)dx, dx_ld, partial);
                 });
@@ -378,7 +385,7 @@ int onebit_layer_norm_grad(const void *dy, int32_t dy_dtype, int64_t dy_ld, cons
         });
     TRY(launched("layer norm gradient launch"));
     if (!sums) return ONEBIT_OK;
-    k_norm_join<<<(int)((2 * width + kJoinCols - 1) / kJoinCols), kJoinCols * kJoinParts, 0, st>>>(
+    k_layer_norm_join<<<(int)((2 * width + kJoinCols - 1) / kJoinCols), kJoinCols * kJoinParts, 0, st>>>(
         partial, parts, (int)width, dweight, dbias, dw_dtype, accumulate);
     return launched("layer norm join launch");
 }
