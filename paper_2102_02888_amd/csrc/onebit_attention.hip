@@ -883,6 +883,7 @@ int onebit_attention_forward(const void *q, int64_t q_ld, const void *k, int64_t
     if ((uintptr_t)lse % 4) return fail(ONEBIT_EALIGN, "lse is not 4-byte aligned");
     TRY(check_tiles(tokens, sequences, heads));
     if (tokens == 0 || sequences == 0) return ONEBIT_OK;
+    if (tokens == 1) q_ld = out_ld = width, k_ld = v_ld = kv_width;  // (not looked at above)
     const Sides s{q_ld, k_ld, v_ld, out_ld, starts, (int)tokens, (int)sequences,
                   heads, kv_heads, dim, scale, causal};
     with_half(dtype, [&](auto *t) {
@@ -932,6 +933,10 @@ int onebit_attention_grad(const void *dout, int64_t dout_ld, const void *q, int6
     if ((uintptr_t)workspace % 16) return fail(ONEBIT_EALIGN, "workspace is not 16-byte aligned");
     TRY(check_tiles(tokens, sequences, heads));
     if (tokens == 0 || sequences == 0) return ONEBIT_OK;
+    if (tokens == 1) {  // (not looked at above)
+        dout_ld = q_ld = out_ld = dq_ld = width;
+        k_ld = v_ld = dk_ld = dv_ld = kv_width;
+    }
     const Sides s{q_ld, k_ld, v_ld, out_ld, starts, (int)tokens, (int)sequences,
                   heads, kv_heads, dim, scale, causal};
     const Grads g{dout_ld, dq_ld, dk_ld, dv_ld, delta_blocks(tokens, heads)};

@@ -170,6 +170,24 @@ def test_tokens_outside_the_sequences(dev, kind, causal):
     _check(dev, [40], 2, 2, 128, kind, causal, before=129, after=1)
 
 
+def test_one_token_of_a_wide_row(dev):
+    """The distance to a next token means nothing where there is none."""
+    import paper_2102_02888_amd as ob
+    q = torch.randn(4, 2, 64, device=dev, generator=_gen(dev, 1)).bfloat16()
+    starts = torch.tensor([0, 1], dtype=torch.int32, device=dev)
+    for t in (q[:1], q[:1].as_strided((1, 2, 64), (0, 64, 1)), q[:1].as_strided((1, 2, 64), (3, 64, 1))):
+        out, lse = torch.empty_like(q[:1]), torch.empty(1, 2, device=dev)
+        ob.onebit_attention_forward(t, t, t, starts, out, lse)
+        assert torch.equal(out, q[:1])  # the one key has all the weight
+        L, p = ob.lib(), t.data_ptr()
+        for ld in (-4, 0, 1 << 50):
+            out.zero_()
+            assert L.onebit_attention_forward(p, ld, p, ld, p, ld, 1, 1, 2, 2, 64, starts.data_ptr(), 1, 1,
+                                              0.125, out.data_ptr(), ld, None,
+                                              torch.cuda.current_stream().cuda_stream) == 0
+            assert torch.equal(out, q[:1])
+
+
 def test_many_short_sequences(dev):
     """More sequences than a wave looks at in a round, and than 64 rounds of it."""
     _check(dev, [1 + k % 5 for k in range(70)], 2, 1, 16, "bf16", True)

@@ -259,6 +259,21 @@ def test_masked_places_are_not_read(dev):
     assert float(v[0]) == 0 and float(v[2]) == 0
 
 
+def test_rows_without_logits(dev):
+    """A vocabulary of none: no token, no distribution, no alternative."""
+    import paper_2102_02888_amd as ob
+    x, ids = torch.zeros(3, 0, device=dev), torch.zeros(3, dtype=torch.int64, device=dev)
+    v, e = torch.full((3,), 7.0, device=dev), torch.full((3,), 7.0, device=dev)
+    top, logp = torch.zeros(3, 2, dtype=torch.int64, device=dev), torch.zeros(3, 2, device=dev)
+    ob.onebit_logprobs_forward(x, ids, v, entropy=e, top_ids=top, top_logprobs=logp)
+    assert not bool(v.any()) and not bool(e.any())
+    assert bool((top == -1).all()) and bool((logp == -INF).all())
+    ob.onebit_logprobs_grad(x, ids, v, x, logprobs=v)
+    v.fill_(7.0)
+    ob.onebit_distill_grad(x, top, logp, e, x, loss=v)
+    assert not bool(v.any())
+
+
 def test_outputs_that_are_left_out(dev):
     import paper_2102_02888_amd as ob
     x = _logits(20, 5000, torch.bfloat16, dev, 0, 1)
