@@ -33,32 +33,41 @@ constexpr int kCandidates = 512;
 constexpr float kLowest = -FLT_MAX;
 constexpr float kLog2e = 1.44269504088896340736f;
 
+// kCols logits as the words that they are; -infinity behind the end.
 template <class T>
-__device__ __forceinline__ void load_logits(const T *row, int at, int vocab, T (&v)[kCols])
-{
-    if (at + kCols <= vocab) {
-        __builtin_memcpy(v, row + at, sizeof v);
-    } else {
+struct Piece {
+    static constexpr int kWords = kCols * sizeof(T) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T *row, int at, int vocab)
+    {
+        if (at + kCols <= vocab) {
+            __builtin_memcpy(w, row + at, sizeof w);
+        } else {
+            T t[kCols];
 #pragma unroll
-        for (int k = 0; k < kCols; ++k) v[k] = at + k < vocab ? row[at + k] : (T)-INFINITY;
+            for (int k = 0; k < kCols; ++k) t[k] = at + k < vocab ? row[at + k] : (T)-INFINITY;
+            __builtin_memcpy(w, t, sizeof w);
+        }
     }
-}
+    __device__ __forceinline__ void widen(float (&x)[kCols]) const
+    {
+        T t[kCols];
+        __builtin_memcpy(t, w, sizeof t);
+#pragma unroll
+        for (int k = 0; k < kCols; ++k) x[k] = (float)t[k];
+    }
+};
 
 // A row of logits over the TH threads of a workgroup, in registers: piece c of a
 // thread is kCols logits from (c TH + thread) kCols on; -infinity behind the end.
 template <class T, int TH, int C>
 struct Held {
     static constexpr bool kHeld = true;
-    static constexpr int kWords = kCols * sizeof(T) / 4;
-    uint32_t v[C][kWords];
+    Piece<T> piece[C];
     __device__ __forceinline__ Held(const T *row, int vocab)
     {
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            T t[kCols];
-            load_logits(row, (c * TH + (int)threadIdx.x) * kCols, vocab, t);
-            __builtin_memcpy(v[c], t, sizeof t);
-        }
+        for (int c = 0; c < C; ++c) piece[c].load(row, (c * TH + (int)threadIdx.x) * kCols, vocab);
     }
     // f(kCols logits as fp32, the first one's column).  Every pass converts them anew:
     // the compiler is kept from holding what another pass made of them, which would
@@ -68,17 +77,10 @@ struct Held {
     {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            uint32_t w[kWords];
 #pragma unroll
-            for (int k = 0; k < kWords; ++k) {
-                w[k] = v[c][k];
-                asm volatile("" : "+v"(w[k]));
-            }
-            T t[kCols];
-            __builtin_memcpy(t, w, sizeof t);
+            for (int k = 0; k < Piece<T>::kWords; ++k) asm volatile("" : "+v"(piece[c].w[k]));
             float x[kCols];
-#pragma unroll
-            for (int k = 0; k < kCols; ++k) x[k] = (float)t[k];
+            piece[c].widen(x);
             f(x, (c * TH + (int)threadIdx.x) * kCols);
             __builtin_amdgcn_sched_barrier(0);  // one piece at a time, for the same reason
         }
@@ -96,11 +98,10 @@ struct Held<T, TH, 0> {
     __device__ __forceinline__ void each(F f)
     {
         for (int at = (int)threadIdx.x * kCols; at < vocab; at += TH * kCols) {
-            T v[kCols];
-            load_logits(row, at, vocab, v);
+            Piece<T> piece;
+            piece.load(row, at, vocab);
             float x[kCols];
-#pragma unroll
-            for (int k = 0; k < kCols; ++k) x[k] = (float)v[k];
+            piece.widen(x);
             f(x, at);
         }
     }
