@@ -15,34 +15,37 @@ from .onebit import _GRAD_DTYPES, _stream
 __all__ = ["layer_norm_workspace", "onebit_layer_norm_forward", "onebit_layer_norm_grad"]
 
 
-def _vectors(width, **named):
-    """(pointers, type code) of 1-D tensors of `width` elements that share a
-    type; None stays None."""
-    pointers, dtype = [], None
-    for name, t in named.items():
-        if t is None:
-            pointers.append(None)
-            continue
-        if not isinstance(t, torch.Tensor):
-            raise TypeError("%s must be a torch.Tensor" % name)
-        if t.dtype not in _GRAD_DTYPES or dtype not in (None, t.dtype):
-            raise TypeError("%s must be float32, bfloat16 or float16, and of one type, got %s"
-                            % (" and ".join(named), t.dtype))
-        if not t.is_cuda:
-            raise ValueError("%s must be a GPU tensor" % name)
-        if t.dim() != 1 or t.shape[0] != width or (width > 1 and t.stride(0) != 1):
-            raise ValueError("%s must be 1-D with %d elements side by side, got %s with strides %s"
-                             % (name, width, tuple(t.shape), t.stride()))
-        dtype = t.dtype
-        pointers.append(t.data_ptr())
-    return pointers, _GRAD_DTYPES.get(dtype, 0)
+def _vector(t, name, width):
+    """Pointer of a 1-D tensor of `width` elements side by side (None stays None)."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.dtype not in _GRAD_DTYPES:
+        raise TypeError("%s must be float32, bfloat16 or float16, got %s" % (name, t.dtype))
+    if not t.is_cuda:
+        raise ValueError("%s must be a GPU tensor" % name)
+    if t.shape != (width,) or (width > 1 and t.stride(0) != 1):
+        raise ValueError("%s must be 1-D with %d elements side by side, got %s with strides %s"
+                         % (name, width, tuple(t.shape), t.stride()))
+    return t.data_ptr()
+
+
+def _pair(one, two, names, width):
+    """(pointers, type code) of two such tensors that share a type."""
+    pointers = _vector(one, names[0], width), _vector(two, names[1], width)
+    if one is not None and two is not None and one.dtype != two.dtype:
+        raise TypeError("%s and %s must be of one type, got %s and %s"
+                        % (*names, one.dtype, two.dtype))
+    given = two if one is None else one
+    return pointers, 0 if given is None else _GRAD_DTYPES[given.dtype]
 
 
 def onebit_layer_norm_forward(x, y, weight=None, bias=None, eps=1e-5, stream=None):
     """y = (x - mean) / sqrt(var + eps) * weight + bias of each row."""
     xp, xcode, xld, rows, width = _matrix(x, "x")
     yp, ycode, yld, _, _ = _matrix(y, "y", rows, width)
-    (wp, bp), wcode = _vectors(width, weight=weight, bias=bias)
+    (wp, bp), wcode = _pair(weight, bias, ("weight", "bias"), width)
     _one_device(*(t for t in (x, y, weight, bias) if t is not None))
     call("onebit_layer_norm_forward", xp, xcode, xld, rows, width, wp, bp, wcode, float(eps), yp,
          ycode, yld, _stream(stream))
@@ -67,8 +70,8 @@ def onebit_layer_norm_grad(grad_y, x, grad_x, workspace, weight=None, grad_weigh
         gp, gcode, gld, _, _ = _matrix(grad_x, "grad_x", rows, width)
         if gcode != xcode:
             raise TypeError("grad_x must be of x's type %s, got %s" % (x.dtype, grad_x.dtype))
-    (wp,), wcode = _vectors(width, weight=weight)
-    (dwp, dbp), dwcode = _vectors(width, grad_weight=grad_weight, grad_bias=grad_bias)
+    wp, wcode = _vector(weight, "weight", width), 0 if weight is None else _GRAD_DTYPES[weight.dtype]
+    (dwp, dbp), dwcode = _pair(grad_weight, grad_bias, ("grad_weight", "grad_bias"), width)
     _one_device(*(t for t in (x, grad_y, grad_x, weight, grad_weight, grad_bias)
                   if t is not None))
     work = None
