@@ -619,7 +619,8 @@ int onebit_distill_grad(const void *logits, int32_t dtype, int64_t ld, int64_t r
  * Scores, their exponentials and all sums are fp32, P and its gradient are rounded to
  * the operands' type between two products.  Tokens in no sequence are neither read
  * nor written.  A NaN or an infinity among a sequence's numbers may make any result of
- * that sequence and head NaN; others are not touched by it. */
+ * that sequence and head NaN; others are not touched by it.  A key whose score is below
+ * fp32's range, -infinity, has no weight; a query that sees no other gets NaN. */
 
 /* lse (may be NULL): tokens x heads floats, the logarithm of the sum over j of
  * exp(scale q_i k_j).  scale is in (0, 1e30].

@@ -12,6 +12,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <type_traits>
@@ -31,6 +32,7 @@ template <class T>
 using vec8 = T __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kTile = 64;       // rows of the other side's tile in LDS
 constexpr int kMostDim = 128;
@@ -363,7 +365,8 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
         qf[d] = load8<DIRECT>(q + token * s.q_ld + head * s.dim, d * 16 + upper() * 8, s.dim, row < in.length);
     const float c = s.scale * kLog2e;
     f32x16 o[DP / 32] = {};
-    float m = -INFINITY, l = 0.f;
+    // (the maximum in base 2, finite from below: scores of -infinity have no weight)
+    float m = -FLT_MAX, l = 0.f;
     finish(stream * kTile, lds);
     __syncthreads();
     constexpr int kStep = W::kStreams * kTile;
@@ -392,9 +395,10 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
         most = both_halves(most, [](float x, float y) { return fmaxf(x, y); });
         // What is summed so far is brought to the new maximum only where that is
         // 2^8 above the one in use: until then numbers grow to 2^8, and lose nothing.
-        if (__ballot((most - m) * c > 8.f)) {
+        most *= c;
+        if (__ballot(most - m > 8.f)) {
             most = fmaxf(m, most);
-            const float alpha = __builtin_amdgcn_exp2f((m - most) * c);
+            const float alpha = __builtin_amdgcn_exp2f(m - most);
             m = most;
             l *= alpha;
 #pragma unroll
@@ -402,12 +406,11 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
         }
-        const float mc = m * c;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                p[h][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[h][i], c, -mc));
+                p[h][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[h][i], c, -m));
                 l += p[h][i];
             }
 #pragma unroll
@@ -441,8 +444,8 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
             [&](int k) { return k < DP / 2 ? o[k / 16][k % 16] : k == DP / 2 ? m : l; },
             [&](auto number) {
                 const float m2 = number(DP / 2), l2 = number(DP / 2 + 1), most = fmaxf(m, m2);
-                const float a = __builtin_amdgcn_exp2f((m - most) * c);
-                const float b = __builtin_amdgcn_exp2f((m2 - most) * c);
+                const float a = __builtin_amdgcn_exp2f(m - most);
+                const float b = __builtin_amdgcn_exp2f(m2 - most);
                 m = most;
                 l = __builtin_fmaf(l, a, l2 * b);
 #pragma unroll
@@ -451,7 +454,7 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
             });
     if (stream > 0 || row >= in.length) return;
     store_column<DIRECT, T, DP>(out + token * s.o_ld + head * s.dim, o, 1.f / l, s.dim);
-    if (lse && upper() == 0) lse[token * s.heads + head] = m * s.scale + logf(l);
+    if (lse && upper() == 0) lse[token * s.heads + head] = m * kLn2 + logf(l);
 }
 
 // ---------------------------------------------------------------------------

@@ -202,6 +202,34 @@ def test_sharp_softmax_and_given_scale(dev, kind):
     _check(dev, [300, 64], 2, 1, 64, kind, False, scale=1.3)
 
 
+@pytest.mark.parametrize("tokens,heads", [(300, 2), (300, 200)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_scores_below_fp32(dev, tokens, heads, causal):
+    """Keys whose scores are below fp32's least number, -infinity, have no weight, also
+    where a query sees nothing else in many tiles.  The other scores are 0, each of which
+    has the same weight: out is the mean of their values, all of which are 1, and
+    lse the logarithm of their number, within its 2^-21 (1 + |lse|) of rounding.  A query
+    that sees no other key has no softmax: NaN, and lse -infinity."""
+    import paper_2102_02888_amd as ob
+    q, k, v = (torch.zeros(tokens, heads, 64, dtype=torch.bfloat16, device=dev) for _ in range(3))
+    starts = torch.tensor([0, tokens], dtype=torch.int32, device=dev)
+    q[:, :, 0] = 3e38
+    v += 1
+    low = torch.zeros(tokens, dtype=torch.bool, device=dev)
+    low[:200] = True
+    low[210:250] = True
+    k[low, :, 0] = -3e38
+    v[low] = 5.0
+    out, lse = torch.empty_like(q), torch.empty(tokens, heads, device=dev)
+    ob.onebit_attention_forward(q, k, v, starts, out, lse, causal=causal)
+    n = (~low).cumsum(0) if causal else (~low).sum().expand(tokens)
+    some = n > 0
+    assert bool((out[some] == 1).all())
+    want = n[some].double().log()[:, None]
+    assert bool(((lse[some] - want).abs() <= 2.0 ** -21 * (1 + want)).all())
+    assert bool(out[~some].isnan().all()) and bool((lse[~some] == -torch.inf).all())
+
+
 @pytest.mark.parametrize("dstd", [1e-6, 3e-5, 300.0])
 def test_gradients_of_any_size_in_fp16(dev, dstd):
     """dS is scaled before it is rounded to fp16, whose least number is 6e-8."""
