@@ -323,7 +323,7 @@ __device__ __forceinline__ void join_streams(char *lds, int stream, int row_wave
 // running maximum m and sum l per query (both halves of a wave have a query; m is the
 // same in both, l adds up at the end).  The matrix cores and the VALU take turns on a
 // SIMD, and bound it together: packed prompts of up to 8,192 tokens, 16 heads on 4 of 128,
-// 375 us (1.0 PFLOP/s), 64 sequences of 512 with 16 heads of 64, not causal, 105 us (0.65).
+// 375 to 390 us (1.0 PFLOP/s), 64 sequences of 512 with 16 heads of 64, not causal, 105 us (0.65).
 // Four waves with 32 rows each, four workgroups a CU with heads of 64: with 64 rows a wave
 // and half the LDS reads 192 us, with tiles of 128 keys and two workgroups 129.
 template <class T, int DP, int WR, int NB, bool DIRECT>
