@@ -289,14 +289,14 @@ __device__ __forceinline__ void top_of(Row &row, const T *logits, int vocab, int
         }
     } else {  // many equal logits: one after another, each by a pass over the row in memory
         Held<T, TH, 0> again(logits, vocab);
-        uint64_t last = ~0ull;
+        uint64_t most = ~0ull;  // (itself a key: NaN in the first column)
         for (int r = 0; r < k; ++r) {
             uint64_t best = 0;
             again.each([&](float(&x)[kCols], int at) {
 #pragma unroll
                 for (int i = 0; i < kCols; ++i) {
                     const uint64_t key = key_of(x[i], at + i);
-                    if (at + i < vocab && key < last && key > best) best = key;
+                    if (at + i < vocab && key <= most && key > best) best = key;
                 }
             });
             for (int d = 1; d < 64; d *= 2) {
@@ -310,7 +310,7 @@ __device__ __forceinline__ void top_of(Row &row, const T *logits, int vocab, int
                 __syncthreads();
             }
             if (tid == 0) give(r, best);
-            last = best;
+            most = best - 1;
         }
     }
     for (int r = min(vocab, k) + tid; r < k; r += TH) put(r, -1, -INFINITY);

@@ -431,3 +431,29 @@ def test_refusals(dev):
         ob.onebit_distill_forward(x, t_ids, z, "loss")
     with pytest.raises(ob.OnebitError, match="loss is NULL"):
         ob.onebit_distill_forward(x, t_ids, z, None)
+
+
+@pytest.mark.parametrize("vocab", [600, 9000, 30522, 40000, 70000])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_nan_in_the_first_column_among_many_candidates(dev, vocab, kind):
+    """NaN is above all and the lowest index first, also where more logits than LDS has
+    room for reach the bound: rows of NaN only, and NaN in column 0 of rows that are
+    otherwise equal, masked or NaN but for one."""
+    import paper_2102_02888_amd as ob
+    nan = float("nan")
+    x = torch.full((5, vocab), nan, device=dev)
+    x[1] = 1.25
+    x[2] = -INF
+    x[3] = 0.5
+    x[4, 5] = 2.0
+    x[1:4, 0] = nan
+    x[2:4, -1] = -nan
+    x = x.to(TYPES[kind])
+    best = torch.sort(x.float().cpu(), dim=1, descending=True, stable=True).indices.to(dev)
+    assert best[0, :3].tolist() == [0, 1, 2] and best[2, :3].tolist() == [0, vocab - 1, 1]
+    for k in (1, 6, 64):
+        top = torch.full((5, k), 99, dtype=torch.int64, device=dev)
+        logp = torch.zeros(5, k, device=dev)
+        ob.onebit_logprobs_forward(x, None, None, top_ids=top, top_logprobs=logp)
+        assert torch.equal(top, best[:, :k]), k
+        assert bool(logp.isnan().all())
