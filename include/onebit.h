@@ -570,10 +570,11 @@ int onebit_logprobs_forward(const void *logits, int32_t dtype, int64_t ld, int64
 /* The logits' gradient of  sum over r of grad_logprobs[r] logprobs[r] + grad_entropy[r]
  * entropy[r]  (either may be NULL, for zeros):
  *   dlogits[r][v] = scale (g ([v = ids[r]] - p_v) - h p_v (log p_v + entropy[r])),
- * and zeros for a row whose id lies outside the vocabulary.  It needs nothing of the
- * forward call, and gives logprobs and entropy itself where they are not NULL, so that
- * a training step whose weights are known takes this call alone.  dlogits: logits'
- * type, d_ld apart; it may be the logits' own buffer (same ld).
+ * and zeros for a row whose id lies outside the vocabulary or that has no distribution;
+ * a NaN in g or h makes any other row NaN, as one among the logits does.  It needs
+ * nothing of the forward call, and gives logprobs and entropy itself where they are not
+ * NULL, so that a training step whose weights are known takes this call alone.
+ * dlogits: logits' type, d_ld apart; it may be the logits' own buffer (same ld).
  * Errors: as above. */
 int onebit_logprobs_grad(const void *logits, int32_t dtype, int64_t ld, int64_t rows,
                          int64_t vocab, const void *ids, int32_t ids_bytes, float scale,

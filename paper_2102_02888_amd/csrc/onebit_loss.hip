@@ -420,6 +420,7 @@ __global__ __launch_bounds__(TH, (kWavesFor<TH>)) void k_logprobs_grad(const T *
     const bool zero = !on || sum == 0.f;
     const float a = zero ? 0.f : -g * in.scale / sum, one = zero ? 0.f : g * in.scale;
     const float b = ENT && grad_entropy && !zero ? -grad_entropy[r] * in.scale / sum : 0.f;
+    const float nothing = (a - a) + (b - b);  // where p is 0: NaN in a row that is NaN
     row.each([&](float(&x)[kCols], int v) {
         if (v >= in.vocab) return;
 #pragma unroll
@@ -428,7 +429,7 @@ __global__ __launch_bounds__(TH, (kWavesFor<TH>)) void k_logprobs_grad(const T *
             const float e = __builtin_amdgcn_exp2f(d * c);
             if constexpr (ENT) {
                 const float more = __builtin_fmaf(b, d * in.scale - ln + entropy, a);
-                x[k] = zero || e == 0.f ? 0.f : e * more;
+                x[k] = zero || e == 0.f ? nothing : e * more;
             } else {
                 x[k] = zero ? 0.f : a * e;
             }

@@ -457,3 +457,28 @@ def test_nan_in_the_first_column_among_many_candidates(dev, vocab, kind):
         ob.onebit_logprobs_forward(x, None, None, top_ids=top, top_logprobs=logp)
         assert torch.equal(top, best[:, :k]), k
         assert bool(logp.isnan().all())
+
+
+@pytest.mark.parametrize("vocab", [9, 300, 3000, 30522, 40000, 70000])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_nan_takes_the_whole_row_of_a_gradient(dev, vocab, kind):
+    """A NaN or +infinity among a row's logits, or a NaN in what its values are weighted
+    with, makes all of its gradient NaN, with the entropy as without, also where p is 0
+    (masked or far below the largest).  Other rows with such places have numbers."""
+    import paper_2102_02888_amd as ob
+    nan = float("nan")
+    x = torch.randn(6, vocab, device=dev, generator=_gen(dev, 1))
+    x[:, 4], x[:, vocab - 2] = -INF, -500.0
+    x[0, 2], x[1, 3] = nan, INF
+    x = x.to(TYPES[kind])
+    ids = torch.full((6,), 1, device=dev)
+    g, h = torch.ones(6, device=dev), torch.ones(6, device=dev)
+    g[2], h[3] = nan, nan
+    d = torch.empty_like(x)
+    ob.onebit_logprobs_grad(x, ids, g, d)
+    assert d.isnan().all(1).tolist() == [True] * 3 + [False] * 3
+    assert not bool(d[3:].isnan().any())
+    for value in (None, torch.empty(6, device=dev)):
+        ob.onebit_logprobs_grad(x, ids, g, d, grad_entropy=h, entropy=value)
+        assert d.isnan().all(1).tolist() == [True] * 4 + [False] * 2
+        assert not bool(d[4:].isnan().any()) and not bool(d[4:, [4, vocab - 2]].any())
