@@ -509,8 +509,9 @@ int onebit_muon_step(onebit_matrices mats, float *x, float *m, const void *grads
  * Element types are ONEBIT_GRAD_*; pointers and leading dimensions need no
  * alignment beyond the element's own.  Statistics and sums are fp32, the mean being
  * taken twice, so that rows far off zero lose nothing; results are rounded once.
- * A NaN or an infinity in a row makes that row NaN.  width is at most 16,384;
- * rows = 0 and width = 0 are allowed. */
+ * A NaN or an infinity in a row makes that row NaN, as does a sum of its numbers past
+ * fp32's range (that of their squares may be).  width is at most 16,384; rows = 0 and
+ * width = 0 are allowed. */
 
 /* Errors: EINVAL (null, rows below 0 or 2^31 and above, a width out of range, a
  * leading dimension below width with more than one row, unknown type, eps below 0 or

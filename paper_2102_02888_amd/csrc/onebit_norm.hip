@@ -68,7 +68,7 @@ __device__ __forceinline__ void fill_tail(int lane, int width, float value, floa
 // Turns a row into its differences from the mean, and gives 1 / sqrt(var + eps).
 // The mean is first rounded to fp32; the differences from that are exact or nearly so
 // where the mean is far above them, and their own mean is what it was off by.
-template <int L, int C>
+template <class T, int L, int C>
 __device__ __forceinline__ float centre(float (&x)[C][kCols], int lane, int width, float eps,
                                         float *lds)
 {
@@ -92,11 +92,28 @@ __device__ __forceinline__ float centre(float (&x)[C][kCols], int lane, int widt
     add_lanes<L>(two, lds + L / 64);
     const float shift = two[0] / (float)width;
     const float var = __builtin_fmaf(-shift, shift, two[1] / (float)width);
+    float r = 1.f / sqrtf(fmaxf(var, 0.f) + eps);
+    // Squares past fp32's range, which no row of fp16 numbers has: once more of the
+    // differences times 2^-64.  (The sum's place is free again behind the second barrier.)
+    if (!std::is_same_v<T, _Float16> && __builtin_expect(two[1] == INFINITY, 0)) {
+        sum[0] = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int k = 0; k < kCols; ++k) {
+                const float d = x[c][k] * 0x1p-64f;
+                sum[0] = __builtin_fmaf(d, d, sum[0]);
+                asm volatile("" : "+v"(sum[0]));  // one at a time, for the registers
+            }
+        add_lanes<L>(sum, lds);
+        const float s = shift * 0x1p-64f, v = __builtin_fmaf(-s, s, sum[0] / (float)width);
+        r = 0x1p-64f / sqrtf(fmaxf(v, 0.f) + eps * 0x1p-128f);
+    }
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int k = 0; k < kCols; ++k) x[c][k] -= shift;
-    return 1.f / sqrtf(fmaxf(var, 0.f) + eps);
+    return r;
 }
 
 template <int L>
@@ -124,7 +141,7 @@ __global__ __launch_bounds__(kThreads<L>) void k_layer_norm(const T *__restrict_
          row += (int64_t)gridDim.x * kRows, turn ^= 1) {
         float v[C][kCols];
         load_row<L, C>(x + row * x_ld, lane, width, v);
-        const float r = centre<L, C>(v, lane, width, eps, lds[turn]);
+        const float r = centre<T, L, C>(v, lane, width, eps, lds[turn]);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int at = (c * L + lane) * kCols;
@@ -157,7 +174,7 @@ __global__ __launch_bounds__(kThreads<L>) void k_layer_norm_grad(
         float v[C][kCols], g[C][kCols];
         load_row<L, C>(x + row * x_ld, lane, width, v);
         load_row<L, C>(dy + row * dy_ld, lane, width, g);
-        const float r = centre<L, C>(v, lane, width, eps, lds[turn]);
+        const float r = centre<T, L, C>(v, lane, width, eps, lds[turn]);
         float two[2] = {0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < C; ++c)

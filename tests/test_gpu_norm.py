@@ -283,3 +283,33 @@ def test_refusals(dev):
         bwd(x, x, x, work[:64], w, w)
     with pytest.raises(TypeError, match="workspace"):
         bwd(x, x, x, None, w, w)
+
+
+@pytest.mark.parametrize("width", [40, 100, 400, 1000, 3001, 8000, 16384])
+def test_deviations_whose_squares_leave_fp32(dev, width):
+    """Rows of numbers up to 1e30 have squares past fp32's range, and a norm like any
+    other: the tolerance is that of any row.  One far off zero beside them, and an
+    ordinary one.  A row whose sum leaves fp32's range is NaN."""
+    import paper_2102_02888_amd as ob
+    x, dy = (torch.randn(6, width, device=dev, generator=_gen(dev, s)) for s in (1, 2))
+    x *= torch.tensor([1e17, 3e19, 1e25, 1e30, 1.0, 1.0], device=dev)[:, None]
+    x[2] += 1e30
+    x[5] = 3e38
+    y, dx, w = torch.empty_like(x), torch.empty_like(x), _vector(width, torch.float32, dev, 3, 1.0)
+    ob.onebit_layer_norm_forward(x, y, w)
+    z, r = _z(x[:5], 1e-5)
+    w64 = w.double()
+    tol = w64.abs() * (z.abs() + 1) * 6e-6 + (z * w64).abs() * 2.0 ** -22
+    assert bool(((y[:5].double() - z * w64).abs() <= tol).all())
+    assert bool(y[5].isnan().all())
+    dw = torch.empty_like(w)
+    ob.onebit_layer_norm_grad(dy[:5], x[:5], dx[:5], ob.layer_norm_workspace(5, width, dev), w, dw)
+    g = dy[:5].double() * w64
+    mg, mgz = g.mean(1, keepdim=True), (g * z).mean(1, keepdim=True)
+    want = r * (g - mg - z * mgz)
+    a, b = g.abs().mean(1, keepdim=True), (g * z).abs().mean(1, keepdim=True)
+    tol = 1e-5 * r * (g.abs() + a + (z.abs() + 1) * (a + b)) + want.abs() * 2.0 ** -24
+    assert bool(((dx[:5].double() - want).abs() <= tol + 2.0 ** -148).all())
+    terms = dy[:5].double() * z
+    tol = terms.abs().sum(0) * 45 * 2.0 ** -24 + 6e-6 * (dy[:5].double().abs() * (z.abs() + 1)).sum(0)
+    assert bool(((dw.double() - terms.sum(0)).abs() <= tol).all())
