@@ -26,6 +26,13 @@ from .onebit import Plan
 from .optimizer import OnebitAdam
 
 
+def _once(name):
+    """A gradient that is to be differentiated again is refused: the operators give none, and
+    autograd would leave that part of the second derivative out."""
+    if torch.is_grad_enabled():
+        raise RuntimeError("%s is not differentiable twice (create_graph)" % name)
+
+
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, workspace):
@@ -37,6 +44,7 @@ class _LayerNorm(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_y):
+        _once("layer norm")
         x, weight = ctx.saved_tensors
         grads = [torch.empty_like(t) for t in (x, weight, weight)]
         onebit_layer_norm_grad(grad_y.contiguous(), x, grads[0], ctx.workspace, weight, *grads[1:])
@@ -59,6 +67,7 @@ class _Attention(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_out):
+        _once("attention")
         sides, out, lse, starts = ctx.saved_tensors
         heads, grad = out.shape[1], torch.empty_like(sides)
         onebit_attention_grad(grad_out.to(out.dtype).contiguous().view(out.shape),

@@ -116,3 +116,20 @@ def test_a_step_runs_and_moves_every_parameter(dev, taught):
     assert all(0 < l < 20 for l in losses)
     for a, b in zip(old, _parameters64(model)):
         assert bool(torch.isfinite(b).all()) and not torch.equal(a, b)
+
+
+def test_second_derivatives_are_refused(dev):
+    """The operators' gradients are not differentiated further: what a second derivative
+    would need of them is not there, and leaving it out would pass for zero."""
+    from paper_2102_02888_amd.attention import attention_workspace
+    from paper_2102_02888_amd.lm_example import _Attention, _LayerNorm
+    from paper_2102_02888_amd.norm import layer_norm_workspace
+    g = torch.Generator(device=dev).manual_seed(3)
+    x = torch.randn(20, 3 * 32, device=dev, generator=g).requires_grad_()
+    w, b = torch.ones(96, device=dev), torch.zeros(96, device=dev)
+    starts = torch.tensor([0, 5, 20], dtype=torch.int32, device=dev)
+    for y in (_LayerNorm.apply(x, w, b, layer_norm_workspace(20, 96, dev)),
+              _Attention.apply(x, starts, 2, attention_workspace(20, 2, dev)).repeat(1, 3)):
+        with pytest.raises(RuntimeError, match="not differentiable twice"):
+            first = torch.autograd.grad((x * y).sum(), x, create_graph=True)[0]
+            torch.autograd.grad(first.square().sum(), x)
