@@ -399,3 +399,48 @@ def test_refusals(dev):
         bwd(q, q, k, k, q, lse, starts, q, k, k, work[:64])
     with pytest.raises(ValueError, match="grad_k is"):
         bwd(q, q, k, k, q, lse, starts, q, q, k, work)
+
+
+def _guarded(shape, dtype, dev, fill, inner):
+    """A tensor filled with `inner` inside a larger one filled with `fill`: (it, whole)."""
+    n = 1
+    for s in shape:
+        n *= s
+    whole = torch.full((n + 16384,), fill, dtype=dtype, device=dev)
+    whole[8192:8192 + n] = inner
+    return whole[8192:8192 + n].view(shape), whole
+
+
+def test_nothing_outside_the_tensors_with_starts_out_of_range(dev):
+    """Starts that decrease or lie outside the tokens: what lies around results, gradients
+    and workspace stays, NaN around the operands is not read; where the cut leaves no
+    token nothing is written, and ranges that are cut give the gradients of the cut ones."""
+    import paper_2102_02888_amd as ob
+    tokens, heads, dim = 100, 2, 32
+    nan = float("nan")
+
+    def calls(at):
+        s = torch.tensor(at, dtype=torch.int32, device=dev)
+        q, k, v, dout = (_guarded((tokens, heads, dim), torch.bfloat16, dev, nan, 0.0)[0] for _ in range(4))
+        for i, t in enumerate((q, k, v, dout)):
+            t.copy_(_side(tokens, heads, dim, torch.bfloat16, dev, 0, i))
+        results = [_guarded((tokens, heads, dim), torch.bfloat16, dev, 7.0, 7.0) for _ in range(4)]
+        results.append(_guarded((tokens, heads), torch.float32, dev, 7.0, 7.0))
+        need = ob.attention_workspace(tokens, heads, dev).numel()
+        work, whole = _guarded((need,), torch.uint8, dev, 0xA5, 0)
+        out, dq, dk, dv, lse = (t for t, _ in results)
+        ob.onebit_attention_forward(q, k, v, s, out, lse)
+        ob.onebit_attention_grad(dout, q, k, v, out, lse, s, dq, dk, dv, work)
+        for t, around in results:
+            n = t.numel()
+            assert bool((around[:8192] == 7.0).all()) and bool((around[8192 + n:] == 7.0).all()), at
+        assert bool((whole[:8192] == 0xA5).all()) and bool((whole[8192 + need:] == 0xA5).all()), at
+        return [t for t, _ in results]
+    want = calls([0, 40, 100])
+    assert not any(bool(t.isnan().any()) for t in want)
+    for a, b in zip(want, calls([-5, 40, 1 << 30])):
+        assert torch.equal(a, b)
+    for at in ([-7, -3], [200, 300], [2147483647, -2147483648], [100, 100], [0, 0]):
+        assert all(bool((t == 7.0).all()) for t in calls(at)), at
+    calls([90, 10, 50])
+    calls([60, 90, 30, 100, -4])
