@@ -619,7 +619,8 @@ int onebit_distill_grad(const void *logits, int32_t dtype, int64_t ld, int64_t r
  * with causal != 0:
  *   out_i = sum over j of P_ij v_j,  P_i = softmax over j of scale q_i k_j.
  * Scores, their exponentials and all sums are fp32, P and its gradient are rounded to
- * the operands' type between two products.  Tokens in no sequence are neither read
+ * the operands' type between two products, with ONEBIT_GRAD_F16 times powers of two, so
+ * that numbers far below the largest keep their bits.  Tokens in no sequence are neither read
  * nor written.  A NaN or an infinity among a sequence's numbers may make any result of
  * that sequence and head NaN; others are not touched by it.  A key whose score is below
  * fp32's range, -infinity, has no weight; a query that sees no other gets NaN. */

@@ -38,6 +38,15 @@ constexpr int kTile = 64;       // rows of the other side's tile in LDS
 constexpr int kMostDim = 128;
 constexpr int kMostParts = 1024;
 
+// fp16 ends at 2^-24, where a weight of one of many keys, or of one far behind another,
+// soon is.  Weights are brought up by powers of two before they are rounded to it:
+// forwards so that a query's largest is 2^kWeightUp or more, and below 2^(kWeightUp + 8);
+// backwards P itself, which is at most 1.
+template <class T>
+constexpr int kWeightUp = std::is_same_v<T, _Float16> ? 7 : 0;
+template <class T>
+constexpr int kPUp = std::is_same_v<T, _Float16> ? 15 : 0;
+
 __device__ __forceinline__ f32x16 mma(vec8<__bf16> a, vec8<__bf16> b, f32x16 c)
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -365,7 +374,8 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
         qf[d] = load8<DIRECT>(q + token * s.q_ld + head * s.dim, d * 16 + upper() * 8, s.dim, row < in.length);
     const float c = s.scale * kLog2e;
     f32x16 o[DP / 32] = {};
-    // (the maximum in base 2, finite from below: scores of -infinity have no weight)
+    // (the maximum in base 2, less kWeightUp; finite from below: scores of -infinity have
+    // no weight)
     float m = -FLT_MAX, l = 0.f;
     finish(stream * kTile, lds);
     __syncthreads();
@@ -394,8 +404,8 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
             for (int i = 0; i < 16; ++i) most = fmaxf(most, p[h][i]);
         most = both_halves(most, [](float x, float y) { return fmaxf(x, y); });
         // What is summed so far is brought to the new maximum only where that is
-        // 2^8 above the one in use: until then numbers grow to 2^8, and lose nothing.
-        most *= c;
+        // 2^8 above the one in use: until then numbers grow by 2^8, and lose nothing.
+        most = most * c - kWeightUp<T>;
         if (__ballot(most - m > 8.f)) {
             most = fmaxf(m, most);
             const float alpha = __builtin_amdgcn_exp2f(m - most);
@@ -657,7 +667,7 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
     const int begin = s.causal ? in.at / W::kStage * W::kStage : 0;
     const int per_head = (in.length - begin + W::kStage - 1) / W::kStage, steps = per_head * group;
     Loader<T, DP, W::kStage, WR, DIRECT> qt(wave % WR, s.q_ld, s.dim), dt(wave % WR, g.d_ld, s.dim);
-    // lse in base 2 and -D of a tile's queries lie behind the tiles
+    // lse in base 2 (less kPUp) and -D of a tile's queries lie behind the tiles
     const auto rows_of = [&](auto *buffer) {
         using F = std::conditional_t<std::is_const_v<std::remove_pointer_t<decltype(buffer)>>, const float, float>;
         return (F *)(buffer + W::kRowsAt) + stream * 2 * W::kStage;
@@ -673,7 +683,7 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
             const int row = at + wave % WR * 64 + (threadIdx.x & 63);
             const int64_t at_row = (int64_t)(in.first + row) * s.heads + head;
             // (behind the end: a score of 0 less infinity has no weight)
-            row_value[0] = row < in.length ? lse[at_row] * kLog2e : INFINITY;
+            row_value[0] = row < in.length ? lse[at_row] * kLog2e - kPUp<T> : INFINITY;
             row_value[1] = row < in.length ? -delta[at_row] : 0.f;
         }
     };
@@ -688,7 +698,7 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
         }
     };
     start(stream, lds);
-    const float grow = gradient_scale<T>(parts, g.parts);
+    const float grow = gradient_scale<T>(parts, g.parts) * (1.f / (1 << kPUp<T>));
     const int row = row0 + column();
     const int64_t token = in.first + row;
     vec8<T> kf[DP / 16], vf[DP / 16];
@@ -771,8 +781,9 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
         join(dva);
     }
     if (stream > 0 || row >= in.length) return;
-    store_column<DIRECT, T, DP>(dk + token * g.dk_ld + kv * s.dim, dka, s.scale / grow, s.dim);
-    store_column<DIRECT, T, DP>(dv + token * g.dv_ld + kv * s.dim, dva, 1.f, s.dim);
+    constexpr float kBack = 1.f / (1 << kPUp<T>);
+    store_column<DIRECT, T, DP>(dk + token * g.dk_ld + kv * s.dim, dka, s.scale / grow * kBack, s.dim);
+    store_column<DIRECT, T, DP>(dv + token * g.dv_ld + kv * s.dim, dva, kBack, s.dim);
 }
 
 template <class F>
