@@ -620,9 +620,9 @@ int onebit_distill_grad(const void *logits, int32_t dtype, int64_t ld, int64_t r
  *   out_i = sum over j of P_ij v_j,  P_i = softmax over j of scale q_i k_j.
  * Scores, their exponentials and all sums are fp32, P and its gradient are rounded to
  * the operands' type between two products, with ONEBIT_GRAD_F16 times powers of two, so
- * that numbers far below the largest keep their bits.  Tokens in no sequence are neither read
- * nor written.  A NaN or an infinity among a sequence's numbers may make any result of
- * that sequence and head NaN; others are not touched by it.  A key whose score is below
+ * that numbers far below the largest keep their bits.  Tokens in no sequence are neither
+ * read nor written.  A NaN or an infinity among a sequence's numbers may make any result
+ * of that sequence and head NaN; others are not touched by it.  A key whose score is below
  * fp32's range, -infinity, has no weight; a query that sees no other gets NaN. */
 
 /* lse (may be NULL): tokens x heads floats, the logarithm of the sum over j of
@@ -646,8 +646,9 @@ int onebit_attention_grad_workspace(int64_t tokens, int32_t heads, size_t *bytes
  *   dk_j = scale sum over i of dS_ij q_i,
  * dk and dv over all heads that share them.  out and lse are the forward call's.  No
  * atomics: results are the same bit for bit from call to call.  With ONEBIT_GRAD_F16
- * dS is scaled by a power of two from the largest magnitude in dout before it is
- * rounded.  dq, dk, dv: of the same type, written for the tokens of the sequences; they
+ * the power of two of dS is each query's own (for dk each key's), from the largest that
+ * it meets, so that a sequence's gradients do not depend on what it is packed with.
+ * dq, dk, dv: of the same type, written for the tokens of the sequences; they
  * may be parts of one buffer's rows.  workspace: 16-byte aligned.  Errors: as above. */
 int onebit_attention_grad(const void *dout, int64_t dout_ld, const void *q, int64_t q_ld,
                           const void *k, int64_t k_ld, const void *v, int64_t v_ld,

@@ -81,7 +81,7 @@ def attention_workspace(tokens, heads, device):
     """Workspace of onebit_attention_grad for at most this many tokens and heads."""
     n = ctypes.c_size_t()
     call("onebit_attention_grad_workspace", int(tokens), int(heads), ctypes.byref(n))
-    return torch.empty(n.value, dtype=torch.uint8, device=device)
+    return torch.empty(max(n.value, 256), dtype=torch.uint8, device=device)
 
 
 def onebit_attention_grad(grad_out, q, k, v, out, lse, starts, grad_q, grad_k, grad_v, workspace,

@@ -36,7 +36,7 @@ constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kTile = 64;       // rows of the other side's tile in LDS
 constexpr int kMostDim = 128;
-constexpr int kMostParts = 1024;
+constexpr int kMostDeltaBlocks = 1024;
 
 // fp16 ends at 2^-24, where a weight of one of many keys, or of one far behind another,
 // soon is.  Weights are brought up by powers of two before they are rounded to it:
@@ -477,20 +477,16 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
 // 64: D 23 us, dk and dv 220 (128 queries at once; 64: 235), dq 131.
 // ---------------------------------------------------------------------------
 
-// D of each token and head, by 8 lanes; with fp16 also the largest finite magnitude in
-// the workgroup's dout, by which dS is scaled before it is rounded (fp16 has no room for
-// gradients of 1e-6 and less).  Tokens outside the sequences are not looked at.
+// D of each token and head, by 8 lanes.  Tokens outside the sequences are not looked at.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_attention_delta(const T *__restrict__ dout,
                                                               int64_t d_ld,
                                                               const T *__restrict__ out, Sides s,
-                                                              float *__restrict__ delta,
-                                                              float *__restrict__ parts)
+                                                              float *__restrict__ delta)
 {
     const auto start = [&](int k) { return (int64_t)min(max(s.starts[k], 0), s.tokens); };
     const int64_t begin = start(0) * s.heads, rows = start(s.sequences) * s.heads;
     const int lane = threadIdx.x & 7;
-    float most = 0.f;
     for (int64_t r = begin + (int64_t)blockIdx.x * (kThreads / 8) + threadIdx.x / 8; r < rows;
          r += (int64_t)gridDim.x * (kThreads / 8)) {
         const int64_t token = r / s.heads;
@@ -500,51 +496,66 @@ __global__ __launch_bounds__(kThreads) void k_attention_delta(const T *__restric
         for (int at = lane * 8; at < s.dim; at += 64) {
             const vec8<T> x = load8<false>(a, at, s.dim, true), y = load8<false>(b, at, s.dim, true);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                sum = __builtin_fmaf((float)x[k], (float)y[k], sum);
-                if constexpr (std::is_same_v<T, _Float16>)
-                    if (fabsf((float)x[k]) < INFINITY) most = fmaxf(most, fabsf((float)x[k]));
-            }
+            for (int k = 0; k < 8; ++k) sum = __builtin_fmaf((float)x[k], (float)y[k], sum);
         }
         sum = over_lanes<8>(sum, [](float x, float y) { return x + y; });
         if (lane == 0) delta[r] = sum;
     }
+}
+
+// dS on its way to fp16, whose numbers span 2^-24 to 2^16: a lane's column (a query's for
+// dq, a key's for dk) is rounded times a power of two of its own, by which the largest that
+// it has met is 2^7 or more and none above 2^15.  It is lowered, with what is summed so
+// far, where a larger one comes; a column of zeros keeps the first.
+constexpr float kFirstGrow = 0x1p100f;
+
+template <class T, int N>
+__device__ __forceinline__ void grow_to_range(f32x16 &ds, float &grow, f32x16 (&acc)[N])
+{
     if constexpr (std::is_same_v<T, _Float16>) {
-        __shared__ float s_most[kWaves];
-        most = over_lanes<64>(most, [](float x, float y) { return fmaxf(x, y); });
-        if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = most;
-        __syncthreads();
-        if (threadIdx.x == 0)
-            parts[blockIdx.x] = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
+        float most = fabsf(ds[0]);
+#pragma unroll
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, fabsf(ds[i]));
+        most = both_halves(most, [](float x, float y) { return fmaxf(x, y); });
+        if (__ballot(most * grow > 0x1p15f)) {
+            const int old = (int)(__builtin_bit_cast(uint32_t, grow) >> 23);
+            const int now = min(old, 261 - (int)(__builtin_bit_cast(uint32_t, most) >> 23));
+            grow = __builtin_bit_cast(float, (uint32_t)now << 23);
+#pragma unroll
+            for (int d = 0; d < N; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[d][i] = ldexpf(acc[d][i], now - old);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ds[i] *= grow;
     }
 }
 
-// The power of two that brings the largest magnitude in dout (2^-24 to 2^16) to 2^-5 ..
-// 2^-4, for fp16: dS then stays in range for values of v up to some thousands, and its
-// step is 2^-20 of that.
-template <class T>
-__device__ __forceinline__ float gradient_scale(const float *__restrict__ parts, int n)
+// Takes the factor out of what a lane has summed, before streams of waves with other ones
+// add to it.
+template <class T, int N>
+__device__ __forceinline__ void ungrow(float &grow, f32x16 (&acc)[N])
 {
-    if constexpr (!std::is_same_v<T, _Float16>) return 1.f;
-    float most = 0.f;
-    for (int k = threadIdx.x & 63; k < n; k += 64) most = fmaxf(most, parts[k]);
-    most = over_lanes<64>(most, [](float x, float y) { return fmaxf(x, y); });
-    const int e = (int)(__builtin_bit_cast(uint32_t, most) >> 23);
-    return most > 0.f ? __builtin_bit_cast(float, (uint32_t)(249 - e) << 23) : 1.f;
+    if constexpr (std::is_same_v<T, _Float16>) {
+        const float back = 1.f / grow;
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] *= back;
+        grow = 1.f;
+    }
 }
 
 // The sides of a backward call.
 struct Grads {
     int64_t d_ld, dq_ld, dk_ld, dv_ld;
-    int parts;
 };
 
 template <class T, int DP, int WR, int NB, bool DIRECT>
 __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_attention_dq(
     const T *__restrict__ dout, const T *__restrict__ q, const T *__restrict__ k,
     const T *__restrict__ v, Sides s, Grads g, const float *__restrict__ lse,
-    const float *__restrict__ delta, const float *__restrict__ parts, T *__restrict__ dq,
-    int tiles)
+    const float *__restrict__ delta, T *__restrict__ dq, int tiles)
 {
     using W = Share<DP, WR, NB, kTile>;
     const Tile<T, DP> tile_at;
@@ -570,7 +581,7 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
         vt.finish(to + other);
     };
     start(stream * kTile, lds);
-    const float grow = gradient_scale<T>(parts, g.parts);
+    float grow = std::is_same_v<T, _Float16> ? kFirstGrow : 1.f;
     const int row = row0 + column();
     const int64_t token = in.first + row;
     const bool there = row < in.length;
@@ -601,15 +612,15 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
                 dp = mma(tile_at.rows(from + other, h * 32, d), df[d], dp);
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -l2)) * (dp[i] * grow);
-            }
+            for (int i = 0; i < 16; ++i)
+                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -l2)) * dp[i];
             if (masked) {
                 asm volatile("");
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) >= end) p[i] = 0.f;
             }
+            grow_to_range<T>(p, grow, acc);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const vec8<T> pf = narrow<T>(p, half);
@@ -636,12 +647,14 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
         if ((at += kStep) >= end) break;
         step(at, lds2, lds);
     }
-    if constexpr (W::kStreams > 1)
+    if constexpr (W::kStreams > 1) {
+        ungrow<T>(grow, acc);
         join_streams<WR, DP / 2>(lds, stream, wave % WR, [&](int k) { return acc[k / 16][k % 16]; },
             [&](auto number) {
 #pragma unroll
                 for (int k = 0; k < DP / 2; ++k) acc[k / 16][k % 16] += number(k);
             });
+    }
     if (stream == 0 && there)
         store_column<DIRECT, T, DP>(dq + token * g.dq_ld + head * s.dim, acc, s.scale / grow, s.dim);
 }
@@ -650,8 +663,7 @@ template <class T, int DP, int WR, int NB, bool DIRECT>
 __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_attention_dkv(
     const T *__restrict__ dout, const T *__restrict__ q, const T *__restrict__ k,
     const T *__restrict__ v, Sides s, Grads g, const float *__restrict__ lse,
-    const float *__restrict__ delta, const float *__restrict__ parts, T *__restrict__ dk,
-    T *__restrict__ dv, int tiles)
+    const float *__restrict__ delta, T *__restrict__ dk, T *__restrict__ dv, int tiles)
 {
     using W = Share<DP, WR, NB, WR == 4 && DP <= 64 ? 2 * kTile : kTile>;
     const Tile<T, DP> tile_at;
@@ -698,7 +710,7 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
         }
     };
     start(stream, lds);
-    const float grow = gradient_scale<T>(parts, g.parts) * (1.f / (1 << kPUp<T>));
+    float grow = std::is_same_v<T, _Float16> ? kFirstGrow : 1.f;
     const int row = row0 + column();
     const int64_t token = in.first + row;
     vec8<T> kf[DP / 16], vf[DP / 16];
@@ -728,7 +740,7 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
             for (int i = 0; i < 16; ++i) {
                 const int r = h * 32 + upper() * 4 + i % 4 + 8 * (i / 4);
                 p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], c, -of_rows[r]));
-                dp[i] = p[i] * (dp[i] * grow);
+                dp[i] *= p[i];
             }
             if (masked) {
                 asm volatile("");
@@ -736,6 +748,7 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
                 for (int i = 0; i < 16; ++i)
                     if (at + h * 32 + upper() * 4 + i % 4 + 8 * (i / 4) < row) p[i] = 0.f, dp[i] = 0.f;
             }
+            grow_to_range<T>(dp, grow, dka);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const vec8<T> pf = narrow<T>(p, half), sf = narrow<T>(dp, half);
@@ -776,6 +789,7 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
                     for (int k = 0; k < DP / 2; ++k) acc[k / 16][k % 16] += number(k);
                 });
         };
+        ungrow<T>(grow, dka);
         join(dka);
         __syncthreads();
         join(dva);
@@ -872,7 +886,7 @@ constexpr int kFewQueryTiles = 255, kFewKeyTiles = 320;
 
 int delta_blocks(int64_t tokens, int heads)
 {
-    return (int)std::min<int64_t>((tokens * heads + kThreads / 8 - 1) / (kThreads / 8), kMostParts);
+    return (int)std::min<int64_t>((tokens * heads + kThreads / 8 - 1) / (kThreads / 8), kMostDeltaBlocks);
 }
 
 }  // namespace
@@ -919,7 +933,7 @@ int onebit_attention_grad_workspace(int64_t tokens, int32_t heads, size_t *bytes
     if (!bytes) return fail(ONEBIT_EINVAL, "bytes is NULL");
     if (tokens < 0 || tokens > (1 << 30) || heads < 1 || heads > (1 << 14))
         return fail(ONEBIT_EINVAL, "%lld tokens, %d heads", (long long)tokens, heads);
-    *bytes = ((size_t)kMostParts + (size_t)tokens * heads) * sizeof(float);
+    *bytes = (size_t)tokens * heads * sizeof(float);
     return ONEBIT_OK;
 }
 
@@ -953,13 +967,13 @@ int onebit_attention_grad(const void *dout, int64_t dout_ld, const void *q, int6
     }
     const Sides s{q_ld, k_ld, v_ld, out_ld, starts, (int)tokens, (int)sequences,
                   heads, kv_heads, dim, scale, causal};
-    const Grads g{dout_ld, dq_ld, dk_ld, dv_ld, delta_blocks(tokens, heads)};
-    float *parts = (float *)workspace, *delta = parts + kMostParts;
+    const Grads g{dout_ld, dq_ld, dk_ld, dv_ld};
+    float *delta = (float *)workspace;
     hipStream_t st = (hipStream_t)stream;
     with_half(dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        k_attention_delta<T><<<g.parts, kThreads, 0, st>>>((const T *)dout, dout_ld,
-                                                           (const T *)out, s, delta, parts);
+        k_attention_delta<T><<<delta_blocks(tokens, heads), kThreads, 0, st>>>(
+            (const T *)dout, dout_ld, (const T *)out, s, delta);
         with_shape(dim, few_tiles(tokens, sequences, kv_heads, kFewKeyTiles),
                    direct_side(q, q_ld, dim) && direct_side(dout, dout_ld, dim),
                    [&](auto padded, auto waves, auto depth, auto direct) {
@@ -967,7 +981,7 @@ int onebit_attention_grad(const void *dout, int64_t dout_ld, const void *q, int6
             k_attention_dkv<T, padded(), waves(), depth(), direct()>
                 <<<tiles * kv_heads, kThreads, 0, st>>>(
                     (const T *)dout, (const T *)q, (const T *)k, (const T *)v, s, g, lse, delta,
-                    parts, (T *)dk, (T *)dv, tiles);
+                    (T *)dk, (T *)dv, tiles);
         });
         with_shape(dim, few_tiles(tokens, sequences, heads, kFewQueryTiles),
                    direct_side(k, k_ld, dim) && direct_side(v, v_ld, dim),
@@ -976,7 +990,7 @@ int onebit_attention_grad(const void *dout, int64_t dout_ld, const void *q, int6
             k_attention_dq<T, padded(), waves(), depth(), direct()>
                 <<<tiles * heads, kThreads, 0, st>>>(
                     (const T *)dout, (const T *)q, (const T *)k, (const T *)v, s, g, lse, delta,
-                    parts, (T *)dq, tiles);
+                    (T *)dq, tiles);
         });
     });
     return launched("attention gradient launch");

@@ -78,7 +78,7 @@ def _check(dev, q, k, v, dout, at, causal, scale=None):
     ob.onebit_attention_grad(dout, q, k, v, out, lse, starts, *grads, ob.attention_workspace(tokens, heads, dev),
                              causal=causal, scale=scale)
     want, tol = _reference(q, k, v, dout, at, causal, scale)
-    for name, t in (("out", out), ("dv", grads[2])):
+    for name, t in zip(("out", "dq", "dk", "dv"), (out, *grads)):
         held = want[name].abs() < 6e4  # (a result of 65,520 and more is infinity in fp16)
         ratio = torch.where(held, (t.double() - want[name]).abs() / tol[name], 0.0)
         assert bool((ratio <= 1).all()), (name, float(ratio.max()))
@@ -88,6 +88,48 @@ def _check(dev, q, k, v, dout, at, causal, scale=None):
 def _operands(dev, tokens, heads, kv, dim):
     return [torch.randn(tokens, h, dim, device=dev, generator=_gen(dev, s)).half()
             for s, h in enumerate((heads, kv, kv, heads))]
+
+
+@pytest.mark.parametrize("lengths,heads,kv,dim", [([300, 700, 90], 4, 2, 64), ([300, 700, 90], 4, 1, 40),
+                                                  ([257, 64, 130], 64, 64, 64), ([257, 64, 130], 120, 60, 80),
+                                                  ([300, 500], 2, 2, 128), ([130, 200, 3], 120, 120, 128),
+                                                  ([150, 200], 2, 1, 33)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_gradients_of_different_size_in_one_call(dev, lengths, heads, kv, dim, causal):
+    """Sequences whose gradients differ by 1e4 and heads whose differ by 30: each has its
+    own, within what its own size leaves, and the same bits as in a call of its own
+    sizes whatever it is packed with."""
+    import paper_2102_02888_amd as ob
+    at = [0]
+    for n in lengths:
+        at.append(at[-1] + n)
+    q, k, v, dout = _operands(dev, at[-1], heads, kv, dim)
+    for n, (a, b) in enumerate(zip(at, at[1:])):
+        dout[a:b] *= (300.0, 0.03, 10.0)[n]
+    dout[:, 1::2] *= 1 / 30
+    out, grads = _check(dev, q, k, v, dout, at, causal)
+    dout[:lengths[0]] *= 2.0 ** -14  # another neighbour: the second sequence stays as it is
+    lse, starts = torch.empty(at[-1], heads, device=dev), torch.tensor(at, dtype=torch.int32, device=dev)
+    ob.onebit_attention_forward(q, k, v, starts, out, lse, causal=causal)
+    others = [torch.empty_like(t) for t in grads]
+    ob.onebit_attention_grad(dout, q, k, v, out, lse, starts, *others,
+                             ob.attention_workspace(at[-1], heads, dev), causal=causal)
+    for x, y in zip(grads, others):
+        assert torch.equal(x[at[1]:], y[at[1]:])
+
+
+@pytest.mark.parametrize("heads", [1, 300])
+def test_values_near_the_largest_number(dev, heads):
+    """dP of up to 128 * 6e4: dS is far outside fp16, its products with small keys and
+    queries are not."""
+    q, k, v, dout = _operands(dev, 44, heads, heads, 128)
+    q *= 1e-3
+    k *= 1e-3
+    v[:4] = 6e4
+    v[0:4:2] *= -1
+    dout *= 0.1
+    dout[:4] = 1.0
+    _check(dev, q, k, v, dout, [0, 2, 4, 44], False)
 
 
 @pytest.mark.parametrize("n,heads", [(4096, 1), (1500, 40)])
