@@ -330,9 +330,11 @@ __device__ __forceinline__ void join_streams(char *lds, int stream, int row_wave
 
 // out = softmax(scale q k') v for 32 queries of a wave, one pass over the keys with a
 // running maximum m and sum l per query (both halves of a wave have a query; m is the
-// same in both, l adds up at the end).  The matrix cores and the VALU take turns on a
-// SIMD, and bound it together: packed prompts of up to 8,192 tokens, 16 heads on 4 of 128,
-// 375 to 390 us (1.0 PFLOP/s), 64 sequences of 512 with 16 heads of 64, not causal, 105 us (0.65).
+// same in both, l adds up at the end).  The matrix cores and the VALU bound it, busy 54% and
+// 43% of the time and hardly ever together, although a SIMD can run products of one wave
+// beside another wave's exponentials: packed prompts of up to 8,192 tokens, 16 heads on 4 of
+// 128, 385 to 405 us (0.95 PFLOP/s), 64 sequences of 512 with 16 heads of 64, not causal,
+// 106 us (0.65).
 // Four waves with 32 rows each, four workgroups a CU with heads of 64: with 64 rows a wave
 // and half the LDS reads 192 us, with tiles of 128 keys and two workgroups 129.
 template <class T, int DP, int WR, int NB, bool DIRECT>
@@ -474,7 +476,8 @@ __global__ __launch_bounds__(kThreads, (WR == 1 && DP > 64 ? 1 : 2)) void k_atte
 // One kernel for D, one for dk and dv, whose workgroups own keys and go through the
 // queries of all heads that share them, and one for dq, whose workgroups own queries:
 // seven products instead of five, and no atomics.  64 sequences of 512 with 16 heads of
-// 64: D 23 us, dk and dv 220 (128 queries at once; 64: 235), dq 131.
+// 64: D 23 us, dk and dv 223 (128 queries at once; 64: 235), dq 138; in fp16 23, 233 to
+// 253 and 144 to 159.
 // ---------------------------------------------------------------------------
 
 // D of each token and head, by 8 lanes.  Tokens outside the sequences are not looked at.

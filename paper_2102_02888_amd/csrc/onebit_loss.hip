@@ -191,7 +191,11 @@ __device__ __forceinline__ void statistics(Row &row, float c, Shared<TH> &s, flo
 // Top alternatives.  A key orders by the logit, then the lowest column first; NaN is
 // above all numbers.  The largest logits of 128 (64) groups of threads are known; the
 // k-th largest of those bounds the row's k-th largest from below, and little more than
-// k logits reach it unless many are equal.  Those are gathered and ranked.
+// k logits reach it unless many are equal or fewer than k groups hold a finite one.  Those
+// are gathered and ranked; too many of them are taken one by one, each by a pass over the
+// row (4,096 rows of 30,522 bf16 logits, 20 alternatives: 80 us, of equal logits or all but
+// three masked 1,490; of 1,000, whose groups are fewer than 64 alternatives, 274, of 1,100
+// 35).
 // ---------------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t order_of(float x)
@@ -330,8 +334,9 @@ struct Values {
     int top, top_bytes;
 };
 
-// 4,096 rows of 30,522 bf16 logits (a floor of 37 us): the log-probabilities 54 us, with
-// entropies and 20 alternatives 87, bounded by the VALU, which is busy 93% of the time.
+// 4,096 rows of 30,522 bf16 logits (a floor of 37 us): the log-probabilities 45 us, with
+// entropies 54, with 20 alternatives too 86, bounded by the VALU, which is busy 89% of the
+// time.
 template <class T, int TH, int C, bool ENT, bool TOP>
 __global__ __launch_bounds__(TH, (kWavesFor<TH>)) void k_logprobs(const T *__restrict__ logits, Logits in,
                                                  const void *__restrict__ ids, int ids_bytes,
@@ -378,7 +383,7 @@ __global__ __launch_bounds__(TH, (kWavesFor<TH>)) void k_logprobs(const T *__res
 
 // dx_v = scale (g ([v = t] - p_v) - h p_v (log p_v + entropy)); a row without a token
 // or without a distribution gets zeros.  8,192 rows of 30,522 bf16 logits (1 GB) take 175
-// us (5.7 TB/s).
+// us (5.7 TB/s), with the entropy's gradient 208.
 template <class T, int TH, int C, bool ENT>
 __global__ __launch_bounds__(TH, (kWavesFor<TH>)) void k_logprobs_grad(const T *logits, Logits in,
                                                       const void *__restrict__ ids, int ids_bytes,
@@ -465,7 +470,8 @@ __device__ __forceinline__ float load_teacher(const Teacher &t, int64_t at)
 // dx_v = g scale ((sum of q) p_v - sum of q_k over id_k = v).  A thread brings an
 // alternative to LDS and, once the row is written, sets the column that it names; the
 // first wave makes the teacher's softmax and the loss of them.  8,192 rows of 30,522 bf16
-// logits with 64 alternatives and the gradient take 214 us, 39 more than without a teacher.
+// logits with 64 alternatives and the gradient take 215 us, 39 more than without a teacher;
+// the loss alone 113.
 template <class T, int TH, int C, bool GRAD>
 __global__ __launch_bounds__(TH, (kWavesFor<TH>)) void k_distill(const T *logits, Logits in, Teacher t,
                                                 const float *__restrict__ grad_loss, T *dlogits,
@@ -564,7 +570,8 @@ __global__ __launch_bounds__(TH, (kWavesFor<TH>)) void k_distill(const T *logits
 // 1,024 threads, from registers and from memory (a floor of 74 for reading, 147 with the
 // gradient): 8,192 rows of 30,522 bf16 logits 109 and 128, gradient 186 and 295,
 // distillation 215 and 319; 4,096 rows of 30,522 fp32 ones 80 and 80, 236 and 233, 341
-// and 247 (half the row's registers are left, and two workgroups no longer fit a CU).
+// and 247 (half the row's registers are left, and two workgroups no longer fit a CU; LDS,
+// of which 5 of 160 KB are used, could hold part of such a row, and does not).
 // 8,192 rows of 9,000 bf16 ones 76 with 1,024 threads.
 template <class T, class F>
 void with_shape(int64_t vocab, F &&f)

@@ -122,7 +122,7 @@ constexpr int kThreads = L < 256 ? 256 : L;
 // y = (x - mean) r w + b, a row per L threads, weight and bias in registers over all rows
 // of a workgroup.  Memory bounds it: 131,072 bf16 rows of 1,024 (537 MB) take 90 us (5.9
 // TB/s; a copy of 8 GiB reaches 6.8), 10,007 fp32 rows of 771 to bf16 11 us (4.2 TB/s), 16
-// rows 3.7.
+// rows 3.8.
 template <class T, class O, int L, int C>
 __global__ __launch_bounds__(kThreads<L>) void k_layer_norm(const T *__restrict__ x, int64_t x_ld,
                                                       int64_t rows, int width,
@@ -155,8 +155,8 @@ __global__ __launch_bounds__(kThreads<L>) void k_layer_norm(const T *__restrict_
 // dx = r (g - mean(g) - z mean(g z)) with z = (x - mean) r and g = dy w, and the sums
 // of dy z and dy over the workgroup's rows, in registers until the last one.  Sums of
 // a column are added in an order that depends on the rows and the width alone.  Memory
-// bounds it: 131,072 bf16 rows of 1,024 (805 MB) take 152 us (5.3 TB/s), 10,007 fp32 rows
-// of 771 19.  Loading a row ahead costs a workgroup per CU in registers: 190 us.
+// bounds it: 131,072 bf16 rows of 1,024 (805 MB) take 155 us (5.2 TB/s), 10,007 fp32 rows
+// of 771 20, 8,192 bf16 rows of 16,384 220 (3.7).  Loading a row ahead costs a workgroup per CU in registers: 190 us.
 template <class D, class T, int L, int C>
 __global__ __launch_bounds__(kThreads<L>) void k_layer_norm_grad(
     const D *dy, int64_t dy_ld, const T *__restrict__ x, int64_t x_ld, int64_t rows,
