@@ -161,3 +161,52 @@ def test_many_keys_of_little_weight(dev, n, heads, dim):
     v[0] = 0.0
     dout *= 1e-2
     _check(dev, q, k, v, dout, [0, n], False, scale=1 / 8)
+
+
+@pytest.mark.parametrize("heads", [2, 300])
+@pytest.mark.parametrize("causal", [True, False])
+def test_no_gradient_and_some(dev, heads, causal):
+    """Gradients of nothing are nothing; with some queries that have none, the others' are
+    within their own size."""
+    import paper_2102_02888_amd as ob
+    q, k, v, dout = _operands(dev, 150, heads, heads, 64)
+    dout[:64] = 0.0
+    dout[100:130] = 0.0
+    _check(dev, q, k, v, dout, [0, 90, 91, 150], causal)
+    starts = torch.tensor([0, 90, 91, 150], dtype=torch.int32, device=dev)
+    out, lse = torch.empty_like(q), torch.empty(150, heads, device=dev)
+    ob.onebit_attention_forward(q, k, v, starts, out, lse, causal=causal)
+    grads = [torch.full_like(q, 7.0) for _ in range(3)]
+    ob.onebit_attention_grad(torch.zeros_like(dout), q, k, v, out, lse, starts, *grads,
+                             ob.attention_workspace(150, heads, dev), causal=causal)
+    assert not any(bool(g.any()) for g in grads)
+
+
+@pytest.mark.parametrize("heads", [4, 200])
+def test_nan_and_infinity_stay_in_their_sequence_and_head(dev, heads):
+    """Other sequences and heads have the same bits as without them."""
+    import paper_2102_02888_amd as ob
+    at = [0, 100, 230, 300]
+    starts = torch.tensor(at, dtype=torch.int32, device=dev)
+    work = ob.attention_workspace(300, heads, dev)
+
+    def calls(sides):
+        q, k, v, dout = sides
+        out, lse = torch.empty_like(q), torch.empty(300, heads, device=dev)
+        ob.onebit_attention_forward(q, k, v, starts, out, lse)
+        grads = [torch.empty_like(t) for t in (q, k, v)]
+        ob.onebit_attention_grad(dout, q, k, v, out, lse, starts, *grads, work)
+        return (out, *grads)
+    want = calls(_operands(dev, 300, heads, heads // 2, 64))
+    for bad in range(4):
+        for value in (float("nan"), float("inf"), -float("inf")):
+            sides = _operands(dev, 300, heads, heads // 2, 64)
+            sides[bad][150, 1, 3] = value
+            # head 1 of the queries, head 1 of the keys with heads 2 and 3 on it
+            touched = {heads: [1] if bad in (0, 3) else [2, 3], heads // 2: [0] if bad in (0, 3) else [1]}
+            for a, b in zip(want, calls(sides)):
+                clean = torch.ones(300, a.shape[1], dtype=torch.bool, device=dev)
+                for h in touched[a.shape[1]]:
+                    clean[100:230, h] = False
+                assert torch.equal(a[clean], b[clean]), (bad, value)
+                assert not bool(a.isnan().any())
